@@ -243,9 +243,9 @@ def _framework(s):
         s["turn"] = 1 - now
         if kind == "fork":
             apex4.apex4_pages_fork(s["pool"], s["table"], s["kv_len"], s["refs"], s["from"][now], s["halves"][1 - now], c["page"])
-            apex4.apex4_pages_free(s["table"], s["kv_len"], s["refs"], s["halves"][now], c["page"])
+            apex4.apex4_pages_free(s["table"], s["kv_len"], s["refs"], s["halves"][now])
         else:
-            apex4.apex4_pages_free(s["table"], s["kv_len"], s["refs"], s["halves"][now], c["page"])
+            apex4.apex4_pages_free(s["table"], s["kv_len"], s["refs"], s["halves"][now])
             apex4.apex4_pages_compact(s["pool"], s["table"], s["refs"])
             apex4.apex4_pages_reserve(s["table"], s["kv_len"], s["refs"], s["halves"][now], s["lens"][now], c["page"])
         return s["pool"], s["table"], s["kv_len"], s["refs"]
