@@ -399,6 +399,142 @@ int apex4_w4a4_gemm_mx_ws(const uint8_t* A_6, const uint8_t* e_a,
                           int64_t M, int64_t N, int64_t K, int64_t G,
                           void* Y, void* workspace, int64_t workspace_bytes, void* stream);
 
+/*
+ * Paged key-value cache and the attention that reads it: what stands between a
+ * decoder layer's qkv projection and its output projection.
+ *
+ * A plane (the keys, or the values, of one layer) is n_pages pages of
+ * apex4_kv_page_bytes bytes.  A page holds `page` tokens (16, 32, 64, 128, 256,
+ * 512 or 1024) of kv_heads heads of head_dim (64 or 128) values:
+ *   APEX4_KV_FP16: binary16 [kv_heads][page][head_dim];
+ *   APEX4_KV_INT4: codes [kv_heads][page][head_dim/2] in the packing above, then
+ *   binary16 scales [kv_heads][page]: SymQuant with G = head_dim, one scale for a
+ *   token's head (the codes and scales of apex4_quantize_act, bit for bit).
+ * Sequence b's token t is in page table[b * width + t / page], at t % page;
+ * kv_len[b] is its number of tokens, those of the current call included.
+ * New tokens are packed, sequence after sequence: q_start[0 .. B], ascending,
+ * q_start[0] = 0 and q_start[B] = T; where it may be NULL, that means one token
+ * a sequence (T = B).  New token i of the n of sequence b is at position
+ * kv_len[b] - n + i.
+ *
+ * int32 buffers need 4-byte alignment, all others 16-byte alignment.  Values in
+ * device memory cannot be validated: page ids outside [0, n_pages), lengths past
+ * width * page (or past max_len) and sequence numbers outside the table are never
+ * used as addresses.  append leaves out tokens that have no page, gather returns
+ * zeros for them, and attention to such positions is unspecified.
+ * Limits: n_pages, max_len up to 2^30, width up to 2^20, B and T up to 2^24,
+ * T heads up to 2^27.
+ */
+#define APEX4_KV_FP16 0
+#define APEX4_KV_INT4 1
+int apex4_kv_page_bytes(int cache, int64_t kv_heads, int64_t head_dim, int64_t page, int64_t* bytes);
+
+/*
+ * Writes new tokens' keys and values into the cache.
+ *   k, v: T rows of kv_heads * head_dim binary16, k_stride and v_stride elements
+ *   apart (multiples of 8; rows of a fused qkv projection can be passed as they
+ *   are).  Other bytes of the cache are left alone.
+ */
+int apex4_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* q_start, int64_t T,
+                    void* k_pages, void* v_pages, int64_t n_pages, const int32_t* table, int64_t width,
+                    const int32_t* kv_len, int64_t B, int64_t kv_heads, int64_t head_dim, int64_t page, int cache,
+                    void* stream);
+
+/*
+ * Reads the last n tokens of every sequence (n = q_start[b + 1] - q_start[b]) as
+ * binary16 into k, v [T, kv_heads, head_dim]; from an int4 cache, code times
+ * scale rounded once.
+ */
+int apex4_kv_gather(const void* k_pages, const void* v_pages, int64_t n_pages, const int32_t* table, int64_t width,
+                    const int32_t* kv_len, int64_t B, int64_t kv_heads, int64_t head_dim, int64_t page, int cache,
+                    const int32_t* q_start, int64_t T, void* k, void* v, void* stream);
+
+/*
+ * Attention of one new token a sequence (its key and value already in the
+ * cache) over the paged cache.
+ *   q [B, heads, head_dim] binary16, rows q_stride elements apart (a multiple of
+ *   8); out [B, heads, head_dim] binary16; heads a multiple of kv_heads, query
+ *   head j reads key head j / (heads / kv_heads).
+ *   out = sum_t w_t v_t / sum_t w_t,  w_t = exp(scale q.k_t - max_t scale q.k_t),
+ * over the positions t that the token at p = kv_len[b] - 1 sees: t <= p and,
+ * with window > 0, t > p - window or t < sinks (a sliding window, and first
+ * tokens that stay visible).  A sequence without tokens gets zeros.  Positions
+ * that are not seen may hold anything, NaN included.  Scores, weights' sums and
+ * output sums are binary32; the weights are rounded to binary16 (the products'
+ * operand), the result once.  scale: positive and finite.
+ *   max_len: a bound of kv_len known on the host (shorter: less to launch);
+ *   tokens past it are not seen.
+ *   workspace: apex4_attn_decode_workspace_size bytes (NULL where that is 0);
+ *   calls that share one must be ordered on one stream.
+ * Where the sequences are few, their length is split over workgroups and the
+ * parts are joined in order: deterministic for given arguments and a device.
+ */
+int apex4_attn_decode_workspace_size(int64_t B, int64_t width, int64_t max_len, int64_t heads, int64_t kv_heads,
+                                     int64_t head_dim, int64_t page, int64_t window, int64_t sinks, int64_t* bytes);
+int apex4_attn_decode(const void* q, int64_t q_stride, const void* k_pages, const void* v_pages, int64_t n_pages,
+                      const int32_t* table, int64_t width, const int32_t* kv_len, int64_t B, int64_t max_len,
+                      int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t page, int cache, int64_t window,
+                      int64_t sinks, float scale, void* out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The same for the packed new tokens of q_start (a prompt, a chunk of one, a few
+ * tokens at a time), each at its own position p: q, out [T, heads, head_dim].
+ *   max_q: a bound of the new tokens of a sequence; those past it get no output.
+ *   A token whose position is negative (more new tokens than kv_len) sees nothing
+ *   and gets zeros.  A value that is infinite or NaN reaches every new token of
+ *   its sequence for which its position lies in a tile with seen ones, also
+ *   those before it.
+ */
+int apex4_attn_prefill_workspace_size(int64_t T, int64_t B, int64_t max_q, int64_t width, int64_t max_len, int64_t heads,
+                                      int64_t kv_heads, int64_t head_dim, int64_t page, int64_t window, int64_t sinks,
+                                      int64_t* bytes);
+int apex4_attn_prefill(const void* q, int64_t q_stride, const int32_t* q_start, int64_t T, int64_t max_q,
+                       const void* k_pages, const void* v_pages, int64_t n_pages, const int32_t* table, int64_t width,
+                       const int32_t* kv_len, int64_t B, int64_t max_len, int64_t heads, int64_t kv_heads,
+                       int64_t head_dim, int64_t page, int cache, int64_t window, int64_t sinks, float scale, void* out,
+                       void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The cache's pages, managed on the device.  State: table [slots, width] (-1: no
+ * page), kv_len [slots], refs [n_pages] (how many table entries hold the page;
+ * 0: free).  Free pages are taken lowest first.  The pool is the planes of all
+ * layers, [planes][n_pages][page_bytes]; page_bytes a multiple of 16.
+ * seqs, parents, children: n slot numbers; ones outside the table are left out,
+ * and a call names no slot twice among those that it changes.
+ * status (int32) receives the outcome on the device.  workspace:
+ * apex4_pages_workspace_size(n_pages, n) bytes.
+ *
+ * reserve: gives slot seqs[i] the pages for new_len[i] tokens, in the order of
+ *   the list, and sets its kv_len (a smaller new_len changes nothing).  All or
+ *   nothing: status 0, or > 0 where free pages are too few, or -1 where a length
+ *   does not fit the table.
+ * fork: slot children[i] (empty) continues parents[i] (and is not a parent in
+ *   the same call): it shares the full pages, and gets a page of its own, with the
+ *   data copied, for the tokens of a partly filled last one, so that appending
+ *   never writes to a shared page.  All or nothing: status 0, or the number of
+ *   missing pages.
+ * free: gives back the slots' pages and empties them.
+ * compact: moves pages so that the live ones are 0 .. live - 1 (those past that
+ *   number, in ascending order, to the free ones below it) and updates table and
+ *   refs; status = live.
+ * copy: page src[i] to dst[i] in every plane; pairs outside the pool are left
+ *   out, and no page is a destination and also in another pair.
+ */
+int apex4_pages_workspace_size(int64_t n_pages, int64_t n, int64_t* bytes);
+int apex4_pages_reserve(int32_t* table, int64_t slots, int64_t width, int32_t* kv_len, int32_t* refs, int64_t n_pages,
+                        const int32_t* seqs, const int32_t* new_len, int64_t n, int64_t page, int32_t* status,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+int apex4_pages_fork(void* pool, int64_t planes, int64_t page_bytes, int32_t* table, int64_t slots, int64_t width,
+                     int32_t* kv_len, int32_t* refs, int64_t n_pages, const int32_t* parents, const int32_t* children,
+                     int64_t n, int64_t page, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
+int apex4_pages_free(int32_t* table, int64_t slots, int64_t width, int32_t* kv_len, int32_t* refs, int64_t n_pages,
+                     const int32_t* seqs, int64_t n, void* stream);
+int apex4_pages_compact(void* pool, int64_t planes, int64_t page_bytes, int32_t* table, int64_t slots, int64_t width,
+                        int32_t* refs, int64_t n_pages, int32_t* status, void* workspace, int64_t workspace_bytes,
+                        void* stream);
+int apex4_pages_copy(void* pool, int64_t planes, int64_t page_bytes, int64_t n_pages, const int32_t* src, const int32_t* dst,
+                     int64_t n, void* stream);
+
 /* Static description of a status code (never NULL). */
 const char* apex4_status_string(int status);
 

@@ -11,6 +11,10 @@ not gfx950 the call raises.
     P = apex4_w4a4_gemm_groupsums(A_q, W_q, G, m0, mr)  # int32 [mr, N, K/G]
     Y = apex4_w4a4_linear(x, W_q, s_w, G)               # quantize + GEMM
     lin = W4A4Linear(w, G); y = lin(x)                  # drop-in layer (weights quantized once)
+
+The paged key-value cache and the attention over it (``PagedKVCache`` and the
+``apex4_kv_*``, ``apex4_attn_*`` and ``apex4_pages_*`` calls) are in ``cache.py``
+and are names of this package too.
 """
 from __future__ import annotations
 
@@ -36,7 +40,10 @@ EXPORTED = ("apex4_quantize_act", "apex4_w4a4_gemm", "apex4_w4a4_gemm_groupsums"
             "apex4_w4a4_gemm_noalloc", "apex4_quantize_mx", "apex4_w4a4_gemm_mx",
             "apex4_w4a4_gemm_mx_workspace_size", "apex4_w4a4_gemm_mx_ws", "apex4_status_string",
             "apex4_version", "apex4_tiled_weights_size", "apex4_tile_weights", "apex4_w4a4_gemm_tiled",
-            "apex4_w4a4_linear_tiled", "apex4_w4a4_linear_ws")
+            "apex4_w4a4_linear_tiled", "apex4_w4a4_linear_ws", "apex4_kv_page_bytes", "apex4_kv_append",
+            "apex4_kv_gather", "apex4_attn_decode_workspace_size", "apex4_attn_decode",
+            "apex4_attn_prefill_workspace_size", "apex4_attn_prefill", "apex4_pages_workspace_size",
+            "apex4_pages_reserve", "apex4_pages_fork", "apex4_pages_free", "apex4_pages_compact", "apex4_pages_copy")
 
 _lib = None
 
@@ -78,12 +85,21 @@ def lib() -> ctypes.CDLL:
     L.apex4_w4a4_gemm_ws.argtypes = [P, P, P, P, I, I, I, I, P, P, I, P]
     L.apex4_w4a4_gemm_noalloc.argtypes = [P, P, P, P, I, I, I, I, P, P]
     L.apex4_w4a4_gemm_fp6.argtypes = [P, P, P, P, I, I, I, I, P, P]
-    for f in ("apex4_quantize_act", "apex4_w4a4_gemm", "apex4_w4a4_gemm_groupsums", "apex4_w4a4_gemm_debug",
-              "apex4_w4a4_gemm_plan", "apex4_w4a4_linear", "apex4_w4a4_linear_debug", "apex4_pack_fp6",
-              "apex4_w4a4_gemm_fp6", "apex4_w4a4_gemm_workspace_size", "apex4_w4a4_gemm_ws",
-              "apex4_w4a4_gemm_noalloc", "apex4_quantize_mx", "apex4_w4a4_gemm_mx",
-              "apex4_w4a4_gemm_mx_workspace_size", "apex4_w4a4_gemm_mx_ws", "apex4_tiled_weights_size",
-              "apex4_tile_weights", "apex4_w4a4_gemm_tiled", "apex4_w4a4_linear_tiled", "apex4_w4a4_linear_ws"):
+    C, F = ctypes.c_int, ctypes.c_float
+    L.apex4_kv_page_bytes.argtypes = [C, I, I, I, P]
+    L.apex4_kv_append.argtypes = [P, I, P, I, P, I, P, P, I, P, I, P, I, I, I, I, C, P]
+    L.apex4_kv_gather.argtypes = [P, P, I, P, I, P, I, I, I, I, C, P, I, P, P, P]
+    L.apex4_attn_decode_workspace_size.argtypes = [I] * 9 + [P]
+    L.apex4_attn_decode.argtypes = [P, I, P, P, I, P, I, P, I, I, I, I, I, I, C, I, I, F, P, P, I, P]
+    L.apex4_attn_prefill_workspace_size.argtypes = [I] * 11 + [P]
+    L.apex4_attn_prefill.argtypes = [P, I, P, I, I, P, P, I, P, I, P, I, I, I, I, I, I, C, I, I, F, P, P, I, P]
+    L.apex4_pages_workspace_size.argtypes = [I, I, P]
+    L.apex4_pages_reserve.argtypes = [P, I, I, P, P, I, P, P, I, I, P, P, I, P]
+    L.apex4_pages_fork.argtypes = [P, I, I, P, I, I, P, P, I, P, P, I, I, P, P, I, P]
+    L.apex4_pages_free.argtypes = [P, I, I, P, P, I, P, I, P]
+    L.apex4_pages_compact.argtypes = [P, I, I, P, I, I, P, I, P, P, I, P]
+    L.apex4_pages_copy.argtypes = [P, I, I, I, P, P, I, P]
+    for f in EXPORTED:
         getattr(L, f).restype = ctypes.c_int
     L.apex4_status_string.argtypes = [ctypes.c_int]
     L.apex4_status_string.restype = ctypes.c_char_p
@@ -569,3 +585,9 @@ class W4A4Linear:
                 xp, W.data_ptr(), self.s_w.data_ptr(), M, self.N, self.K, self.G, Y.data_ptr(), Aq.data_ptr(),
                 sa.data_ptr(), wsp, wsn, APEX4_DEBUG_W_TILED if self.tiled else 0, handle))
         return Y
+
+
+from .cache import (KV_CACHES, PagedKVCache, apex4_attn_decode, apex4_attn_decode_workspace_size,  # noqa: E402,F401
+                    apex4_attn_prefill, apex4_attn_prefill_workspace_size, apex4_kv_append, apex4_kv_gather,
+                    apex4_kv_page_bytes, apex4_pages_compact, apex4_pages_copy, apex4_pages_fork, apex4_pages_free,
+                    apex4_pages_reserve, apex4_pages_workspace_size)

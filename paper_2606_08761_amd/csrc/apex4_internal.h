@@ -9,6 +9,9 @@
 
 namespace apex4 {
 
+// APEX4_OK if the current device is gfx950, APEX4_ERR_DEVICE otherwise.
+int check_device();
+
 // Allows `bytes` of dynamic LDS for kernel k on the current device, once per
 // device: `done` (one per kernel, static at the call site) holds a bit per
 // device id below 64; a larger id sets the attribute on every call.
@@ -166,5 +169,79 @@ int64_t mx_splitk_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t G);
 hipError_t launch_gemm_mx_splitk(const uint8_t* A6, const uint8_t* ea, const uint8_t* W6, const uint8_t* ew,
                                  int64_t M, int64_t N, int64_t K, int64_t G, uint16_t* Y, float* part,
                                  hipStream_t stream);
+
+// A paged key-value cache as the kernels see it (layout: kv_cache.h).
+struct KvView {
+    const uint8_t* k = nullptr;       // planes of the keys and of the values
+    const uint8_t* v = nullptr;
+    const int32_t* table = nullptr;   // [B, width] page ids
+    const int32_t* kv_len = nullptr;  // [B] cached tokens, the new ones included
+    int64_t n_pages = 0;
+    int64_t page_bytes = 0;
+    int64_t max_len = 0;              // the caller's bound of kv_len
+    int width = 0;
+    int page_shift = 0;               // page = 1 << page_shift tokens
+    int B = 0;
+    int kv_heads = 0;
+    int D = 0;
+    bool i4 = false;
+};
+
+// New tokens' keys and values (rows of kv_heads * D binary16, `stride` elements
+// apart) into the cache, and back out of it (contiguous rows).
+hipError_t launch_kv_append(const KvView& c, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                            const int32_t* q_start, int64_t T, hipStream_t stream);
+hipError_t launch_kv_gather(const KvView& c, uint16_t* k, uint16_t* v, const int32_t* q_start, int64_t T,
+                            hipStream_t stream);
+
+// Attention over the cache.  q rows are heads * D binary16, q_stride elements
+// apart; out is [T, heads, D].  One new token a sequence (T = B), or the packed
+// tokens of q_start, at most max_q a sequence.
+struct AttnArgs {
+    const uint16_t* q = nullptr;
+    int64_t q_stride = 0;
+    const int32_t* q_start = nullptr;
+    int64_t T = 0;
+    int64_t max_q = 1;
+    int heads = 0;
+    int window = 0;                   // 0: none
+    int sinks = 0;
+    float scale = 1.f;
+    uint16_t* out = nullptr;
+    void* workspace = nullptr;
+};
+// Bytes of the parts when the cache's length is split (0: no split).
+int64_t attn_decode_workspace(const KvView& c, const AttnArgs& a);
+hipError_t launch_attn_decode(const KvView& c, const AttnArgs& a, hipStream_t stream);
+int64_t attn_prefill_workspace(const KvView& c, const AttnArgs& a);
+hipError_t launch_attn_prefill(const KvView& c, const AttnArgs& a, hipStream_t stream);
+
+// Joins parts of attention rows: part[row][S][D] float and ml[row][S][2] (the
+// running maximum in units of log2, and the sum) into out[row][D].
+hipError_t launch_attn_join(const float* part, const float* ml, int64_t rows, int S, int D, uint16_t* out,
+                            hipStream_t stream);
+
+// The page tables of a cache's sequence slots, their lengths and the pages'
+// reference counts (0: free), all device memory.
+struct PageTable {
+    int32_t* table = nullptr;   // [slots, width]
+    int32_t* kv_len = nullptr;  // [slots]
+    int32_t* refs = nullptr;    // [n_pages]
+    int slots = 0;
+    int width = 0;
+    int n_pages = 0;
+    int page_shift = 0;
+};
+// int32 words of scratch that each of the calls below with `work` may use.
+inline int64_t pages_work_words(int64_t n_pages, int64_t n) { return 3 * n_pages + 2 * n + 4; }
+hipError_t launch_pages_reserve(const PageTable& p, const int32_t* seqs, const int32_t* new_len, int n, int32_t* status,
+                                int32_t* work, hipStream_t stream);
+hipError_t launch_pages_fork(const PageTable& p, uint8_t* pool, int planes, int64_t page_bytes, const int32_t* parents,
+                             const int32_t* children, int n, int32_t* status, int32_t* work, hipStream_t stream);
+hipError_t launch_pages_free(const PageTable& p, const int32_t* seqs, int n, hipStream_t stream);
+hipError_t launch_pages_compact(const PageTable& p, uint8_t* pool, int planes, int64_t page_bytes, int32_t* status,
+                                int32_t* work, hipStream_t stream);
+hipError_t launch_pages_copy(uint8_t* pool, int planes, int64_t page_bytes, int n_pages, const int32_t* src,
+                             const int32_t* dst, int n, hipStream_t stream);
 
 }  // namespace apex4

@@ -20,21 +20,6 @@ constexpr int64_t kMaxChannelK = 65536;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-int check_device() {
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0) return APEX4_ERR_DEVICE;
-    if (dev < kMaxDevices) {
-        const int known = g_arch_ok[dev].load(std::memory_order_relaxed);
-        if (known == 1) return APEX4_OK;
-        if (known == -1) return APEX4_ERR_DEVICE;
-    }
-    hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return APEX4_ERR_DEVICE;
-    const bool ok = strncmp(prop.gcnArchName, "gfx950", 6) == 0;
-    if (dev < kMaxDevices) g_arch_ok[dev].store(ok ? 1 : -1, std::memory_order_relaxed);
-    return ok ? APEX4_OK : APEX4_ERR_DEVICE;
-}
-
 // Shape rules shared by the GEMM entry points.
 int check_gemm_shape(int64_t M, int64_t N, int64_t K) {
     if (M < 0 || N < 1 || K < 32 || (K % 32) != 0) return APEX4_ERR_SHAPE;
@@ -79,6 +64,25 @@ int check_gemm_args(const void* A_q, const void* s_a, const void* W_q, const voi
 }
 
 }  // namespace
+
+namespace apex4 {
+int check_device() {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0) return APEX4_ERR_DEVICE;
+    if (dev < kMaxDevices) {
+        const int known = g_arch_ok[dev].load(std::memory_order_relaxed);
+        if (known == 1) return APEX4_OK;
+        if (known == -1) return APEX4_ERR_DEVICE;
+    }
+    hipDeviceProp_t prop;
+    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return APEX4_ERR_DEVICE;
+    const bool ok = strncmp(prop.gcnArchName, "gfx950", 6) == 0;
+    if (dev < kMaxDevices) g_arch_ok[dev].store(ok ? 1 : -1, std::memory_order_relaxed);
+    return ok ? APEX4_OK : APEX4_ERR_DEVICE;
+}
+}  // namespace apex4
+
+using apex4::check_device;
 
 extern "C" {
 

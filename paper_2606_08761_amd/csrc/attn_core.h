@@ -1,0 +1,102 @@
+// What the attention kernels over the paged cache share: the tiles of positions
+// a range of rows sees, and the arithmetic of the 4-bit codes.
+#pragma once
+
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "apex4_internal.h"
+#include "kv_cache.h"
+
+namespace apex4 {
+namespace attn {
+namespace {   // internal linkage in every translation unit that includes it
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+// A running maximum that no finite score is below, and that leaves 2^(s - m)
+// zero, not NaN, where every score so far is masked (s = -inf).
+constexpr float kNoMax = -1e30f;
+// Scores may pass the running maximum by this much (in units of log2) before
+// the sums are rescaled: the weights stay below 2^8, exact enough in binary16,
+// and after the first tiles a rescale is rare.
+constexpr float kSlack = 8.f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Two weights rounded to binary16 (nearest even): their error of 2^-12 of a
+// weight stays below the output's own rounding.
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    f16x2 r;
+    r[0] = static_cast<_Float16>(a);
+    r[1] = static_cast<_Float16>(b);
+    return __builtin_bit_cast(uint32_t, r);
+}
+
+// Tiles of W positions that rows at positions p_lo .. p_hi see (causal, a
+// window of `window` positions up to the row's own unless it is 0, and the
+// first `sinks`): the tiles of the first positions, then from the window's
+// start on, as one list of `count` tiles.
+template <int W>
+struct Tiles {
+    int lo;        // first position the window of the lowest row reaches
+    int sinks;     // first positions visible besides
+    int n_sink;    // tiles of the list before the window's
+    int first;     // tile of the window's start
+    int count;
+    __device__ __forceinline__ Tiles(int p_lo, int p_hi, int window, int sinks_all) {
+        lo = window ? p_lo - window + 1 : 0;
+        lo = lo > 0 ? lo : 0;
+        sinks = sinks_all < lo ? sinks_all : lo;
+        first = lo / W;
+        n_sink = (sinks + W - 1) / W;
+        n_sink = n_sink < first ? n_sink : first;
+        count = p_hi < 0 ? 0 : n_sink + p_hi / W + 1 - first;
+    }
+    // position of the first token of tile i of the list
+    __device__ __forceinline__ int start(int i) const { return (i < n_sink ? i : first + i - n_sink) * W; }
+};
+
+// 4-bit codes as binary16 without a conversion: code + 8 in the low mantissa
+// bits of 1024 (bits 0-3 of a half), or of 1024 in steps of 16 (bits 4-7), then
+// one packed subtraction or fused multiply-add, exact.  The halves of r[i] are
+// codes i and i + 4 of x's 8.
+__device__ __forceinline__ void codes_f16(uint32_t x, uint32_t r[4]) {
+    x ^= 0x88888888u;
+    const uint32_t y = x >> 8;
+    const uint32_t a[4] = {(x & 0x000F000Fu) | 0x64006400u, (x & 0x00F000F0u) | 0x64006400u,
+                           (y & 0x000F000Fu) | 0x64006400u, (y & 0x00F000F0u) | 0x64006400u};
+    const f16x2 one = {static_cast<_Float16>(1032.f), static_cast<_Float16>(1032.f)};
+    const f16x2 six = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
+    const f16x2 off = {static_cast<_Float16>(-72.f), static_cast<_Float16>(-72.f)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f16x2 h = __builtin_bit_cast(f16x2, a[i]);
+        r[i] = __builtin_bit_cast(uint32_t, (i & 1) ? __builtin_elementwise_fma(h, six, off) : h - one);
+    }
+}
+
+// 8 binary16 values in the order codes_f16 leaves codes in.
+__device__ __forceinline__ u32x4 code_order(u32x4 w) {
+    u32x4 r;
+    r[0] = __builtin_amdgcn_perm(w[2], w[0], 0x05040100u);
+    r[1] = __builtin_amdgcn_perm(w[2], w[0], 0x07060302u);
+    r[2] = __builtin_amdgcn_perm(w[3], w[1], 0x05040100u);
+    r[3] = __builtin_amdgcn_perm(w[3], w[1], 0x07060302u);
+    return r;
+}
+
+// The low, or high, halves of two words side by side.
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+}  // namespace
+}  // namespace attn
+}  // namespace apex4
