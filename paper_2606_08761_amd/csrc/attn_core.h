@@ -28,6 +28,8 @@ constexpr float kNoMax = -1e30f;
 // the sums are rescaled: the weights stay below 2^8, exact enough in binary16,
 // and after the first tiles a rescale is rare.
 constexpr float kSlack = 8.f;
+constexpr float kMostWeight = 256.f;
+constexpr float kMostSum = 0x1p60f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -64,15 +66,22 @@ struct Tiles {
     __device__ __forceinline__ int start(int i) const { return (i < n_sink ? i : first + i - n_sink) * W; }
 };
 
-// 4-bit codes as binary16 without a conversion: code + 8 in the low mantissa
-// bits of 1024 (bits 0-3 of a half), or of 1024 in steps of 16 (bits 4-7), then
-// one packed subtraction or fused multiply-add, exact.  The halves of r[i] are
-// codes i and i + 4 of x's 8.
+// 4-bit codes as binary16 without a conversion.  A two's complement nibble with
+// its top bit flipped is code + 8; in bits 0-3 of a half under the exponent of
+// 1024 it stands for 1032 + code, in bits 4-7 for 1152 + 16 code, or, under the
+// exponent of 64, for 72 + code.  One masked exclusive or sets the exponent and
+// flips the bit.  The mask is kept in a vector register: an instruction takes one
+// scalar constant.
+__device__ __forceinline__ uint32_t masked_xor(uint32_t x, uint32_t mask, uint32_t flip) {
+    asm("" : "+v"(mask));
+    return (x & mask) ^ flip;
+}
+
+// 8 codes, exact: the halves of r[i] are codes i and i + 4.
 __device__ __forceinline__ void codes_f16(uint32_t x, uint32_t r[4]) {
-    x ^= 0x88888888u;
     const uint32_t y = x >> 8;
-    const uint32_t a[4] = {(x & 0x000F000Fu) | 0x64006400u, (x & 0x00F000F0u) | 0x64006400u,
-                           (y & 0x000F000Fu) | 0x64006400u, (y & 0x00F000F0u) | 0x64006400u};
+    const uint32_t a[4] = {masked_xor(x, 0x000F000Fu, 0x64086408u), masked_xor(x, 0x00F000F0u, 0x64806480u),
+                           masked_xor(y, 0x000F000Fu, 0x64086408u), masked_xor(y, 0x00F000F0u, 0x64806480u)};
     const f16x2 one = {static_cast<_Float16>(1032.f), static_cast<_Float16>(1032.f)};
     const f16x2 six = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
     const f16x2 off = {static_cast<_Float16>(-72.f), static_cast<_Float16>(-72.f)};
@@ -81,6 +90,28 @@ __device__ __forceinline__ void codes_f16(uint32_t x, uint32_t r[4]) {
         const f16x2 h = __builtin_bit_cast(f16x2, a[i]);
         r[i] = __builtin_bit_cast(uint32_t, (i & 1) ? __builtin_elementwise_fma(h, six, off) : h - one);
     }
+}
+
+// code + 72, in the same order and without the subtraction, for a product that
+// starts at -72 times the other side's sum (its 32-bit sums lose log2(72) bits
+// to the offset: fine for 128 products, not for a sum over all positions).
+__device__ __forceinline__ u32x4 codes_bias72(uint32_t x) {
+    return u32x4{masked_xor(x << 4, 0x00F000F0u, 0x54805480u), masked_xor(x, 0x00F000F0u, 0x54805480u),
+                 masked_xor(x >> 4, 0x00F000F0u, 0x54805480u), masked_xor(x >> 8, 0x00F000F0u, 0x54805480u)};
+}
+
+__device__ __forceinline__ float half_of(uint32_t w, int high) {
+    const f16x2 h = __builtin_bit_cast(f16x2, w);
+    return static_cast<float>(high ? h[1] : h[0]);
+}
+
+// y times a half of w (one instruction takes the binary16 operand as it is).
+__device__ __forceinline__ float times_half(float y, uint32_t w, int high) { return fmaf(half_of(w, high), y, 0.f); }
+
+// l + both halves of w.
+__device__ __forceinline__ float add_pair(uint32_t w, float l) {
+    const f16x2 one = {static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)};
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), one, l, false);
 }
 
 // 8 binary16 values in the order codes_f16 leaves codes in.

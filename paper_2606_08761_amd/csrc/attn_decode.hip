@@ -19,12 +19,12 @@
 //         of its group and transposes them in registers (half a v_perm a value);
 //         product i takes the rows d = D / 16 (lane % 16) + i.  The order of the
 //         rows and of the positions inside a product is free.
-// The scores' maximum is kept per head, raised only when a score passes it by
-// 2^8: the weights are at most 2^8 and in most tiles nothing is rescaled.
+// The scores' maximum is kept per head, raised only when a weight passes 2^8:
+// in most tiles nothing is rescaled.
 // 4-bit codes enter the products as small integers in binary16 (exact); a
-// position's two scales multiply its score and its weight in 32 bits, the
-// latter over a power of two near the largest scale so far, so that small scales
-// do not push the weights out of binary16's range.
+// position's two scales multiply its score and its weight in 32 bits.  The
+// maximum is then that of the score plus log2 of the value's scale, so that
+// weights times scales, whatever the scales are, stay in binary16's range.
 //
 // Four waves share a range of positions and add their sums through LDS; with
 // more than one range a sequence, a second kernel joins the ranges' sums in
@@ -38,11 +38,11 @@ using namespace attn;
 
 constexpr int kTile = 32;      // positions a wave takes at a time
 constexpr int kWaves = 4;
-constexpr int kMaxTiles = 128; // tiles of a range: 4096 positions, 256 pages at most
+constexpr int kMaxTiles = 64;  // tiles of a range at most
 constexpr int kHeads = 16;     // query heads a workgroup takes
 
 template <int D, bool I4>
-__global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(KvView c, AttnArgs a, int S, int range,
+__global__ __launch_bounds__(64 * kWaves, 3) void attn_decode_kernel(KvView c, AttnArgs a, int S, int range,
                                                                   int head_tiles, float* __restrict__ part,
                                                                   float* __restrict__ ml) {
     constexpr int DV = D / 16;  // values d of a lane in the second product
@@ -52,14 +52,18 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(KvView c, Attn
     __shared__ float sum_ml[2][kWaves][kHeads];
     __shared__ __align__(16) float sums[kWaves][kHeads][P];
 
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
+    // Workgroups go to the 8 XCDs in turn.  Every group of 8 is rotated by its
+    // number, so that no XCD gets the same heads or ranges of every sequence, which
+    // differ in length; the later ranges, missing from short sequences, come last.
     uint32_t id = blockIdx.x;
-    const int split = static_cast<int>(id % S);
-    id /= S;
+    if ((id | 7) < gridDim.x) id = (id & ~7u) | ((id + (id >> 3)) & 7u);
+    const int h = static_cast<int>(id % c.kv_heads);
+    id /= c.kv_heads;
     const int ht = static_cast<int>(id % head_tiles);
     id /= head_tiles;
-    const int h = static_cast<int>(id % c.kv_heads);
-    const int b = static_cast<int>(id / c.kv_heads);
+    const int b = static_cast<int>(id % c.B);
+    const int split = static_cast<int>(id / c.B);
     const int group = a.heads / c.kv_heads;
     const int heads = min(kHeads, group - ht * kHeads);  // of this workgroup
     const int64_t row0 = static_cast<int64_t>(b) * a.heads + h * group + ht * kHeads;
@@ -111,11 +115,14 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(KvView c, Attn
     const int k_off = 8 * (r16 >> 2), v_off = 8 * g4;  // runs of 8 positions lie in one page
     const int k_half = halves == 2 ? k_off >> 4 : 0, v_half = halves == 2 ? v_off >> 4 : 0;
 
-    u32x4 kf[2][I4 ? 1 : KS];
-    u32x4 vf[I4 ? 2 : 8];   // a lane's values of 8 positions: DV binary16, or DV codes
-    u32x4 ks, vs;           // scales of the lane's 8 positions
-
-    auto load_k = [&](int t) {
+    // one tile in registers: a lane's keys of 4 + 4 positions, its values of 8 (DV
+    // binary16, or DV codes), and the scales of the 8
+    struct Loaded {
+        u32x4 k[2][I4 ? 1 : KS];
+        u32x4 v[I4 ? 2 : 8];
+        u32x4 ks, vs;
+    };
+    auto load_k = [&](int t, Loaded& x) {
         const int at = (tiles.start(t) + k_off) & page_mask;
         const int64_t page = pages[(t - t0) * halves + k_half] * c.page_bytes;
 #pragma unroll
@@ -123,90 +130,88 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(KvView c, Attn
             const int64_t row = head_at + at + 4 * u + (r16 & 3);
             if constexpr (I4) {
                 const uint8_t* p = c.k + page + row * (D / 2) + 4 * KS * g4;
-                if constexpr (KS == 4) kf[u][0] = *reinterpret_cast<const u32x4*>(p);
+                if constexpr (KS == 4) x.k[u][0] = *reinterpret_cast<const u32x4*>(p);
                 else {
                     const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-                    kf[u][0][0] = w[0];
-                    kf[u][0][1] = w[1];
+                    x.k[u][0][0] = w[0];
+                    x.k[u][0][1] = w[1];
                 }
             } else {
                 const uint8_t* p = c.k + page + row * (2 * D) + 16 * g4;
 #pragma unroll
-                for (int s = 0; s < KS; ++s) kf[u][s] = *reinterpret_cast<const u32x4*>(p + 64 * s);
+                for (int s = 0; s < KS; ++s) x.k[u][s] = *reinterpret_cast<const u32x4*>(p + 64 * s);
             }
         }
-        if constexpr (I4) {  // scales in the layout of the scores
-            const int av = (tiles.start(t) + v_off) & page_mask;
-            const int64_t pv = pages[(t - t0) * halves + v_half] * c.page_bytes;
-            ks = *reinterpret_cast<const u32x4*>(c.k + pv + scale_at + 2 * (head_at + av));
-        }
     };
-    auto load_v = [&](int t) {
+    auto load_v = [&](int t, Loaded& x) {
         const int at = (tiles.start(t) + v_off) & page_mask;
         const int64_t page = pages[(t - t0) * halves + v_half] * c.page_bytes;
+        const int64_t row = head_at + at;
+        const uint8_t* p = c.v + page + row * (I4 ? D / 2 : 2 * D) + (I4 ? DV / 2 : 2 * DV) * r16;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int64_t row = head_at + at + j;
+            const uint8_t* pj = p + j * (I4 ? D / 2 : 2 * D);
             if constexpr (I4) {
-                const uint8_t* p = c.v + page + row * (D / 2) + (DV / 2) * r16;
-                if constexpr (DV == 8) vf[j >> 2][j & 3] = *reinterpret_cast<const uint32_t*>(p);
-                else vf[j >> 2][j & 3] = *reinterpret_cast<const uint16_t*>(p);
+                if constexpr (DV == 8) x.v[j >> 2][j & 3] = *reinterpret_cast<const uint32_t*>(pj);
+                else x.v[j >> 2][j & 3] = *reinterpret_cast<const uint16_t*>(pj);
             } else {
-                const uint8_t* p = c.v + page + row * (2 * D) + 2 * DV * r16;
-                if constexpr (DV == 8) vf[j] = *reinterpret_cast<const u32x4*>(p);
+                if constexpr (DV == 8) x.v[j] = *reinterpret_cast<const u32x4*>(pj);
                 else {
-                    const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-                    vf[j][0] = w[0];
-                    vf[j][1] = w[1];
+                    const u32x2 w = *reinterpret_cast<const u32x2*>(pj);
+                    x.v[j][0] = w[0];
+                    x.v[j][1] = w[1];
                 }
             }
         }
-        if constexpr (I4) vs = *reinterpret_cast<const u32x4*>(c.v + page + scale_at + 2 * (head_at + at));
+        if constexpr (I4) {  // both in the layout of the scores
+            x.ks = *reinterpret_cast<const u32x4*>(c.k + page + scale_at + 2 * row);
+            x.vs = *reinterpret_cast<const u32x4*>(c.v + page + scale_at + 2 * row);
+        }
     };
 
     f32x4 o[DV];
 #pragma unroll
     for (int i = 0; i < DV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = kNoMax, l = 0.f, ref = 0.f, ref_inv = 0.f;
+    float m = kNoMax, l = 0.f;
     const float to_log2 = a.scale * kLog2e;
-
-    int t = t0 + wave;
-    if (t < t1) {
-        load_k(t);
-        load_v(t);
+    // the first product of codes + 72 (codes_bias72) starts at -72 sum q
+    float minus = 0.f;
+    if constexpr (I4) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) minus += half_of(qf[s][i], 0) + half_of(qf[s][i], 1);
+        minus += __shfl_xor(minus, 16, 64);
+        minus += __shfl_xor(minus, 32, 64);
+        minus *= -72.f;
     }
-    for (; t < t1; t += kWaves) {
+
+    // One tile.  more(): issues the loads that may go out once the keys, and
+    // more_v() once the values, are used.
+    auto step = [&](int t, Loaded& x, auto more_k, auto more_v) {
         const int at = tiles.start(t);
-        // scores, 8 positions of one head a lane
         f32x4 sc[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            sc[u] = f32x4{minus, minus, minus, minus};
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 u32x4 kk;
-                if constexpr (I4) {
-                    uint32_t w[4];
-                    codes_f16(kf[u][0][s], w);
-                    kk = u32x4{w[0], w[1], w[2], w[3]};
-                } else {
-                    kk = kf[u][s];
-                }
+                if constexpr (I4) kk = codes_bias72(x.k[u][0][s]);
+                else kk = x.k[u][s];
                 sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, kk), __builtin_bit_cast(f16x8, qf[s]),
                                                                sc[u], 0, 0, 0);
             }
         }
-        float x[8], w[8];
+        float y[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            x[j] = sc[j >> 2][j & 3] * to_log2;
+            y[j] = sc[j >> 2][j & 3];
             if constexpr (I4) {
-                x[j] *= __half2float(__ushort_as_half(static_cast<uint16_t>(ks[j >> 1] >> (16 * (j & 1)))));
-                w[j] = __half2float(__ushort_as_half(static_cast<uint16_t>(vs[j >> 1] >> (16 * (j & 1)))));
+                y[j] = times_half(y[j], x.ks[j >> 1], j & 1);
             }
         }
-        const bool more = t + kWaves < t1;
-        if (more) load_k(t + kWaves);
+        more_k();
         // positions past the end, or between the first ones and the window: their
         // scores do not count, and their values, whatever they are, are zero
         const bool masked = at + kTile > len || (at < tiles.lo && at + kTile > tiles.sinks);
@@ -215,76 +220,62 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(KvView c, Attn
             for (int j = 0; j < 8; ++j) {
                 const int p = at + v_off + j;
                 const bool seen = p < len && (p >= tiles.lo || p < tiles.sinks);
-                x[j] = seen ? x[j] : -INFINITY;
+                y[j] = seen ? y[j] : -INFINITY;
                 if constexpr (I4) {
-                    w[j] = seen ? w[j] : 0.f;
+                    x.vs[j >> 1] &= seen ? 0xFFFFFFFFu : (j & 1) ? 0x0000FFFFu : 0xFFFF0000u;
                 } else {
 #pragma unroll
-                    for (int i = 0; i < DV / 2; ++i) vf[j][i] = seen ? vf[j][i] : 0u;
+                    for (int i = 0; i < DV / 2; ++i) x.v[j][i] = seen ? x.v[j][i] : 0u;
                 }
             }
         }
-        float top = x[0];
+        // weights under the maximum so far (of a score, or of a score plus log2 of
+        // its value's scale); where one is past the slack the maximum is raised first
+        float e[8], w[8], top = 0.f, sum_top = 0.f;
 #pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
-        bool raise = top > m + kSlack;
-        float wide = 0.f;
-        if constexpr (I4) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) wide = fmaxf(wide, w[j]);
-            raise = raise || wide > 16.f * ref;
+        for (int j = 0; j < 8; ++j) {
+            e[j] = exp2_fast(fmaf(y[j], to_log2, -m));
+            w[j] = I4 ? times_half(e[j], x.vs[j >> 1], j & 1) : e[j];
+            top = fmaxf(top, w[j]);
+            if constexpr (I4) sum_top = fmaxf(sum_top, e[j]);  // a scale of zero leaves the sum alone to grow
         }
-        if (__any(raise)) {
+        if (__any(top > kMostWeight || (I4 && sum_top > kMostSum))) {
+            top = kNoMax;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float z = y[j] * to_log2;
+                if constexpr (I4) z += __builtin_amdgcn_logf(fmaxf(half_of(x.vs[j >> 1], j & 1), 0x1p-24f));
+                top = fmaxf(top, z);
+            }
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             top = fmaxf(top, m);
-            float f = exp2_fast(m - top);
+            const float f = exp2_fast(m - top);
             l *= f;
             m = top;
-            if constexpr (I4) {
-                wide = fmaxf(wide, __shfl_xor(wide, 16, 64));
-                wide = fmaxf(wide, __shfl_xor(wide, 32, 64));
-                // the power of two at or below the largest scale
-                const float r = fmaxf(ref, __uint_as_float(__float_as_uint(wide) & 0x7F800000u));
-                f *= ref == r ? 1.f : ref / r;
-                ref = r;
-                ref_inv = r > 0.f ? 1.f / r : 0.f;
-            }
 #pragma unroll
             for (int i = 0; i < DV; ++i) o[i] *= f;
-        }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            x[j] = exp2_fast(x[j] - m);
-            l += x[j];
-            if constexpr (I4) x[j] *= w[j] * ref_inv;
+            for (int j = 0; j < 8; ++j) {
+                e[j] = exp2_fast(fmaf(y[j], to_log2, -m));
+                w[j] = I4 ? times_half(e[j], x.vs[j >> 1], j & 1) : e[j];
+            }
         }
         u32x4 pw;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) pw[j] = pack_f16(x[2 * j], x[2 * j + 1]);
-        // values: 8 positions x DV to DV operands of 8 positions
-#pragma unroll
-        for (int i = 0; i < DV / 2; ++i) {
-            u32x4 even, odd;
-            if constexpr (!I4) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    even[j] = low_halves(vf[2 * j][i], vf[2 * j + 1][i]);
-                    odd[j] = high_halves(vf[2 * j][i], vf[2 * j + 1][i]);
-                }
-                o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, even), __builtin_bit_cast(f16x8, pw),
-                                                                  o[2 * i], 0, 0, 0);
-                o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, odd),
-                                                                      __builtin_bit_cast(f16x8, pw), o[2 * i + 1], 0, 0, 0);
-            }
+        for (int j = 0; j < 4; ++j) {
+            pw[j] = pack_f16(w[2 * j], w[2 * j + 1]);
+            if constexpr (I4) l += e[2 * j] + e[2 * j + 1];
+            else l = add_pair(pw[j], l);  // the rounded weights: one large weight's rounding cancels
         }
+        // values: 8 positions x DV to DV operands of 8 positions
         if constexpr (I4) {
 #pragma unroll
             for (int i = 0; i < DV / 4; ++i) {  // codes 4 i .. 4 i + 3 of the lane's
                 uint32_t cf[4][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t va = vf[j >> 1][2 * (j & 1)], vb = vf[j >> 1][2 * (j & 1) + 1];
+                    const uint32_t va = x.v[j >> 1][2 * (j & 1)], vb = x.v[j >> 1][2 * (j & 1) + 1];
                     codes_f16(i ? high_halves(va, vb) : low_halves(va, vb), cf[j]);
                 }
 #pragma unroll
@@ -294,8 +285,58 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(KvView c, Attn
                         __builtin_bit_cast(f16x8, av), __builtin_bit_cast(f16x8, pw), o[4 * i + n], 0, 0, 0);
                 }
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < DV / 2; ++i) {
+                u32x4 even, odd;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    even[j] = low_halves(x.v[2 * j][i], x.v[2 * j + 1][i]);
+                    odd[j] = high_halves(x.v[2 * j][i], x.v[2 * j + 1][i]);
+                }
+                o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, even), __builtin_bit_cast(f16x8, pw),
+                                                                  o[2 * i], 0, 0, 0);
+                o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, odd),
+                                                                      __builtin_bit_cast(f16x8, pw), o[2 * i + 1], 0, 0, 0);
+            }
         }
-        if (more) load_v(t + kWaves);
+        more_v();
+    };
+
+    int t = t0 + wave;
+    if constexpr (I4) {  // a tile is 4 KB: two in flight
+        Loaded x, y;
+        auto none = [] {};
+        if (t < t1) {
+            load_k(t, x);
+            load_v(t, x);
+        }
+        while (t < t1) {
+            if (t + kWaves < t1) {
+                load_k(t + kWaves, y);
+                load_v(t + kWaves, y);
+            }
+            step(t, x, none, none);
+            t += kWaves;
+            if (t >= t1) break;
+            if (t + kWaves < t1) {
+                load_k(t + kWaves, x);
+                load_v(t + kWaves, x);
+            }
+            step(t, y, none, none);
+            t += kWaves;
+        }
+    } else {
+        Loaded x;
+        if (t < t1) {
+            load_k(t, x);
+            load_v(t, x);
+        }
+        for (; t < t1; t += kWaves) {
+            const bool more = t + kWaves < t1;
+            step(
+                t, x, [&] { if (more) load_k(t + kWaves, x); }, [&] { if (more) load_v(t + kWaves, x); });
+        }
     }
 
     // the four waves' sums
@@ -310,8 +351,7 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(KvView c, Attn
 #pragma unroll
     for (int i = 1; i < kWaves; ++i) top = fmaxf(top, sum_ml[0][i][r16]);
     {
-        float f = exp2_fast(m - top);
-        if constexpr (I4) f *= ref;
+        const float f = exp2_fast(m - top);
         // lane's rows: d = DV (4 g4 + r) + i
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -362,48 +402,75 @@ __global__ __launch_bounds__(64 * kWaves) void attn_decode_kernel(KvView c, Attn
 }
 
 // out[row] = sum_s part[row][s] 2^(m_s - M) / sum_s l_s 2^(m_s - M).  A workgroup
-// takes a row: its threads are D / 4 columns times slices of the parts, added in
-// a fixed order.
-template <int D>
+// takes C columns of four values of a row: its threads are the columns times
+// slices of the parts, added in a fixed order.  With many parts a row's columns
+// go to several workgroups (64 rows of 256 parts: 13.9 -> 5 us).
+template <int D, int C>
 __global__ __launch_bounds__(256) void attn_join_kernel(const float* __restrict__ part, const float* __restrict__ ml, int S,
                                                         uint16_t* __restrict__ out) {
-    constexpr int C = D / 4, N = 256 / C;  // columns, slices
+    constexpr int N = 256 / C, kFactors = 1024;
     __shared__ float top_of[4];
-    __shared__ float sum_of[N];
+    __shared__ int last_of[4];
+    __shared__ float factor[kFactors];
+    __shared__ float sum_of[4];
     __shared__ __align__(16) f32x4 sums[N][C];
-    const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x / (D / 4 / C);
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int col = static_cast<int>(blockIdx.x % (D / 4 / C)) * C + tid % C, slice = tid / C;
     const float* mlr = ml + row * S * 2;
+    const float* p = part + row * S * D + 4 * col;
     float top = kNoMax;
-    for (int s = tid; s < S; s += 256) top = fmaxf(top, mlr[2 * s]);
+    int last = 0;  // parts after the last one with a sum have none, and wrote none
+    for (int s = tid; s < S; s += 256) {
+        if (mlr[2 * s + 1] != 0.f) {
+            top = fmaxf(top, mlr[2 * s]);
+            last = s + 1;
+        }
+    }
 #pragma unroll
-    for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i, 64));
-    if ((tid & 63) == 0) top_of[tid >> 6] = top;
+    for (int i = 1; i < 64; i *= 2) {
+        top = fmaxf(top, __shfl_xor(top, i, 64));
+        last = max(last, __shfl_xor(last, i, 64));
+    }
+    if ((tid & 63) == 0) {
+        top_of[wave] = top;
+        last_of[wave] = last;
+    }
     __syncthreads();
     top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
-    const int col = tid % C, slice = tid / C;
+    last = max(max(last_of[0], last_of[1]), max(last_of[2], last_of[3]));
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
-    for (int s = slice; s < S; s += N) {
-        const float ls = mlr[2 * s + 1];
-        if (ls == 0.f) continue;  // a part without positions wrote no sums
-        const float f = exp2_fast(mlr[2 * s] - top);
-        l += ls * f;
-        const f32x4 v = *reinterpret_cast<const f32x4*>(part + (row * S + s) * D + 4 * col);
+    for (int s0 = 0; s0 < last; s0 += kFactors) {
+        const int n = min(kFactors, last - s0);
+        __syncthreads();  // the factors before are used
+        for (int s = tid; s < n; s += 256) {
+            const float f = exp2_fast(mlr[2 * (s0 + s)] - top);
+            factor[s] = f;
+            l = fmaf(mlr[2 * (s0 + s) + 1], f, l);
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int s = slice; s < n; s += N) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(p + static_cast<int64_t>(s0 + s) * D);
+            const float f = factor[s];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = fmaf(v[j], f, y[j]);
+            for (int j = 0; j < 4; ++j) y[j] = fmaf(v[j], f, y[j]);
+        }
     }
-    sums[slice][col] = y;
-    if (col == 0) sum_of[slice] = l;
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) l += __shfl_xor(l, i, 64);
+    if ((tid & 63) == 0) sum_of[wave] = l;
+    sums[slice][tid % C] = y;
     __syncthreads();
     if (slice) return;
 #pragma unroll
     for (int s = 1; s < N; ++s) {
-        const f32x4 v = sums[s][col];
+        const f32x4 v = sums[s][tid % C];
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] += v[j];
-        l += sum_of[s];
     }
+    l = (sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]);
     const float inv = l != 0.f ? 1.f / l : 0.f;
     *reinterpret_cast<u32x2*>(out + row * D + 4 * col) = u32x2{pack_f16(y[0] * inv, y[1] * inv), pack_f16(y[2] * inv, y[3] * inv)};
 }
@@ -430,7 +497,7 @@ Plan plan_decode(const KvView& c, const AttnArgs& a) {
     const int64_t units = static_cast<int64_t>(c.B) * c.kv_heads * p.head_tiles;
     const int64_t want = (4 * device_cu_count() + units - 1) / units;
     int64_t range = (tiles + want - 1) / want;
-    range = std::min<int64_t>(std::max<int64_t>(range, kWaves), kMaxTiles);
+    range = std::min<int64_t>(std::max<int64_t>(range, kWaves), c.i4 ? kMaxTiles : kMaxTiles / 2);
     p.range = static_cast<int>((range + kWaves - 1) / kWaves * kWaves);
     p.S = static_cast<int>((tiles + p.range - 1) / p.range);
     return p;
@@ -450,8 +517,13 @@ int64_t attn_decode_workspace(const KvView& c, const AttnArgs& a) {
 
 hipError_t launch_attn_join(const float* part, const float* ml, int64_t rows, int S, int D, uint16_t* out,
                             hipStream_t stream) {
-    auto run = [&](auto kernel) { kernel<<<static_cast<unsigned>(rows), 256, 0, stream>>>(part, ml, S, out); };
-    D == 128 ? run(attn_join_kernel<128>) : run(attn_join_kernel<64>);
+    // 32 parts or more, and rows too few to fill the compute units twice
+    const bool wide = S >= 32 && rows < 2 * device_cu_count();
+    auto run = [&](auto kernel, int per_row) {
+        kernel<<<static_cast<unsigned>(rows * per_row), 256, 0, stream>>>(part, ml, S, out);
+    };
+    if (D == 128) wide ? run(attn_join_kernel<128, 8>, 4) : run(attn_join_kernel<128, 32>, 1);
+    else wide ? run(attn_join_kernel<64, 8>, 2) : run(attn_join_kernel<64, 16>, 1);
     return hipGetLastError();
 }
 

@@ -32,31 +32,69 @@ namespace {
 using namespace attn;
 
 constexpr int kW = 64;            // positions of a tile
-constexpr int kWaves = 4;
-constexpr int kRows = 32 * kWaves;  // rows of a workgroup
-constexpr int kThreads = 64 * kWaves;
 
-template <int D, bool I4>
+// Keys and values of a tile lie in LDS as they lie in a binary16 page, a row of D
+// values a position, but with the 16-byte pieces of a row exchanged (piece c at
+// c ^ the numbers below), so that the 16 lanes that read at a time find theirs in
+// different banks: 16 positions' piece c of the keys; and of the values 32
+// bytes of 4 positions next to 32 other bytes of the same (the transposing read).
+template <int D>
+__device__ __forceinline__ int k_swizzle(int t) { return D == 128 ? (t & 15) : ((t >> 1) & 7); }
+template <int D>
+__device__ __forceinline__ int v_swizzle(int t) { return D == 128 ? (t & 3) << 2 : (t & 2) << 1; }
+
+template <int D, bool I4, int kWaves>
 struct Smem {
-    static constexpr int kChunk = kW * 16 + 16;  // bytes of 8 values d of every position; the padding spreads the writes
-    uint8_t k[2][D / 8 * kChunk];
-    uint8_t v[2][8 * D * 16];
+    uint8_t k[2][kW * D * 2];
+    uint8_t v[2][kW * D * 2];
     float ks[2][I4 ? kW : 4];  // scales, the softmax's factor in the keys'
     float vs[2][I4 ? kW : 4];
+    float vs_most[2][4];       // the largest of the positions that each wave staged
 };
 
-template <int D, bool I4>
-__global__ __launch_bounds__(kThreads, 2) void attn_prefill_kernel(KvView c, AttnArgs a, int S, int row_tiles,
-                                                                   float* __restrict__ part, float* __restrict__ ml) {
-    constexpr int KS = D / 16;                        // products along d in the first
-    constexpr int DT = D / 32;                        // tiles of d in the second
-    constexpr int KL = I4 ? D / 32 : D / 8;           // lanes a position's 16-byte pieces take
-    constexpr int KN = kW * KL / kThreads > 0 ? kW * KL / kThreads : 1;  // pieces a thread loads
-    constexpr int KR = kThreads / KL < kW ? kThreads / KL : kW;          // positions the threads cover at a time
-    extern __shared__ __align__(16) uint8_t smem_raw[];
-    Smem<D, I4>& sm = *reinterpret_cast<Smem<D, I4>*>(smem_raw);
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_u8*)p));
+}
 
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r32 = lane & 31, half = lane >> 5;
+// 16 bytes a lane from base + off straight into LDS at `to` + 16 lane.  The
+// compiler does not see these loads: landed() waits for all of them.  (The wait
+// states let M0, and a base that came out of a vector instruction, settle.)
+__device__ __forceinline__ void copy_to_lds(uint32_t to, uint32_t off, const uint8_t* base) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off),
+                 "s"(static_cast<uint64_t>(hi) << 32 | lo)
+                 : "memory");
+}
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// 4 positions' value d for the lane's d: lanes 4 j + i of 16 point at 4 values
+// each of position j, and the lane numbered n gets the n-th of the 16 of all four.
+__device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         (__attribute__((address_space(3))) s16x4*)static_cast<uintptr_t>(at)));
+}
+__device__ __forceinline__ u32x4 read_lds(uint32_t at) {
+    return *(const __attribute__((address_space(3))) u32x4*)static_cast<uintptr_t>(at);
+}
+__device__ __forceinline__ void write_lds(uint32_t at, u32x4 v) {
+    *(__attribute__((address_space(3))) u32x4*)static_cast<uintptr_t>(at) = v;
+}
+
+template <int D, bool I4, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, AttnArgs a, int S, int row_tiles,
+                                                                   float* __restrict__ part, float* __restrict__ ml) {
+    constexpr int kRows = 32 * kWaves;
+    constexpr int KS = D / 16;        // products along d in the first
+    constexpr int DT = D / 32;        // tiles of d in the second
+    constexpr int kRow = 2 * D;       // bytes of a position in LDS
+    constexpr int kTileBytes = kW * kRow;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    Smem<D, I4, kWaves>& sm = *reinterpret_cast<Smem<D, I4, kWaves>*>(smem_raw);
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r32 = lane & 31, half = lane >> 5;
     uint32_t id = blockIdx.x;
     const int h = static_cast<int>(id % c.kv_heads);  // workgroups of one key head on one XCD's L2 where the heads allow it
     id /= c.kv_heads;
@@ -80,138 +118,168 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prefill_kernel(KvView c, Att
     const int t1 = static_cast<int>(static_cast<int64_t>(tiles.count) * (split + 1) / S);
 
     // the lane's row
-    const int64_t R = R0 + wave * 32 + r32;
-    const int tok = static_cast<int>(R / group), hq = h * group + static_cast<int>(R % group);
-    const bool valid = R < rows && q0 >= 0 && q0 + tok < a.T;
-    const int pos = before + tok;
-    const int64_t row = (static_cast<int64_t>(q0) + tok) * a.heads + hq;
-
+    const int r_wave = static_cast<int>(R0 % group) + 32 * wave;  // of the tile's first token
+    const int tok_wave = static_cast<int>(R0 / group);
+    struct Row {
+        int tok, head;
+        bool valid;
+    };
+    auto row_of = [&](int r) {
+        Row x;
+        x.tok = tok_wave + (r_wave + r) / group;
+        x.head = h * group + (r_wave + r) % group;
+        x.valid = x.tok < n && R0 + 32 * wave + r < rows && q0 >= 0 && q0 + x.tok < a.T;
+        return x;
+    };
+    const bool idle = R0 + 32 * wave >= rows;  // a wave without rows only stages
+    int pos;
     u32x4 qf[KS];  // right operand: d = 16 s + 8 half ..
+    {
+        const Row x = row_of(r32);
+        pos = before + x.tok;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        qf[s] = u32x4{0u, 0u, 0u, 0u};
-        if (valid) qf[s] = *reinterpret_cast<const u32x4*>(a.q + (q0 + tok) * a.q_stride + hq * D + 16 * s + 8 * half);
-        if constexpr (I4) qf[s] = code_order(qf[s]);
+        for (int s = 0; s < KS; ++s) {
+            qf[s] = u32x4{0u, 0u, 0u, 0u};
+            if (x.valid) qf[s] = *reinterpret_cast<const u32x4*>(a.q + (q0 + x.tok) * a.q_stride + x.head * D + 16 * s + 8 * half);
+            if constexpr (I4) qf[s] = code_order(qf[s]);
+        }
     }
 
+    // Values that a thread could keep over the loop are made anew from this (a
+    // few instructions a tile): the registers are worth more.
+    auto anew = [](uint32_t x) {
+        asm("" : "+v"(x));
+        return static_cast<int>(x);
+    };
     const float to_log2 = a.scale * kLog2e;
     const int page_mask = (1 << c.page_shift) - 1;
     const int64_t head_at = static_cast<int64_t>(h) << c.page_shift;
     const int64_t scale_at = (static_cast<int64_t>(c.kv_heads) << c.page_shift) * (D / 2);
+    const uint32_t k_lds = lds_offset(sm.k), v_lds = lds_offset(sm.v);
+    const uint32_t ks_lds = lds_offset(sm.ks), vs_lds = lds_offset(sm.vs);
 
-    u32x4 kr[KN];
-    uint32_t vr[8][I4 ? 1 : 2];
-    float ksr = 0.f, vsr = 0.f;
-    const int kl = tid % KL, kt = tid / KL;               // piece and first position of a thread's keys
-    constexpr int VL = D / 4;                             // threads a position's values take, 4 each
-    const int vd = tid % VL, vg = tid / VL;               // values 4 vd .. of positions 16 s + 4 vh .. + 3, and 8 further on
-    const int vs_step = vg >> 1, vh = vg & 1;
-    const bool v_thread = vg < 8;
-    const bool k_thread = kt < kW;
-
-    // the pages of what a thread loads of a tile (16 positions lie in one page)
-    int k_page[KN], v_page, s_page;
-    auto load_pages = [&](int t) {
-        const int at = tiles.start(t);
-        auto page = [&](int x) {
-            const int p = page_of(c, b, at + x);
-            return p < 0 ? 0 : p;  // positions past the last page are masked, and read page 0
-        };
-#pragma unroll
-        for (int i = 0; i < KN; ++i) k_page[i] = page((kt + i * KR) & (kW - 1));
-        v_page = page((16 * vs_step) & (kW - 1));
-        if constexpr (I4) s_page = page(tid & (kW - 1));
-    };
-
-    auto load_tile = [&](int t) {
-        const int at = tiles.start(t);
-        if (k_thread) {
-#pragma unroll
-            for (int i = 0; i < KN; ++i) {
-                const int x = kt + i * KR;
-                const int64_t r = head_at + ((at + x) & page_mask);
-                kr[i] = *reinterpret_cast<const u32x4*>(c.k + k_page[i] * c.page_bytes + r * (I4 ? D / 2 : 2 * D) + 16 * kl);
-            }
-        }
-        if (v_thread) {
-            const int64_t r = head_at + ((at + 16 * vs_step + 4 * vh) & page_mask);
-            const uint8_t* p = c.v + v_page * c.page_bytes + r * (I4 ? D / 2 : 2 * D) + (I4 ? 2 : 8) * vd;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint8_t* pj = p + ((j & 3) + 8 * (j >> 2)) * (I4 ? D / 2 : 2 * D);
-                if constexpr (I4) vr[j][0] = *reinterpret_cast<const uint16_t*>(pj);
-                else {
-                    const u32x2 w = *reinterpret_cast<const u32x2*>(pj);
-                    vr[j][0] = w[0];
-                    vr[j][1] = w[1];
-                }
-            }
-        }
-        if constexpr (I4) {
-            if (tid < kW) {
-                const int64_t o = s_page * c.page_bytes + scale_at + 2 * (head_at + ((at + tid) & page_mask));
-                ksr = __half2float(*reinterpret_cast<const __half*>(c.k + o));
-                vsr = __half2float(*reinterpret_cast<const __half*>(c.v + o));
-            }
-        }
-    };
     // positions that no row of the workgroup sees hold anything: their values,
     // times a weight of zero, must not count
     auto seen_by_some = [&](int t) { return t <= p_hi && (t >= tiles.lo || t < tiles.sinks); };
-    auto store_tile = [&](int t, int buf) {
+    auto at_edge = [&](int t) {
         const int at = tiles.start(t);
-        const bool edge = at + kW > p_hi + 1 || (at < tiles.lo && at + kW > tiles.sinks);
-        if (k_thread) {
+        return at + kW > p_hi + 1 || (at < tiles.lo && at + kW > tiles.sinks);
+    };
+    // Staging.  begin_k/v(t) sends the loads of tile t out, end_k/v(t, buf) has it
+    // in LDS before the next barrier.
+    // binary16: every 1 KB that a wave copies is kPos positions of 16 (one page)
+    constexpr int kPos = 1024 / kRow;          // 4 (D = 128) or 8
+    constexpr int kCopies = kW / kPos / kWaves;  // 4 or 2
+    constexpr int kPieces = kRow / 16;
+    const int c_pos = lane / kPieces, c_slot = lane % kPieces;
+    auto first_of = [&](int i) { return kPos * (kWaves * i + wave); };
+    const uint32_t k_off = c_pos * kRow + 16 * (c_slot ^ k_swizzle<D>(kPos * wave + c_pos));
+    const uint32_t v_off = c_pos * kRow + 16 * (c_slot ^ v_swizzle<D>(c_pos));
+    // int4: a thread takes 16 bytes, 32 codes, of one position; the first four
+    // waves the keys', the others the values'
+    constexpr int kLanes = D / 32;
+    static_assert(!I4 || kWaves == 8, "four waves for the keys, four for the values");
+    const bool i_values = wave >= 4;
+    const int i_pos = (tid & 255) / kLanes, i_part = tid % kLanes;
+    const bool i_thread = i_pos < kW;
+    u32x4 i_codes;
+    uint16_t i_scale = 0;
+
+    // The pages of what a wave, or a thread, loads of a tile: ids are looked up a
+    // step before they are needed, and make the places of a tile's keys, then of its
+    // values.
+    constexpr int kIds = I4 ? 1 : kCopies;
+    struct Ids {
+        int page[kIds];
+    };
+    const bool one_page = c.page_shift >= 6;  // a tile lies in one page
+    struct Places {
+        int64_t at[kIds];
+        int64_t scale;
+    };
+    const __attribute__((address_space(4))) int32_t* table =
+        (const __attribute__((address_space(4))) int32_t*)(c.table + static_cast<int64_t>(b) * c.width);
+    auto first = [&](int i) { return I4 ? i_pos & (kW - 1) : first_of(i); };
+    auto look_up = [&](int t) {
+        const int at = tiles.start(t);
+        Ids r;
 #pragma unroll
-            for (int i = 0; i < KN; ++i) {
-                const int x = kt + i * KR;
-                if constexpr (I4) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t w[4];
-                        codes_f16(kr[i][j], w);
-                        *reinterpret_cast<u32x4*>(&sm.k[buf][(4 * kl + j) * Smem<D, I4>::kChunk + x * 16]) = u32x4{w[0], w[1], w[2], w[3]};
-                    }
-                } else {
-                    *reinterpret_cast<u32x4*>(&sm.k[buf][kl * Smem<D, I4>::kChunk + x * 16]) = kr[i];
-                }
-            }
+        for (int i = 0; i < kIds; ++i) {
+            if (i && one_page) break;
+            const int p = (at + first(i)) >> c.page_shift;
+            r.page[i] = table[p < c.width ? p : c.width - 1];
         }
-        if (v_thread) {
-            if (!I4 && edge) {
+        return r;
+    };
+    // positions past the last page are masked, and read page 0
+    auto places = [&](int t, const Ids& ids) {
+        const int at = tiles.start(t);
+        Places r;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool seen = seen_by_some(at + 16 * vs_step + 4 * vh + (j & 3) + 8 * (j >> 2));
-                    vr[j][0] = seen ? vr[j][0] : 0u;
-                    if constexpr (!I4) vr[j][1] = seen ? vr[j][1] : 0u;
-                }
+        for (int i = 0; i < kIds; ++i) {
+            if (i && one_page) {
+                r.at[i] = r.at[0] + kPos * kWaves * kRow * i;
+                continue;
             }
-            u32x4 item[4];  // one of 8 positions for each of the 4 values
+            const int p = static_cast<uint32_t>(ids.page[i]) < static_cast<uint32_t>(c.n_pages) ? ids.page[i] : 0;
+            const int x = static_cast<int>(head_at) + ((at + first(i)) & page_mask);  // below 2^26
+            r.at[i] = p * c.page_bytes + static_cast<int64_t>(x) * (I4 ? D / 2 : kRow);
+            if constexpr (I4) r.scale = p * c.page_bytes + scale_at + 2 * x;
+        }
+        return r;
+    };
+    // Sends out tile t's loads, and has what they brought in LDS before the next
+    // barrier (values of positions that nobody sees as zeros).
+    auto begin_copies = [&](int buf, const Places& at, const uint8_t* plane, uint32_t lds, uint32_t off) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (I4) {
+        for (int i = 0; i < kCopies; ++i) copy_to_lds(lds + buf * kTileBytes + first_of(i) * kRow, off, plane + at.at[i]);
+    };
+    auto clear_unseen = [&](int t, int buf) {  // a wave clears what it copied itself
+        if (!at_edge(t)) return;
+        const int at = tiles.start(t);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int x = first_of(i);
+            if (!seen_by_some(at + x + c_pos)) write_lds(v_lds + buf * kTileBytes + x * kRow + 16 * lane, u32x4{0u, 0u, 0u, 0u});
+        }
+    };
+    auto begin_codes = [&](const Places& at) {
+        if (i_thread) {
+            const uint8_t* plane = i_values ? c.v : c.k;
+            i_codes = *reinterpret_cast<const u32x4*>(plane + at.at[0] + 16 * i_part);
+            i_scale = *reinterpret_cast<const uint16_t*>(plane + at.scale);
+        }
+    };
+    auto end_codes = [&](int t, int buf) {
+        const int i_pos = (anew(tid) & 255) / kLanes, i_part = anew(tid) % kLanes;
+        const bool i_thread = i_pos < kW;
+        if (!i_values) {
+            if (i_thread) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
                     uint32_t w[4];
-                    codes_f16(low_halves(vr[2 * j][0], vr[2 * j + 1][0]), w);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) item[i][j] = w[i];
-                } else {
-                    item[0][j] = low_halves(vr[2 * j][0], vr[2 * j + 1][0]);
-                    item[1][j] = high_halves(vr[2 * j][0], vr[2 * j + 1][0]);
-                    item[2][j] = low_halves(vr[2 * j][1], vr[2 * j + 1][1]);
-                    item[3][j] = high_halves(vr[2 * j][1], vr[2 * j + 1][1]);
+                    codes_f16(i_codes[j], w);
+                    write_lds(k_lds + buf * kTileBytes + i_pos * kRow + 16 * ((4 * i_part + j) ^ k_swizzle<D>(i_pos)), u32x4{w[0], w[1], w[2], w[3]});
                 }
+                if (i_part == 0) sm.ks[buf][i_pos] = half_of(i_scale, 0) * to_log2;
             }
-            // value d = 4 vd + i in slot i D/4 + vd: neighbours write side by side
+        } else {
+            float most = 0x1p-24f;  // a scale of zero leaves the sum of the weights alone to grow
+            if (i_thread) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<u32x4*>(&sm.v[buf][((2 * vs_step + vh) * D + i * VL + vd) * 16]) = item[i];
-        }
-        if constexpr (I4) {
-            if (tid < kW) {
-                const bool seen = seen_by_some(at + tid);
-                sm.ks[buf][tid] = ksr * to_log2;
-                sm.vs[buf][tid] = seen ? vsr : 0.f;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t w[4];
+                    codes_f16(i_codes[j], w);  // back in order: the halves of w[i] are codes i and i + 4
+                    write_lds(v_lds + buf * kTileBytes + i_pos * kRow + 16 * ((4 * i_part + j) ^ v_swizzle<D>(i_pos)),
+                              u32x4{low_halves(w[0], w[1]), low_halves(w[2], w[3]), high_halves(w[0], w[1]), high_halves(w[2], w[3])});
+                }
+                const float x = seen_by_some(tiles.start(t) + i_pos) ? half_of(i_scale, 0) : 0.f;
+                if (i_part == 0) sm.vs[buf][i_pos] = x;
+                most = fmaxf(most, x);
             }
+#pragma unroll
+            for (int i = kLanes; i < 64; i *= 2) most = fmaxf(most, __shfl_xor(most, i, 64));
+            if (lane == 0) sm.vs_most[buf][wave - 4] = most;
         }
     };
 
@@ -220,139 +288,211 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prefill_kernel(KvView c, Att
     for (int i = 0; i < DT; ++i)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-    float m = kNoMax, l = 0.f, ref = 0.f, ref_inv = 0.f;
+    float m = kNoMax, l = 0.f;
 
-    if (t0 < t1) {
-        load_pages(t0);
-        load_tile(t0);
-        store_tile(t0, 0);
-        if (t0 + 1 < t1) {
-            load_pages(t0 + 1);
-            load_tile(t0 + 1);
+    const uint32_t k_read = k_lds + r32 * kRow + 16 * (half ^ k_swizzle<D>(r32));
+    // the transposing read: 16 lanes at 4 positions' 32 bytes of d = 32 i + 16 (lane / 16 % 2) ..
+    const uint32_t v_read = v_lds + (4 * half + ((lane & 15) >> 2)) * kRow +
+                            ((32 * ((lane >> 4) & 1) + 8 * (lane & 3)) ^ (16 * v_swizzle<D>((lane & 15) >> 2)));
+
+    // Fragments of the products, a quarter of a tile's at a time: KS / 4 steps of
+    // d for both halves of the keys, one step of 16 positions for all values d.
+    constexpr int KQ = KS / 4;
+    struct KeyFrags {
+        u32x4 f[KQ][2];
+    };
+    struct ValueFrags {
+        u32x4 f[DT];
+    };
+    auto read_k = [&](int s, uint32_t base) {
+        KeyFrags r;
+#pragma unroll
+        for (int i = 0; i < KQ; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) r.f[i][u] = read_lds((base ^ (32 * (KQ * s + i))) + 32 * u * kRow);
+        return r;
+    };
+    auto read_v = [&](int s, uint32_t base) {
+        ValueFrags r;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const uint32_t p = (base ^ (64 * i)) + 16 * s * kRow;
+            const u32x2 v0 = read_transposed(p), v1 = read_transposed(p + 8 * kRow);
+            r.f[i] = u32x4{v0[0], v0[1], v1[0], v1[1]};
         }
-    }
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1, at = tiles.start(t);
-        if (t + 2 < t1) load_pages(t + 2);
-        f32x16 sc[2];
+        return r;
+    };
+    auto add_scores = [&](f32x16 (&sc)[2], int s, const KeyFrags& k) {
+        if (s == 0) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sc[u][j] = 0.f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const u32x4 kk = *reinterpret_cast<const u32x4*>(&sm.k[buf][(2 * s + half) * Smem<D, I4>::kChunk + (32 * u + r32) * 16]);
-                sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kk), __builtin_bit_cast(f16x8, qf[s]), sc[u], 0, 0, 0);
-            }
+                for (int j = 0; j < 16; ++j) sc[u][j] = 0.f;
         }
+#pragma unroll
+        for (int i = 0; i < KQ; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, k.f[i][u]),
+                                                               __builtin_bit_cast(f16x8, qf[KQ * s + i]), sc[u], 0, 0, 0);
+    };
+
+    // One tile, whose scores are in sc; the next one's products run into next
+    // beside the exponentials.
+    Places next_v;  // tile t + 1's values
+    Ids ids;        // of tile t + 2 (int4: of t + 1 where the thread stages values)
+    auto step = [&](int t, f32x16 (&sc)[2], f32x16 (&next)[2], int buf) {
+        const int at = tiles.start(t);
+        const int staged = I4 && i_values ? t + 1 : t + 2;
+        const Places next_k = places(staged, ids);
         if constexpr (I4) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x4 s4 = *reinterpret_cast<const f32x4*>(&sm.ks[buf][32 * u + 8 * i + 4 * half]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sc[u][4 * i + j] *= s4[j];
-                }
+            if (staged < t1) begin_codes(next_k);
+        } else {
+            if (t + 2 < t1) begin_copies(buf, next_k, c.k, k_lds, k_off);
+            if (t + 1 < t1) begin_copies(buf ^ 1, next_v, c.v, v_lds, v_off);
+            next_v = next_k;
         }
-        const float f_log2 = I4 ? 1.f : to_log2;
-        const bool full = at + kW - 1 <= p_lo && (a.window == 0 || at > p_hi - a.window || at + kW <= tiles.sinks);
-        if (!full) {
-            // visible: t <= pos, and t > pos - window or t < sinks
-            const int from = a.window ? pos - a.window + 1 : 0;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int p = at + 32 * u + 8 * (j >> 2) + 4 * half + (j & 3);
-                    const bool seen = p <= pos && (p >= from || p < a.sinks);
-                    sc[u][j] = seen ? sc[u][j] : -INFINITY;
-                }
-        }
-        float top = sc[0][0];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[u][j]);
-        top *= f_log2;
-        bool raise = top > m + kSlack;
-        float wide = 0.f;
-        if constexpr (I4) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x4 s4 = *reinterpret_cast<const f32x4*>(&sm.vs[buf][32 * u + 8 * i + 4 * half]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) wide = fmaxf(wide, s4[j]);
-                }
-            raise = raise || wide > 16.f * ref;
-        }
-        if (__any(raise)) {
-            top = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
-            float f = exp2_fast(m - top);
-            l *= f;
-            m = top;
+        ids = look_up(staged + 1);
+        if (!idle) {
+            const uint32_t sb = 16 * (anew(tid) >> 5 & 1);
             if constexpr (I4) {
-                wide = fmaxf(wide, __shfl_xor(wide, 32, 64));
-                const float r = fmaxf(ref, __uint_as_float(__float_as_uint(wide) & 0x7F800000u));
-                f *= ref == r ? 1.f : ref / r;
-                ref = r;
-                ref_inv = r > 0.f ? 1.f / r : 0.f;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x4 s4 = __builtin_bit_cast(f32x4, read_lds(ks_lds + sb + 4 * kW * buf + 128 * u + 32 * i));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sc[u][4 * i + j] *= s4[j];
+                    }
             }
+            const float f_log2 = I4 ? 1.f : to_log2;
+            const bool full = at + kW - 1 <= p_lo && (a.window == 0 || at > p_hi - a.window || at + kW <= tiles.sinks);
+            if (!full) {
+                // visible: t <= pos, and t > pos - window or t < sinks; as bounds of t less
+                // the lane's first position
+                const int p0 = at + 4 * (anew(tid) >> 5 & 1), last = pos - p0;
+                const int from = a.window ? last - a.window + 1 : -p0, first = a.sinks - p0;
 #pragma unroll
-            for (int i = 0; i < DT; ++i)
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) o[i][j] *= f;
-        }
+                    for (int j = 0; j < 16; ++j) {
+                        const int p = 32 * u + 8 * (j >> 2) + (j & 3);
+                        const bool seen = (p <= last) & ((p >= from) | (p < first));
+                        sc[u][j] = seen ? sc[u][j] : -INFINITY;
+                    }
+            }
+            float top = sc[0][0];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                u32x4 pw;
+                for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[u][j]);
+            top *= f_log2;
+            if constexpr (I4) {  // a bound of the scores with their values' scales
+                const f32x4 w = *reinterpret_cast<const f32x4*>(sm.vs_most[buf]);
+                top += __builtin_amdgcn_logf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])));
+            }
+            if (__any(top > m + kSlack)) {
+                top = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
+                const float f = exp2_fast(m - top);
+                l *= f;
+                m = top;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float x = sc[u][8 * s + j], e = exp2_fast(I4 ? x - m : fmaf(x, f_log2, -m));
-                    sc[u][8 * s + j] = e;
-                    l += e;
-                }
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[i][j] *= f;
+            }
+            // the next tile's products (past the last tile: of whatever lies there, and
+            // not used) a quarter at a time beside a quarter of the exponentials
+            u32x4 pw[4];
+            const uint32_t kb = anew(k_read + (buf ^ 1) * kTileBytes), vb = anew(v_read + buf * kTileBytes);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                add_scores(next, s, read_k(s, kb));
+                float e[8];
+                f32x4 sv[2];
                 if constexpr (I4) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const f32x4 s4 = *reinterpret_cast<const f32x4*>(&sm.vs[buf][32 * u + 16 * s + 8 * i + 4 * half]);
+                    for (int i = 0; i < 2; ++i) sv[i] = __builtin_bit_cast(f32x4, read_lds(vs_lds + sb + 4 * kW * buf + 64 * s + 32 * i));
+                }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) sc[u][8 * s + 4 * i + j] *= s4[j] * ref_inv;
+                for (int j = 0; j < 8; ++j) {
+                    const float x = sc[s >> 1][8 * (s & 1) + j];
+                    e[j] = exp2_fast(I4 ? x - m : fmaf(x, f_log2, -m));
+                    if constexpr (I4) {
+                        l += e[j];
+                        e[j] *= sv[j >> 2][j & 3];
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) pw[j] = pack_f16(sc[u][8 * s + 2 * j], sc[u][8 * s + 2 * j + 1]);
-#pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    const u32x4 vv = *reinterpret_cast<const u32x4*>(&sm.v[buf][((2 * (2 * u + s) + half) * D + 32 * i + r32) * 16]);
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, vv), __builtin_bit_cast(f16x8, pw), o[i], 0, 0, 0);
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t p = pack_f16(e[2 * j], e[2 * j + 1]);
+                    if constexpr (!I4) l = add_pair(p, l);  // the rounded weights: one large weight's rounding cancels
+                    pw[s][j] = p;
                 }
+                        }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const ValueFrags vf = read_v(s, vb);
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, vf.f[i]), __builtin_bit_cast(f16x8, pw[s]), o[i], 0, 0, 0);
             }
-        if (t + 1 < t1) store_tile(t + 1, buf ^ 1);
-        if (t + 2 < t1) load_tile(t + 2);
+        }
+        if constexpr (I4) {
+            if (staged < t1) end_codes(staged, i_values ? buf ^ 1 : buf);
+        } else {
+            landed();
+            if (t + 1 < t1) clear_unseen(t + 1, buf ^ 1);
+        }
         __syncthreads();
+    };
+
+    f32x16 s0[2], s1[2];
+    if (t0 < t1) {
+        ids = look_up(t0);
+        next_v = places(t0, ids);
+        if constexpr (I4) {
+            begin_codes(next_v);
+            end_codes(t0, 0);
+            if (!i_values && t0 + 1 < t1) {
+                begin_codes(places(t0 + 1, look_up(t0 + 1)));
+                end_codes(t0 + 1, 1);
+            }
+            ids = look_up(i_values ? t0 + 1 : t0 + 2);
+        } else {
+            ids = look_up(t0 + 1);
+            begin_copies(0, next_v, c.k, k_lds, k_off);
+            begin_copies(0, next_v, c.v, v_lds, v_off);
+            next_v = places(t0 + 1, ids);
+            if (t0 + 1 < t1) begin_copies(1, next_v, c.k, k_lds, k_off);
+            ids = look_up(t0 + 2);
+            landed();
+            clear_unseen(t0, 0);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < 4; ++s) add_scores(s0, s, read_k(s, k_read));
+        __syncthreads();  // the keys' first buffer is free
+        for (int t = t0; t < t1; t += 2) {
+            step(t, s0, s1, 0);
+            if (t + 1 < t1) step(t + 1, s1, s0, 1);
+        }
     }
 
     l += __shfl_xor(l, 32, 64);
-    if (!valid) return;
-    // slot 32 i + r of the values is d = 4 (slot % (D / 4)) + slot / (D / 4), and
-    // the lane's rows r = 8 x + 4 half + y: 4 consecutive d for every (x, y)
-    float f = 1.f;
-    if constexpr (I4) f = ref;
-    if (S == 1) f *= l != 0.f ? 1.f / l : 0.f;
+    const Row x = row_of(anew(r32));
+    if (!x.valid) return;
+    const int64_t row = (static_cast<int64_t>(q0) + x.tok) * a.heads + x.head;
+    // the lane's rows of the sums are d = 32 i + 8 k + 4 half + y
+    const float f = S > 1 ? 1.f : l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x)
+    for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
+        for (int k = 0; k < 4; ++k) {
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (D == 128 ? o[e % DT][4 * x + y] : o[e >> 1][4 * x + 8 * (e & 1) + y]) * f;
-            const int d = 4 * (8 * x + 4 * half + y);
+            for (int y = 0; y < 4; ++y) v[y] = o[i][4 * k + y] * f;
+            const int d = 32 * i + 8 * k + 4 * half;
             if (S == 1) {
                 *reinterpret_cast<u32x2*>(a.out + row * D + d) = u32x2{pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
             } else {
@@ -366,25 +506,31 @@ __global__ __launch_bounds__(kThreads, 2) void attn_prefill_kernel(KvView c, Att
 }
 
 struct Plan {
+    int waves;
     int row_tiles;
     int S;
 };
 
-// The tiles are split where the workgroups number fewer than the compute
-// units, into parts of at least four tiles, up to two workgroups a unit.
+// Eight waves (256 rows, half the staging a row) where that leaves two
+// workgroups a compute unit, and always for codes; four otherwise, so that few
+// rows spread over more of the units.  The tiles are split where the workgroups
+// number fewer than the compute units, into parts of at least four tiles, up to two
+// workgroups a unit.
 Plan plan_prefill(const KvView& c, const AttnArgs& a) {
     Plan p;
-    const int64_t group = a.heads / c.kv_heads;
-    p.row_tiles = static_cast<int>((a.max_q * group + kRows - 1) / kRows);
+    const int64_t group = a.heads / c.kv_heads, cu = device_cu_count();
+    const int64_t heads = static_cast<int64_t>(c.B) * c.kv_heads;
+    p.waves = c.i4 || (c.D == 128 && heads * ((a.max_q * group + 255) / 256) >= 4 * cu) ? 8 : 4;
+    const int64_t rows = 32 * p.waves;
+    p.row_tiles = static_cast<int>((a.max_q * group + rows - 1) / rows);
     const int64_t most = std::min<int64_t>(c.max_len, static_cast<int64_t>(c.width) << c.page_shift);
     int64_t tiles = (most + kW - 1) / kW;
     if (a.window) {
-        const int64_t tokens = std::min<int64_t>(a.max_q, (kRows - 1) / group + 2);  // new tokens of a row tile
+        const int64_t tokens = std::min<int64_t>(a.max_q, (rows - 1) / group + 2);  // new tokens of a row tile
         const int64_t w = (static_cast<int64_t>(a.window) + tokens + kW - 2) / kW + 1 + (static_cast<int64_t>(a.sinks) + kW - 1) / kW;
         tiles = std::min(tiles, w);
     }
-    const int64_t units = static_cast<int64_t>(c.B) * c.kv_heads * p.row_tiles;
-    const int cu = device_cu_count();
+    const int64_t units = heads * p.row_tiles;
     int64_t S = 1;
     if (units < cu) S = std::min<int64_t>((2 * cu + units - 1) / units, tiles / 4);
     p.S = static_cast<int>(std::min<int64_t>(std::max<int64_t>(S, 1), 128));
@@ -395,32 +541,38 @@ int64_t blocks_of(const KvView& c, const Plan& p) {
     return static_cast<int64_t>(c.B) * c.kv_heads * p.row_tiles * p.S;
 }
 
+template <int D, bool I4, int kWaves>
+hipError_t run(const KvView& c, const AttnArgs& a, const Plan& p, float* part, float* ml, hipStream_t stream) {
+    static std::atomic<uint64_t> done;
+    constexpr int lds = sizeof(Smem<D, I4, kWaves>);
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(attn_prefill_kernel<D, I4, kWaves>), lds, done);
+    if (e != hipSuccess) return e;
+    attn_prefill_kernel<D, I4, kWaves><<<static_cast<unsigned>(blocks_of(c, p)), 64 * kWaves, lds, stream>>>(c, a, p.S, p.row_tiles, part, ml);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 int64_t attn_prefill_workspace(const KvView& c, const AttnArgs& a) {
-    const Plan p = plan_prefill(c, a);
-    if (blocks_of(c, p) > 0x7FFFFFFFll) return -1;
-    return p.S == 1 ? 0 : a.T * a.heads * p.S * static_cast<int64_t>(c.D + 2) * 4;
+    // the size for either kind of cache: callers ask without naming it
+    int64_t most = 0;
+    for (const bool i4 : {false, true}) {
+        KvView v = c;
+        v.i4 = i4;
+        const Plan p = plan_prefill(v, a);
+        if (blocks_of(v, p) > 0x7FFFFFFFll) return -1;
+        most = std::max(most, p.S == 1 ? 0 : a.T * a.heads * p.S * static_cast<int64_t>(c.D + 2) * 4);
+    }
+    return most;
 }
 
 hipError_t launch_attn_prefill(const KvView& c, const AttnArgs& a, hipStream_t stream) {
     const Plan p = plan_prefill(c, a);
     float* part = static_cast<float*>(a.workspace);
     float* ml = part + a.T * a.heads * p.S * c.D;
-    auto run = [&](auto kernel, int lds, std::atomic<uint64_t>& done) {
-        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, done);
-        if (e != hipSuccess) return e;
-        kernel<<<static_cast<unsigned>(blocks_of(c, p)), kThreads, lds, stream>>>(c, a, p.S, p.row_tiles, part, ml);
-        return hipGetLastError();
-    };
-    static std::atomic<uint64_t> done[4];
     hipError_t e;
-    if (c.D == 128)
-        e = c.i4 ? run(attn_prefill_kernel<128, true>, sizeof(Smem<128, true>), done[0])
-                 : run(attn_prefill_kernel<128, false>, sizeof(Smem<128, false>), done[1]);
-    else
-        e = c.i4 ? run(attn_prefill_kernel<64, true>, sizeof(Smem<64, true>), done[2])
-                 : run(attn_prefill_kernel<64, false>, sizeof(Smem<64, false>), done[3]);
+    if (c.D == 128) e = c.i4 ? run<128, true, 8>(c, a, p, part, ml, stream) : p.waves == 8 ? run<128, false, 8>(c, a, p, part, ml, stream) : run<128, false, 4>(c, a, p, part, ml, stream);
+    else e = c.i4 ? run<64, true, 8>(c, a, p, part, ml, stream) : p.waves == 8 ? run<64, false, 8>(c, a, p, part, ml, stream) : run<64, false, 4>(c, a, p, part, ml, stream);
     if (e != hipSuccess || p.S == 1) return e;
     return launch_attn_join(part, ml, a.T * a.heads, p.S, c.D, a.out, stream);
 }

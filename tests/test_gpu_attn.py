@@ -106,6 +106,23 @@ def test_int4_scales_far_apart(pk):
 
 
 @pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("zeros", ["all", "values", "keys", "first", "last"])
+def test_zero_tokens(pk, cache, zeros):
+    """Keys or values of nothing but zeros (scales of zero), everywhere or beside
+    ordinary ones; scores far above those of the tokens with values."""
+    n = 300
+    c = paged.Case(67, [n], [1], 4, 1, 128, 16, cache, spoil=False)
+    c.q *= np.float16(8)  # scores of some tens
+    for t in range(n):
+        for plane, keep, name in ((c.k, c.K, "keys"), (c.v, c.V, "values")):
+            if zeros in ("all", name) or (name == "values" and ((zeros == "first" and t < 100) or (zeros == "last" and t >= 250))):
+                plane.put(c.table[0, t // 16], t % 16, np.zeros((1, 128), np.float16))
+                keep[0][t] = 0
+    check(decode(pk, c), c)
+    check(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("page,Hq,H", [(16, 8, 1), (64, 6, 2), (32, 5, 5), (256, 34, 2)])
 def test_prefill(pk, cache, D, page, Hq, H):
