@@ -45,28 +45,29 @@ def _rows(t, name):
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens, heads, head_dim]")
     T, H, D = t.shape
-    s = t.stride()
-    if (s[2] != 1 and D > 1) or (s[1] != D and H > 1):
+    row, head, one = t.stride()
+    if (one != 1 and D > 1) or (head != D and H > 1):
         raise ValueError(f"the heads of {name}'s rows must be contiguous")
-    return t.data_ptr(), s[0] if T > 1 else H * D
+    return t.data_ptr(), row if T > 1 else H * D
 
 
 def _planes(k_pages, v_pages, kv_heads, head_dim, page, cache):
     torch = _torch()
     kp, vp = _dev(k_pages, torch.uint8, "k_pages"), _dev(v_pages, torch.uint8, "v_pages")
     n = apex4_kv_page_bytes(cache, kv_heads, head_dim, page)
-    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-        if t.dim() != 2 or t.shape[1] != n:
-            raise ValueError(f"{name} must be [pages, {n}]: {kv_heads} heads of {head_dim}, {page} tokens a page, {cache}")
-    if k_pages.shape[0] != v_pages.shape[0]:
-        raise ValueError("k_pages and v_pages must have as many pages")
-    return kp, vp, k_pages.shape[0]
+    shape = k_pages.shape
+    if len(shape) != 2 or shape[1] != n or v_pages.shape != shape:
+        raise ValueError(f"k_pages and v_pages must be [pages, {n}]: {kv_heads} heads of {head_dim}, {page} tokens a page, "
+                         f"{cache}")
+    return kp, vp, shape[0]
 
 
 def _tables(table, kv_len):
-    if table.dim() != 2 or kv_len.dim() != 1 or table.shape[0] != kv_len.shape[0]:
+    shape = table.shape
+    if len(shape) != 2 or kv_len.shape != shape[:1]:
         raise ValueError("table must be [B, width] and kv_len [B]")
-    return _index(table, "table"), table.shape[1], _index(kv_len, "kv_len"), table.shape[0]
+    i32 = _torch().int32
+    return _dev(table, i32, "table"), shape[1], _dev(kv_len, i32, "kv_len"), shape[0]
 
 
 def _starts(q_start, B):
@@ -78,9 +79,8 @@ def _starts(q_start, B):
 
 
 def _output(out, shape, like):
-    torch = _torch()
     if out is None:
-        return torch.empty(shape, dtype=torch.float16, device=like.device)
+        return like.new_empty(shape, dtype=_torch().float16)
     if tuple(out.shape) != tuple(shape):
         raise ValueError(f"the output must be {tuple(shape)}")
     return out
@@ -88,12 +88,12 @@ def _output(out, shape, like):
 
 def _workspace(workspace, need, like):
     """(pointer, bytes): the caller's, or one made here where one is needed."""
-    torch = _torch()
     if workspace is None:
         if not need:
             return None, 0, None
-        workspace = torch.empty((need,), dtype=torch.uint8, device=like.device)
-    return _dev(workspace, torch.uint8, "workspace"), workspace.numel(), workspace
+        workspace = like.new_empty((need,), dtype=_torch().uint8)
+        return workspace.data_ptr(), need, workspace
+    return _dev(workspace, _torch().uint8, "workspace"), workspace.numel(), workspace
 
 
 @functools.lru_cache(maxsize=256)

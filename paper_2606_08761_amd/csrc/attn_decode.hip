@@ -26,7 +26,8 @@
 // maximum is then that of the score plus log2 of the value's scale, so that
 // weights times scales, whatever the scales are, stay in binary16's range.
 //
-// Four waves share a range of positions and add their sums through LDS; with
+// Four waves (eight where the workgroups are few) share a range of positions and
+// add their sums through LDS; with
 // more than one range a sequence, a second kernel joins the ranges' sums in
 // order (the same bits every time).
 #include "attn_core.h"
@@ -37,12 +38,12 @@ namespace {
 using namespace attn;
 
 constexpr int kTile = 32;      // positions a wave takes at a time
-constexpr int kWaves = 4;
 constexpr int kMaxTiles = 64;  // tiles of a range at most
+constexpr int kOneRange = 40;  // tiles that are not cut: 5 rounds of eight waves
 constexpr int kHeads = 16;     // query heads a workgroup takes
 
-template <int D, bool I4>
-__global__ __launch_bounds__(64 * kWaves, 3) void attn_decode_kernel(KvView c, AttnArgs a, int S, int range,
+template <int D, bool I4, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_kernel(KvView c, AttnArgs a, int S, int range,
                                                                   int head_tiles, float* __restrict__ part,
                                                                   float* __restrict__ ml) {
     constexpr int DV = D / 16;  // values d of a lane in the second product
@@ -68,9 +69,28 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_decode_kernel(KvView c, A
     const int heads = min(kHeads, group - ht * kHeads);  // of this workgroup
     const int64_t row0 = static_cast<int64_t>(b) * a.heads + h * group + ht * kHeads;
 
+    // The range's pages: an entry for every tile, or for each half of one, one a
+    // thread.  Without a window their places in the table do not wait for the length.
+    static_assert(2 * kMaxTiles <= 64 * kWaves);
+    const int halves = c.page_shift == 4 ? 2 : 1;
+    const int t0 = split * range;
+    int page = 0;
+    if (a.window == 0) page = page_of(c, b, (t0 + tid / halves) * kTile + (tid % halves) * 16);
+    // q as the right operand of the first product: head r16, d = 32 s + 8 g4 ..
+    // (codes: a lane holds 8 KS consecutive d of its position)
+    u32x4 qf[KS];
+    {
+        const uint16_t* q = a.q + b * a.q_stride + static_cast<int64_t>(h * group + ht * kHeads + r16) * D;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            qf[s] = u32x4{0u, 0u, 0u, 0u};
+            if (r16 < heads) qf[s] = *reinterpret_cast<const u32x4*>(q + (I4 ? 8 * KS * g4 + 8 * s : 32 * s + 8 * g4));
+            if constexpr (I4) qf[s] = code_order(qf[s]);
+        }
+    }
     const int len = cached_tokens(c, b);
     const Tiles<kTile> tiles(len - 1, len - 1, a.window, a.sinks);
-    const int t0 = split * range, t1 = min(t0 + range, tiles.count);
+    const int t1 = min(t0 + range, tiles.count);
     if (t0 >= t1) {
         if (S > 1) {
             if (tid < heads) {
@@ -85,28 +105,9 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_decode_kernel(KvView c, A
         return;
     }
 
-    // the range's pages: an entry for every tile, or for each half of one
-    const int halves = c.page_shift == 4 ? 2 : 1;
-    for (int i = tid; i < (t1 - t0) * halves; i += 64 * kWaves) {
-        const int at = tiles.start(t0 + i / halves) + (i % halves) * 16;
-        const int p = page_of(c, b, at);
-        pages[i] = p < 0 ? 0 : p;  // positions past the last page are masked, and read page 0
-    }
-
-    // q as the right operand of the first product: head r16, d = 32 s + 8 g4 ..
-    // (codes: a lane holds 8 KS consecutive d of its position)
-    u32x4 qf[KS];
-    {
-        const uint16_t* q = a.q + b * a.q_stride + static_cast<int64_t>(h * group + ht * kHeads + r16) * D;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            qf[s] = u32x4{0u, 0u, 0u, 0u};
-            if (r16 < heads) {
-                qf[s] = *reinterpret_cast<const u32x4*>(q + (I4 ? 8 * KS * g4 + 8 * s : 32 * s + 8 * g4));
-                if constexpr (I4) qf[s] = code_order(qf[s]);
-            }
-        }
-    }
+    if (a.window != 0 && tid < (t1 - t0) * halves)
+        page = page_of(c, b, tiles.start(t0 + tid / halves) + (tid % halves) * 16);
+    if (tid < 2 * kMaxTiles) pages[tid] = page < 0 ? 0 : page;  // positions past the last page are masked, and read page 0
     __syncthreads();
 
     const int page_mask = (1 << c.page_shift) - 1;
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_decode_kernel(KvView c, A
                     f32x4{o[i][r] * f, o[i + 1][r] * f, o[i + 2][r] * f, o[i + 3][r] * f};
     }
     __syncthreads();
-    constexpr int PT = kHeads * D / (64 * kWaves);  // values a thread adds
+    constexpr int PT = kHeads * D / (64 * kWaves) > 4 ? kHeads * D / (64 * kWaves) : 4;  // values a thread adds
     const int hd = tid / (D / PT), d0 = (tid % (D / PT)) * PT;
     if (hd >= heads) return;
     float y[PT];
@@ -476,13 +477,17 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const float* __restrict_
 }
 
 struct Plan {
+    int waves;
     int head_tiles;
     int range;   // tiles of a range
     int S;       // ranges a sequence
 };
 
-// The longest sequence's tiles cut into ranges so that the workgroups number
-// about four a compute unit, of one to 32 tiles a wave.
+// A range for every sequence where that is quick: the second launch costs 4 us
+// (and as much again on the host), a round of the waves, one tile each, 1.1 us
+// (int4: 0.7).  Otherwise the longest sequence's tiles are cut so that the workgroups
+// number about four a compute unit, of up to 8 tiles a wave (int4: 16).  Eight
+// waves where the workgroups of whole sequences leave compute units idle.
 Plan plan_decode(const KvView& c, const AttnArgs& a) {
     Plan p;
     p.head_tiles = (a.heads / c.kv_heads + kHeads - 1) / kHeads;
@@ -494,11 +499,15 @@ Plan plan_decode(const KvView& c, const AttnArgs& a) {
         tiles = std::min(full, w);
     }
     tiles = std::max<int64_t>(tiles, 1);
-    const int64_t units = static_cast<int64_t>(c.B) * c.kv_heads * p.head_tiles;
-    const int64_t want = (4 * device_cu_count() + units - 1) / units;
-    int64_t range = (tiles + want - 1) / want;
-    range = std::min<int64_t>(std::max<int64_t>(range, kWaves), c.i4 ? kMaxTiles : kMaxTiles / 2);
-    p.range = static_cast<int>((range + kWaves - 1) / kWaves * kWaves);
+    const int64_t units = static_cast<int64_t>(c.B) * c.kv_heads * p.head_tiles, cu = device_cu_count();
+    const bool few = units <= cu;
+    p.waves = few && tiles <= kOneRange ? 8 : 4;
+    int64_t range = (tiles + kOneRange - 1) / kOneRange * kOneRange;
+    if (tiles > kOneRange) {
+        const int64_t want = (4 * cu + units - 1) / units;
+        range = std::min<int64_t>(std::max<int64_t>((tiles + want - 1) / want, p.waves), c.i4 ? kMaxTiles : kMaxTiles / 2);
+    }
+    p.range = static_cast<int>((range + p.waves - 1) / p.waves * p.waves);
     p.S = static_cast<int>((tiles + p.range - 1) / p.range);
     return p;
 }
@@ -532,10 +541,16 @@ hipError_t launch_attn_decode(const KvView& c, const AttnArgs& a, hipStream_t st
     float* part = static_cast<float*>(a.workspace);
     float* ml = part + a.T * a.heads * p.S * c.D;
     auto run = [&](auto kernel) {
-        kernel<<<static_cast<unsigned>(blocks_of(c, p)), 64 * kWaves, 0, stream>>>(c, a, p.S, p.range, p.head_tiles, part, ml);
+        kernel<<<static_cast<unsigned>(blocks_of(c, p)), 64 * p.waves, 0, stream>>>(c, a, p.S, p.range, p.head_tiles, part, ml);
     };
-    if (c.D == 128) c.i4 ? run(attn_decode_kernel<128, true>) : run(attn_decode_kernel<128, false>);
-    else c.i4 ? run(attn_decode_kernel<64, true>) : run(attn_decode_kernel<64, false>);
+    auto pick = [&](auto few, auto many) { p.waves == 8 ? run(few) : run(many); };
+    if (c.D == 128) {
+        if (c.i4) pick(attn_decode_kernel<128, true, 8>, attn_decode_kernel<128, true, 4>);
+        else pick(attn_decode_kernel<128, false, 8>, attn_decode_kernel<128, false, 4>);
+    } else {
+        if (c.i4) pick(attn_decode_kernel<64, true, 8>, attn_decode_kernel<64, true, 4>);
+        else pick(attn_decode_kernel<64, false, 8>, attn_decode_kernel<64, false, 4>);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.S == 1) return e;
     return launch_attn_join(part, ml, a.T * a.heads, p.S, c.D, a.out, stream);
