@@ -31,8 +31,18 @@ def _kind(cache):
         raise ValueError("cache must be 'fp16' or 'int4'") from None
 
 
+def _ptr(t, dtype, name):
+    """_dev, quicker where nothing is wrong (small calls are bound by this)."""
+    try:
+        if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _dev(t, dtype, name)
+
+
 def _index(t, name):
-    return _dev(t, _torch().int32, name)
+    return _ptr(t, _torch().int32, name)
 
 
 def _rows(t, name):
@@ -53,7 +63,7 @@ def _rows(t, name):
 
 def _planes(k_pages, v_pages, kv_heads, head_dim, page, cache):
     torch = _torch()
-    kp, vp = _dev(k_pages, torch.uint8, "k_pages"), _dev(v_pages, torch.uint8, "v_pages")
+    kp, vp = _ptr(k_pages, torch.uint8, "k_pages"), _ptr(v_pages, torch.uint8, "v_pages")
     n = apex4_kv_page_bytes(cache, kv_heads, head_dim, page)
     shape = k_pages.shape
     if len(shape) != 2 or shape[1] != n or v_pages.shape != shape:
@@ -67,7 +77,7 @@ def _tables(table, kv_len):
     if len(shape) != 2 or kv_len.shape != shape[:1]:
         raise ValueError("table must be [B, width] and kv_len [B]")
     i32 = _torch().int32
-    return _dev(table, i32, "table"), shape[1], _dev(kv_len, i32, "kv_len"), shape[0]
+    return _ptr(table, i32, "table"), shape[1], _ptr(kv_len, i32, "kv_len"), shape[0]
 
 
 def _starts(q_start, B):
@@ -129,7 +139,7 @@ def apex4_kv_gather(k_pages, v_pages, table, kv_len, T: int, kv_heads: int, head
     kpp, vpp, n = _planes(k_pages, v_pages, kv_heads, head_dim, page, cache)
     tp, width, lp, B = _tables(table, kv_len)
     rc = lib().apex4_kv_gather(kpp, vpp, n, tp, width, lp, B, kv_heads, head_dim, page, _kind(cache), _starts(q_start, B), T,
-                               _dev(k, torch.float16, "k"), _dev(v, torch.float16, "v"), _stream(k_pages, stream))
+                               _ptr(k, torch.float16, "k"), _ptr(v, torch.float16, "v"), _stream(k_pages, stream))
     _check("apex4_kv_gather", rc)
     return k, v
 
@@ -180,7 +190,7 @@ def apex4_attn_decode(q, k_pages, v_pages, table, kv_len, kv_heads: int, page: i
     need = _decode_need(q.get_device(), B, width, most, H, kv_heads, D, page, window, sinks) if workspace is None else 0
     wp, wn, held = _workspace(workspace, need, q)
     rc = lib().apex4_attn_decode(qp, qs, kpp, vpp, n, tp, width, lp, B, most, H, kv_heads, D, page, _kind(cache), window,
-                                 sinks, 1.0 / math.sqrt(D) if scale is None else scale, _dev(out, torch.float16, "out"), wp,
+                                 sinks, 1.0 / math.sqrt(D) if scale is None else scale, _ptr(out, torch.float16, "out"), wp,
                                  wn, _stream(q, stream))
     _check("apex4_attn_decode", rc)
     return out
@@ -206,11 +216,12 @@ def apex4_attn_prefill(q, q_start, k_pages, v_pages, table, kv_len, kv_heads: in
     wp, wn, held = _workspace(workspace, need, q)
     rc = lib().apex4_attn_prefill(qp, qs, sp, T, most_q, kpp, vpp, n, tp, width, lp, B, most, H, kv_heads, D, page,
                                   _kind(cache), window, sinks, 1.0 / math.sqrt(D) if scale is None else scale,
-                                  _dev(out, torch.float16, "out"), wp, wn, _stream(q, stream))
+                                  _ptr(out, torch.float16, "out"), wp, wn, _stream(q, stream))
     _check("apex4_attn_prefill", rc)
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def apex4_pages_workspace_size(n_pages: int, n: int) -> int:
     """Bytes of workspace the page calls need for n slots."""
     b = ctypes.c_int64(0)
@@ -229,12 +240,11 @@ def _pool(pool, refs):
     torch = _torch()
     if pool.dim() != 3 or pool.shape[1] != refs.shape[0]:
         raise ValueError("pool must be [planes, pages, page bytes]")
-    return _dev(pool, torch.uint8, "pool"), pool.shape[0], pool.shape[2]
+    return _ptr(pool, torch.uint8, "pool"), pool.shape[0], pool.shape[2]
 
 
 def _status(status, like):
-    torch = _torch()
-    return torch.empty((1,), dtype=torch.int32, device=like.device) if status is None else status
+    return like.new_empty((1,)) if status is None else status
 
 
 def _pages_work(workspace, n_pages, n, like):

@@ -79,12 +79,26 @@ int make_attn(AttnArgs& a, const KvView& c, const void* q, int64_t q_stride, con
     a.q_stride = q_stride;
     a.q_start = q_start;
     a.T = T;
-    a.max_q = max_q;
+    a.max_q = min64(max_q, T);  // a sequence has no more
     a.heads = static_cast<int>(heads);
     a.window = static_cast<int>(min64(window, kMaxLen));
     a.sinks = static_cast<int>(min64(sinks, kMaxLen));
     a.scale = scale;
     a.out = static_cast<uint16_t*>(out);
+    return APEX4_OK;
+}
+
+// The workspace that serves either kind of cache.
+int largest(KvView c, const AttnArgs& a, bool empty, int64_t (*size)(const KvView&, const AttnArgs&), int64_t* bytes) {
+    int64_t most = 0;
+    for (const bool i4 : {false, true}) {
+        if (empty) break;
+        c.i4 = i4;
+        const int64_t need = size(c, a);
+        if (need < 0) return APEX4_ERR_SHAPE;
+        most = need > most ? need : most;
+    }
+    *bytes = most;
     return APEX4_OK;
 }
 
@@ -165,9 +179,7 @@ int apex4_attn_decode_workspace_size(int64_t B, int64_t width, int64_t max_len, 
     if (rc) return rc;
     if ((rc = make_attn(a, c, nullptr, heads * head_dim, nullptr, B, 1, heads, window, sinks, 1.f, nullptr))) return rc;
     if ((rc = check_device())) return rc;
-    const int64_t need = B == 0 ? 0 : apex4::attn_decode_workspace(c, a);
-    if (need < 0) return APEX4_ERR_SHAPE;
-    *bytes = need;
+    return largest(c, a, B == 0, apex4::attn_decode_workspace, bytes);
     return APEX4_OK;
 }
 
@@ -201,9 +213,7 @@ int apex4_attn_prefill_workspace_size(int64_t T, int64_t B, int64_t max_q, int64
     if (rc) return rc;
     if ((rc = make_attn(a, c, nullptr, heads * head_dim, nullptr, T, max_q, heads, window, sinks, 1.f, nullptr))) return rc;
     if ((rc = check_device())) return rc;
-    const int64_t need = T == 0 || B == 0 || max_q == 0 ? 0 : apex4::attn_prefill_workspace(c, a);
-    if (need < 0) return APEX4_ERR_SHAPE;
-    *bytes = need;
+    return largest(c, a, T == 0 || B == 0 || max_q == 0, apex4::attn_prefill_workspace, bytes);
     return APEX4_OK;
 }
 

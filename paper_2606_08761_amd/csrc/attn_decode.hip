@@ -1,5 +1,5 @@
-// Attention of one new token a sequence over the paged cache, its length split
-// over workgroups and joined.
+// Attention of one new token a sequence, or a few, over the paged cache, its length
+// split over workgroups and joined.
 //
 //   o = sum_t e^(s_t - m) v_t / sum_t e^(s_t - m),  s_t = scale q . k_t, m = max s_t
 //
@@ -40,18 +40,18 @@ using namespace attn;
 constexpr int kTile = 32;      // positions a wave takes at a time
 constexpr int kMaxTiles = 64;  // tiles of a range at most
 constexpr int kOneRange = 40;  // tiles that are not cut: 5 rounds of eight waves
-constexpr int kHeads = 16;     // query heads a workgroup takes
+constexpr int kRows = 16;      // rows (new token, query head) a workgroup takes
 
 template <int D, bool I4, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_kernel(KvView c, AttnArgs a, int S, int range,
-                                                                  int head_tiles, float* __restrict__ part,
+                                                                  int row_tiles, float* __restrict__ part,
                                                                   float* __restrict__ ml) {
     constexpr int DV = D / 16;  // values d of a lane in the second product
     constexpr int KS = D / 32;  // products along d in the first
     constexpr int P = D + 4;    // floats a row of the sums takes in LDS (rows 16 bytes apart in the banks)
     __shared__ int32_t pages[2 * kMaxTiles];
-    __shared__ float sum_ml[2][kWaves][kHeads];
-    __shared__ __align__(16) float sums[kWaves][kHeads][P];
+    __shared__ float sum_ml[2][kWaves][kRows];
+    __shared__ __align__(16) float sums[kWaves][kRows][P];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
     // Workgroups go to the 8 XCDs in turn.  Every group of 8 is rotated by its
@@ -61,13 +61,30 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
     if ((id | 7) < gridDim.x) id = (id & ~7u) | ((id + (id >> 3)) & 7u);
     const int h = static_cast<int>(id % c.kv_heads);
     id /= c.kv_heads;
-    const int ht = static_cast<int>(id % head_tiles);
-    id /= head_tiles;
+    const int rt = static_cast<int>(id % row_tiles);
+    id /= row_tiles;
     const int b = static_cast<int>(id % c.B);
     const int split = static_cast<int>(id / c.B);
     const int group = a.heads / c.kv_heads;
-    const int heads = min(kHeads, group - ht * kHeads);  // of this workgroup
-    const int64_t row0 = static_cast<int64_t>(b) * a.heads + h * group + ht * kHeads;
+    // the sequence's rows of this key head: its new tokens times the heads that share it
+    const int q0 = a.q_start ? a.q_start[b] : b;
+    const int n = a.q_start ? a.q_start[b + 1] - q0 : 1;
+    const int64_t all_rows = static_cast<int64_t>(n) * group;
+    if (static_cast<int64_t>(rt) * kRows >= all_rows) return;
+    const int rows = static_cast<int>(all_rows - rt * kRows < kRows ? all_rows - rt * kRows : kRows);  // of this workgroup
+    struct Row {
+        int tok, head;
+        bool valid;
+        int64_t at;  // its number among all tokens' heads
+    };
+    auto row_of = [&](int r) {
+        Row x;
+        x.tok = (rt * kRows + r) / group;
+        x.head = h * group + (rt * kRows + r) % group;
+        x.at = (static_cast<int64_t>(q0) + x.tok) * a.heads + x.head;
+        x.valid = r < rows && q0 >= 0 && q0 + x.tok < a.T;
+        return x;
+    };
 
     // The range's pages: an entry for every tile, or for each half of one, one a
     // thread.  Without a window their places in the table do not wait for the length.
@@ -79,28 +96,35 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
     // q as the right operand of the first product: head r16, d = 32 s + 8 g4 ..
     // (codes: a lane holds 8 KS consecutive d of its position)
     u32x4 qf[KS];
+    int tok;
     {
-        const uint16_t* q = a.q + b * a.q_stride + static_cast<int64_t>(h * group + ht * kHeads + r16) * D;
+        const Row x = row_of(r16);
+        tok = x.tok;
+        const uint16_t* q = a.q + (q0 + x.tok) * a.q_stride + x.head * D;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             qf[s] = u32x4{0u, 0u, 0u, 0u};
-            if (r16 < heads) qf[s] = *reinterpret_cast<const u32x4*>(q + (I4 ? 8 * KS * g4 + 8 * s : 32 * s + 8 * g4));
+            if (x.valid) qf[s] = *reinterpret_cast<const u32x4*>(q + (I4 ? 8 * KS * g4 + 8 * s : 32 * s + 8 * g4));
             if constexpr (I4) qf[s] = code_order(qf[s]);
         }
     }
     const int len = cached_tokens(c, b);
-    const Tiles<kTile> tiles(len - 1, len - 1, a.window, a.sinks);
+    const int pos = len - n + tok;  // of the lane's row (negative: it sees nothing)
+    const Tiles<kTile> tiles(len - n, len - 1, a.window, a.sinks);
     const int t1 = min(t0 + range, tiles.count);
     if (t0 >= t1) {
         if (S > 1) {
-            if (tid < heads) {
-                float* o = ml + ((row0 + tid) * S + split) * 2;
+            const Row x = row_of(tid);
+            if (x.valid) {
+                float* o = ml + (x.at * S + split) * 2;
                 o[0] = kNoMax;
                 o[1] = 0.f;
             }
         } else {
-            for (int i = tid; i < heads * (D / 8); i += 64 * kWaves)
-                reinterpret_cast<u32x4*>(a.out + row0 * D)[i] = u32x4{0u, 0u, 0u, 0u};
+            for (int i = tid; i < rows * (D / 8); i += 64 * kWaves) {
+                const Row x = row_of(i / (D / 8));
+                if (x.valid) reinterpret_cast<u32x4*>(a.out + x.at * D)[i % (D / 8)] = u32x4{0u, 0u, 0u, 0u};
+            }
         }
         return;
     }
@@ -187,6 +211,9 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
         minus *= -72.f;
     }
 
+    // first position that the windows of all rows hold
+    const int edge = a.window ? len - a.window : 0;
+
     // One tile.  more(): issues the loads that may go out once the keys, and
     // more_v() once the values, are used.
     auto step = [&](int t, Loaded& x, auto more_k, auto more_v) {
@@ -213,20 +240,21 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
             }
         }
         more_k();
-        // positions past the end, or between the first ones and the window: their
-        // scores do not count, and their values, whatever they are, are zero
-        const bool masked = at + kTile > len || (at < tiles.lo && at + kTile > tiles.sinks);
+        // positions that a row does not see: their scores do not count, and the values
+        // of those that no row sees, whatever they are, are zero
+        const bool masked = at + kTile > len - n + 1 || (at < edge && at + kTile > tiles.sinks);
         if (masked) {
+            const int from = a.window ? pos - a.window + 1 : 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int p = at + v_off + j;
-                const bool seen = p < len && (p >= tiles.lo || p < tiles.sinks);
+                const bool seen = p <= pos && (p >= from || p < a.sinks), some = p < len && (p >= tiles.lo || p < tiles.sinks);
                 y[j] = seen ? y[j] : -INFINITY;
                 if constexpr (I4) {
-                    x.vs[j >> 1] &= seen ? 0xFFFFFFFFu : (j & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+                    x.vs[j >> 1] &= some ? 0xFFFFFFFFu : (j & 1) ? 0x0000FFFFu : 0xFFFF0000u;
                 } else {
 #pragma unroll
-                    for (int i = 0; i < DV / 2; ++i) x.v[j][i] = seen ? x.v[j][i] : 0u;
+                    for (int i = 0; i < DV / 2; ++i) x.v[j][i] = some ? x.v[j][i] : 0u;
                 }
             }
         }
@@ -362,9 +390,10 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
                     f32x4{o[i][r] * f, o[i + 1][r] * f, o[i + 2][r] * f, o[i + 3][r] * f};
     }
     __syncthreads();
-    constexpr int PT = kHeads * D / (64 * kWaves) > 4 ? kHeads * D / (64 * kWaves) : 4;  // values a thread adds
+    constexpr int PT = kRows * D / (64 * kWaves) > 4 ? kRows * D / (64 * kWaves) : 4;  // values a thread adds
     const int hd = tid / (D / PT), d0 = (tid % (D / PT)) * PT;
-    if (hd >= heads) return;
+    const Row out_row = row_of(hd);
+    if (!out_row.valid) return;
     float y[PT];
 #pragma unroll
     for (int i = 0; i < PT; ++i) y[i] = 0.f;
@@ -387,11 +416,11 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
         uint32_t q[PT / 2];
 #pragma unroll
         for (int i = 0; i < PT / 2; ++i) q[i] = pack_f16(y[2 * i] * inv, y[2 * i + 1] * inv);
-        uint16_t* out = a.out + (row0 + hd) * D + d0;
+        uint16_t* out = a.out + out_row.at * D + d0;
         if constexpr (PT == 8) *reinterpret_cast<u32x4*>(out) = u32x4{q[0], q[1], q[2], q[3]};
         else *reinterpret_cast<u32x2*>(out) = u32x2{q[0], q[1]};
     } else {
-        const int64_t at = (row0 + hd) * S + split;
+        const int64_t at = out_row.at * S + split;
         if (d0 == 0) {
             ml[at * 2] = mt;
             ml[at * 2 + 1] = lt;
@@ -478,7 +507,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const float* __restrict_
 
 struct Plan {
     int waves;
-    int head_tiles;
+    int row_tiles;
     int range;   // tiles of a range
     int S;       // ranges a sequence
 };
@@ -490,16 +519,16 @@ struct Plan {
 // waves where the workgroups of whole sequences leave compute units idle.
 Plan plan_decode(const KvView& c, const AttnArgs& a) {
     Plan p;
-    p.head_tiles = (a.heads / c.kv_heads + kHeads - 1) / kHeads;
+    p.row_tiles = static_cast<int>((a.max_q * (a.heads / c.kv_heads) + kRows - 1) / kRows);
     const int64_t most = std::min<int64_t>(c.max_len, static_cast<int64_t>(c.width) << c.page_shift);
     const int64_t full = (most + kTile - 1) / kTile;
     int64_t tiles = full;
-    if (a.window) {  // the window's tiles (one more where it starts inside one), and the first ones
-        const int64_t w = (static_cast<int64_t>(a.window) + kTile - 2) / kTile + 1 + (static_cast<int64_t>(a.sinks) + kTile - 1) / kTile;
+    if (a.window) {  // the rows' windows (one more where they start inside a tile), and the first positions
+        const int64_t w = (static_cast<int64_t>(a.window) + a.max_q + kTile - 3) / kTile + 1 + (static_cast<int64_t>(a.sinks) + kTile - 1) / kTile;
         tiles = std::min(full, w);
     }
     tiles = std::max<int64_t>(tiles, 1);
-    const int64_t units = static_cast<int64_t>(c.B) * c.kv_heads * p.head_tiles, cu = device_cu_count();
+    const int64_t units = static_cast<int64_t>(c.B) * c.kv_heads * p.row_tiles, cu = device_cu_count();
     const bool few = units <= cu;
     p.waves = few && tiles <= kOneRange ? 8 : 4;
     int64_t range = (tiles + kOneRange - 1) / kOneRange * kOneRange;
@@ -513,7 +542,7 @@ Plan plan_decode(const KvView& c, const AttnArgs& a) {
 }
 
 int64_t blocks_of(const KvView& c, const Plan& p) {
-    return static_cast<int64_t>(c.B) * c.kv_heads * p.head_tiles * p.S;
+    return static_cast<int64_t>(c.B) * c.kv_heads * p.row_tiles * p.S;
 }
 
 }  // namespace
@@ -541,7 +570,7 @@ hipError_t launch_attn_decode(const KvView& c, const AttnArgs& a, hipStream_t st
     float* part = static_cast<float*>(a.workspace);
     float* ml = part + a.T * a.heads * p.S * c.D;
     auto run = [&](auto kernel) {
-        kernel<<<static_cast<unsigned>(blocks_of(c, p)), 64 * p.waves, 0, stream>>>(c, a, p.S, p.range, p.head_tiles, part, ml);
+        kernel<<<static_cast<unsigned>(blocks_of(c, p)), 64 * p.waves, 0, stream>>>(c, a, p.S, p.range, p.row_tiles, part, ml);
     };
     auto pick = [&](auto few, auto many) { p.waves == 8 ? run(few) : run(many); };
     if (c.D == 128) {

@@ -537,6 +537,13 @@ Plan plan_prefill(const KvView& c, const AttnArgs& a) {
     return p;
 }
 
+// Rows (new tokens times the heads that share a key head) up to which the decode
+// kernel, 16 at a time, is the faster one.  14 sequences of 7954 with 8 key heads of
+// 128: binary16 16 rows 92 us against 119, 32 rows 137 against 119 (it reads the
+// cache twice); int4 32 rows 56 against 130, 64 rows 89 against 138 (the codes are
+// made binary16 in LDS by a workgroup whose products are few).
+bool few_rows(const KvView& c, const AttnArgs& a) { return a.max_q * (a.heads / c.kv_heads) <= (c.i4 ? 64 : 16); }
+
 int64_t blocks_of(const KvView& c, const Plan& p) {
     return static_cast<int64_t>(c.B) * c.kv_heads * p.row_tiles * p.S;
 }
@@ -554,19 +561,14 @@ hipError_t run(const KvView& c, const AttnArgs& a, const Plan& p, float* part, f
 }  // namespace
 
 int64_t attn_prefill_workspace(const KvView& c, const AttnArgs& a) {
-    // the size for either kind of cache: callers ask without naming it
-    int64_t most = 0;
-    for (const bool i4 : {false, true}) {
-        KvView v = c;
-        v.i4 = i4;
-        const Plan p = plan_prefill(v, a);
-        if (blocks_of(v, p) > 0x7FFFFFFFll) return -1;
-        most = std::max(most, p.S == 1 ? 0 : a.T * a.heads * p.S * static_cast<int64_t>(c.D + 2) * 4);
-    }
-    return most;
+    if (few_rows(c, a)) return attn_decode_workspace(c, a);
+    const Plan p = plan_prefill(c, a);
+    if (blocks_of(c, p) > 0x7FFFFFFFll) return -1;
+    return p.S == 1 ? 0 : a.T * a.heads * p.S * static_cast<int64_t>(c.D + 2) * 4;
 }
 
 hipError_t launch_attn_prefill(const KvView& c, const AttnArgs& a, hipStream_t stream) {
+    if (few_rows(c, a)) return launch_attn_decode(c, a, stream);
     const Plan p = plan_prefill(c, a);
     float* part = static_cast<float*>(a.workspace);
     float* ml = part + a.T * a.heads * p.S * c.D;

@@ -139,6 +139,18 @@ def test_prefill_window(pk, cache, window, sinks):
 
 
 @pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D,Hq,H", [(128, 8, 2), (64, 3, 3), (128, 7, 1)])
+@pytest.mark.parametrize("most,window,sinks", [(2, 0, 0), (4, 0, 0), (4, 20, 3), (9, 1, 2), (9, 100, 40)])
+def test_prefill_few_rows(pk, cache, D, Hq, H, most, window, sinks):
+    """Few new tokens a sequence, as many as there are and fewer, with each its
+    own mask in the last tile."""
+    lens = [1, 2, 31, 32, 33, 40, 129, 260, 1400]
+    news = [min(n, most - i % 2) for i, n in enumerate(lens)]
+    c = paged.Case(71 + most, lens, news, Hq, H, D, 16, cache, window=window, sinks=sinks)
+    check(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
 def test_prefill_split(pk, cache):
     """Few rows and a long cache: cut along the positions, and joined."""
     c = paged.Case(31, [4100, 900], [3, 2], 8, 1, 128, 64, cache)
