@@ -204,6 +204,7 @@ struct AttnArgs {
     int64_t T = 0;
     int64_t max_q = 1;
     int heads = 0;
+    int group = 1;                    // heads that share a key head
     int window = 0;                   // 0: none
     int sinks = 0;
     float scale = 1.f;

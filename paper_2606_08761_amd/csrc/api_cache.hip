@@ -81,6 +81,7 @@ int make_attn(AttnArgs& a, const KvView& c, const void* q, int64_t q_stride, con
     a.T = T;
     a.max_q = min64(max_q, T);  // a sequence has no more
     a.heads = static_cast<int>(heads);
+    a.group = static_cast<int>(heads / c.kv_heads);
     a.window = static_cast<int>(min64(window, kMaxLen));
     a.sinks = static_cast<int>(min64(sinks, kMaxLen));
     a.scale = scale;

@@ -42,6 +42,12 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     return __builtin_bit_cast(uint32_t, r);
 }
 
+// New tokens of sequence b of the packed ones.
+__device__ __forceinline__ int new_tokens(const AttnArgs& a, int b) {
+    const int n = a.q_start[b + 1] - a.q_start[b];
+    return n < 0 ? 0 : n < a.T ? n : static_cast<int>(a.T);
+}
+
 // Tiles of W positions that rows at positions p_lo .. p_hi see (causal, a
 // window of `window` positions up to the row's own unless it is 0, and the
 // first `sinks`): the tiles of the first positions, then from the window's

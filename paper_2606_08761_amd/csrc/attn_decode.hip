@@ -65,13 +65,13 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
     id /= row_tiles;
     const int b = static_cast<int>(id % c.B);
     const int split = static_cast<int>(id / c.B);
-    const int group = a.heads / c.kv_heads;
+    const uint32_t group = a.group;
     // the sequence's rows of this key head: its new tokens times the heads that share it
     const int q0 = a.q_start ? a.q_start[b] : b;
-    const int n = a.q_start ? a.q_start[b + 1] - q0 : 1;
-    const int64_t all_rows = static_cast<int64_t>(n) * group;
-    if (static_cast<int64_t>(rt) * kRows >= all_rows) return;
-    const int rows = static_cast<int>(all_rows - rt * kRows < kRows ? all_rows - rt * kRows : kRows);  // of this workgroup
+    const int n = a.q_start ? new_tokens(a, b) : 1;
+    const uint32_t all_rows = n * group, row0 = rt * kRows;  // T heads and max_q heads are below 2^28
+    if (row0 >= all_rows) return;
+    const int rows = min(static_cast<int>(all_rows - row0), kRows);  // of this workgroup
     struct Row {
         int tok, head;
         bool valid;
@@ -79,8 +79,8 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
     };
     auto row_of = [&](int r) {
         Row x;
-        x.tok = (rt * kRows + r) / group;
-        x.head = h * group + (rt * kRows + r) % group;
+        x.tok = (row0 + r) / group;
+        x.head = h * group + (row0 + r) - x.tok * group;
         x.at = (static_cast<int64_t>(q0) + x.tok) * a.heads + x.head;
         x.valid = r < rows && q0 >= 0 && q0 + x.tok < a.T;
         return x;

@@ -102,33 +102,34 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     id /= S;
     const int b = static_cast<int>(id % c.B);
     const int mt = row_tiles - 1 - static_cast<int>(id / c.B);  // the last rows see the most: first
-    const int group = a.heads / c.kv_heads;
+    const uint32_t group = a.group;
 
     const int q0 = a.q_start[b];
-    const int n = a.q_start[b + 1] - q0;
-    const int64_t rows = static_cast<int64_t>(n) * group;
-    const int64_t R0 = static_cast<int64_t>(mt) * kRows;
+    const int n = new_tokens(a, b);
+    const uint32_t rows = n * group, R0 = mt * kRows;  // T heads and max_q heads are below 2^28
     if (R0 >= rows) return;
     const int len = cached_tokens(c, b);
     const int before = len - n;  // position of the sequence's first new token (negative: it has no place)
-    const int p_lo = before + static_cast<int>(R0 / group);
+    const uint32_t tok0 = R0 / group;
+    const int p_lo = before + static_cast<int>(tok0);
     const int p_hi = before + static_cast<int>(((R0 + kRows < rows ? R0 + kRows : rows) - 1) / group);
     const Tiles<kW> tiles(p_lo, p_hi, a.window, a.sinks);
-    const int t0 = static_cast<int>(static_cast<int64_t>(tiles.count) * split / S);
-    const int t1 = static_cast<int>(static_cast<int64_t>(tiles.count) * (split + 1) / S);
+    // the split's share of the tiles (below 2^24 of them, S below 2^8)
+    const int t0 = S == 1 ? 0 : static_cast<uint32_t>(tiles.count) * split / static_cast<uint32_t>(S);
+    const int t1 = S == 1 ? tiles.count : static_cast<uint32_t>(tiles.count) * (split + 1) / static_cast<uint32_t>(S);
 
     // the lane's row
-    const int r_wave = static_cast<int>(R0 % group) + 32 * wave;  // of the tile's first token
-    const int tok_wave = static_cast<int>(R0 / group);
+    const uint32_t r_wave = R0 - tok0 * group + 32 * wave;  // of the tile's first token
     struct Row {
         int tok, head;
         bool valid;
     };
     auto row_of = [&](int r) {
         Row x;
-        x.tok = tok_wave + (r_wave + r) / group;
-        x.head = h * group + (r_wave + r) % group;
-        x.valid = x.tok < n && R0 + 32 * wave + r < rows && q0 >= 0 && q0 + x.tok < a.T;
+        const uint32_t t = (r_wave + r) / group;
+        x.tok = tok0 + t;
+        x.head = h * group + (r_wave + r - t * group);
+        x.valid = R0 + 32 * wave + r < rows && q0 >= 0 && q0 + x.tok < a.T;
         return x;
     };
     const bool idle = R0 + 32 * wave >= rows;  // a wave without rows only stages
