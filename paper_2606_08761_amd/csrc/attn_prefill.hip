@@ -105,25 +105,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     // ragged chunks took 137 us instead of 96.)
     int b = static_cast<int>(id / row_tiles);
     const int from_last = static_cast<int>(id) - b * row_tiles;
+    int q0, n, len;
     {
-        const int first = b & ~63, many = min(c.B - first, 64);
-        const int mine = lane < many ? cached_tokens(c, first + lane) : -1;
+        const int first = b & ~63, many = min(c.B - first, 64), x = first + min(lane, many - 1);
+        const int mine = cached_tokens(c, x), q_mine = a.q_start[x], n_mine = new_tokens(a, x);
         int rank = 0;
         for (int i = 0; i < many; ++i) {
             const int other = __builtin_amdgcn_readlane(mine, i);
             rank += other > mine || (other == mine && i < lane);
         }
-        b = first + __builtin_ctzll(__ballot(lane < many && rank == b - first));  // one lane has each rank
+        const int at = __builtin_ctzll(__ballot(lane < many && rank == b - first));  // one lane has each rank
+        b = first + at;
+        q0 = __builtin_amdgcn_readlane(q_mine, at);
+        n = __builtin_amdgcn_readlane(n_mine, at);
+        len = __builtin_amdgcn_readlane(mine, at);
     }
     const uint32_t group = a.group;
 
-    const int q0 = a.q_start[b];
-    const int n = new_tokens(a, b);
     const uint32_t rows = n * group;  // T heads and max_q heads are below 2^28
     const int mt = static_cast<int>((rows + kRows - 1) / kRows) - 1 - from_last;
     if (mt < 0) return;
     const uint32_t R0 = mt * kRows;
-    const int len = cached_tokens(c, b);
     const int before = len - n;  // position of the sequence's first new token (negative: it has no place)
     const uint32_t tok0 = R0 / group;
     const int p_lo = before + static_cast<int>(tok0);

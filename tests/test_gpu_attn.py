@@ -151,6 +151,17 @@ def test_prefill_few_rows(pk, cache, D, Hq, H, most, window, sinks):
 
 
 @pytest.mark.parametrize("cache", ["fp16", "int4"])
+def test_prefill_many_sequences(pk, cache):
+    """More sequences than one wave orders by length, equal lengths among them."""
+    g = np.random.default_rng(5)
+    news = g.integers(0, 40, 131)
+    news[::7] = 33
+    lens = news + g.integers(0, 3, 131) * 16
+    c = paged.Case(73, lens.tolist(), news.tolist(), 3, 1, 64, 16, cache)
+    check(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
 def test_prefill_split(pk, cache):
     """Few rows and a long cache: cut along the positions, and joined."""
     c = paged.Case(31, [4100, 900], [3, 2], 8, 1, 128, 64, cache)
