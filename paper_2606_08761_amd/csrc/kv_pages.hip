@@ -5,9 +5,9 @@
 // and one reference count a page; a page is free where its count is zero, and
 // free pages are handed out lowest first, so that every result is a function of
 // the state alone.  The bookkeeping of reserve, fork and compact is one
-// workgroup: it reads the counts 4096 at a time and ranks the pages it looks for
-// by a scan (a cache of 288 GB has some ten thousand pages, a few steps; a pass
-// costs about 2 us, and the launch).  The data then moves in one launch over
+// workgroup: it reads the counts 16384 at a time, ahead of what else it looks up,
+// and ranks the pages it looks for by one scan (a cache of 288 GB has some ten
+// thousand pages); a chain of a few latencies.  The data then moves in one launch over
 // all planes, bound by HBM: 2 page_bytes a moved page and plane.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -45,39 +45,76 @@ __device__ __forceinline__ int scan(int v, int* total) {
     return before + s - v;
 }
 
-// Writes the pages p in [from, to) with pick(refs[p]) to list[0 .. most), in
-// ascending order; returns how many there are, or some number >= most once that
-// many are found.
-template <class Pick>
-__device__ __forceinline__ int list_pages(const int32_t* refs, int from, int to, Pick pick, int32_t* list, int most) {
+// A chunk of kSpan pages: a thread has every 1024th, bit i of its word for page
+// 1024 i + thread of the chunk, so that the loads lie side by side and do not wait
+// for one another.
+constexpr int kPer = 16, kSpan = kPer * kThreads;
+// Numbers i that hold a page at all: a small pool's chunk has few.
+__device__ __forceinline__ int numbers_of(int n_pages, int chunk) {
+    const int64_t n = (n_pages - static_cast<int64_t>(chunk) * kSpan + kThreads - 1) / kThreads;
+    return n < kPer ? static_cast<int>(n) : kPer;
+}
+__device__ __forceinline__ uint32_t live_bits(const int32_t* refs, int n_pages, int chunk) {
+    const int64_t p0 = static_cast<int64_t>(chunk) * kSpan + threadIdx.x;
+    const int numbers = numbers_of(n_pages, chunk);
+    int32_t r[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        r[i] = 0;
+        if (i < numbers && p0 + i * kThreads < n_pages) r[i] = refs[p0 + i * kThreads];
+    }
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) bits |= r[i] > 0 ? 1u << i : 0u;
+    return bits;
+}
+__device__ __forceinline__ uint32_t pages_here(int n_pages, int chunk) {  // which of the bits are pages at all
+    const int64_t left = n_pages - static_cast<int64_t>(chunk) * kSpan - threadIdx.x;
+    return left <= 0 ? 0u : left > kSpan - kThreads ? 0xFFFFu : (1u << ((left + kThreads - 1) / kThreads)) - 1u;
+}
+__device__ __forceinline__ int chunks_of(int n_pages) { return (n_pages + kSpan - 1) / kSpan; }
+
+// Ranks the set bits of a chunk in page order: before[16 i + wave] is the number
+// of those before a wave's pages of number i.  Returns how many there are.
+__device__ __forceinline__ int rank_bits(uint32_t bits, int numbers, int32_t* before) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();  // what is there is read
+    for (int i = 0; i < numbers; ++i) {
+        const int n = __popcll(__ballot(bits >> i & 1u));
+        if ((threadIdx.x & 63) == 0) before[i * kWavesPerGroup + wave] = n;
+    }
+    __syncthreads();
+    const bool mine = static_cast<int>(threadIdx.x) < numbers * kWavesPerGroup;
+    int all;
+    const int at = scan(mine ? before[threadIdx.x] : 0, &all);
+    if (mine) before[threadIdx.x] = at;
+    __syncthreads();
+    return all;
+}
+// The rank of the thread's page i among the set bits (or, of one that is not set,
+// how many come before it).
+__device__ __forceinline__ int rank_of(uint32_t bits, int i, const int32_t* before) {
+    const uint64_t mask = __ballot(bits >> i & 1u);
+    return before[i * kWavesPerGroup + (threadIdx.x >> 6)] + __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1ull));
+}
+
+// Writes the free pages to list[0 .. most), in ascending order; returns how many
+// there are, or some number >= most once that many are found.  live0: live_bits of
+// the first chunk, loaded before.
+__device__ __forceinline__ int list_free(const int32_t* refs, int n_pages, uint32_t live0, int32_t* before, int32_t* list,
+                                         int most) {
     int found = 0;
-    for (int p0 = from; p0 < to && found < most; p0 += 4 * kThreads) {
-        const int p = p0 + 4 * threadIdx.x;
-        int n = 0, take[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            take[i] = p + i < to && pick(refs[p + i]);
-            n += take[i];
+    for (int c = 0; c < chunks_of(n_pages) && found < most; ++c) {
+        const uint32_t free = ~(c ? live_bits(refs, n_pages, c) : live0) & pages_here(n_pages, c);
+        const int numbers = numbers_of(n_pages, c), all = rank_bits(free, numbers, before);
+        for (int i = 0; i < numbers; ++i) {
+            const int at = found + rank_of(free, i, before);
+            if ((free >> i & 1u) && at < most) list[at] = c * kSpan + i * kThreads + threadIdx.x;
         }
-        int all;
-        int at = found + scan(n, &all);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (take[i]) {
-                if (at < most) list[at] = p + i;
-                ++at;
-            }
         found += all;
     }
     return found;
 }
-
-struct IsFree {
-    __device__ bool operator()(int32_t r) const { return r <= 0; }
-};
-struct IsLive {
-    __device__ bool operator()(int32_t r) const { return r > 0; }
-};
 
 __device__ __forceinline__ int pages_for(int64_t tokens, int shift) {
     return static_cast<int>((tokens + (int64_t{1} << shift) - 1) >> shift);
@@ -92,6 +129,8 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(int32_t* __restrict__
                                                            int32_t* __restrict__ status, int32_t* free_list,
                                                            int32_t* first) {
     __shared__ int too_long;
+    __shared__ int32_t before_of[kPer * kWavesPerGroup];
+    const uint32_t live0 = live_bits(refs, n_pages, 0);
     if (threadIdx.x == 0) too_long = 0;
     __syncthreads();
     int need_all = 0;
@@ -118,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(int32_t* __restrict__
         if (threadIdx.x == 0) *status = -1;
         return;
     }
-    const int found = need_all > n_pages ? 0 : list_pages(refs, 0, n_pages, IsFree(), free_list, need_all);
+    const int found = need_all > n_pages ? 0 : list_free(refs, n_pages, live0, before_of, free_list, need_all);
     if (need_all > found) {
         if (threadIdx.x == 0) *status = need_all - found;
         return;
@@ -154,6 +193,8 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(int32_t* __restrict__ ta
         const int len = max(kv_len[s], 0);
         return (len & ((1 << shift) - 1)) != 0 && (len >> shift) < width;
     };
+    __shared__ int32_t before_of[kPer * kWavesPerGroup];
+    const uint32_t live0 = live_bits(refs, n_pages, 0);
     int need = 0;
     for (int i0 = 0; i0 < n; i0 += kThreads) {
         const int i = i0 + threadIdx.x;
@@ -163,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(int32_t* __restrict__ ta
         if (i < n) dst[i] = one ? need + before : -1;
         need += all;
     }
-    const int found = need > n_pages ? 0 : list_pages(refs, 0, n_pages, IsFree(), free_list, need);
+    const int found = need > n_pages ? 0 : list_free(refs, n_pages, live0, before_of, free_list, need);
     const bool enough = found >= need;
     if (threadIdx.x == 0) *status = enough ? 0 : need - found;
     __syncthreads();  // the lists are written, and no count changes before they are
@@ -219,34 +260,60 @@ __global__ __launch_bounds__(256) void free_kernel(int32_t* __restrict__ table, 
 
 // Live pages past the number of live pages move to the free ones below it:
 // src[i] -> dst[i] (both ascending) for i < *count; to[p] is page p's new id.
+// held[i]: the references of src[i].
 __global__ __launch_bounds__(kThreads) void compact_plan_kernel(int32_t* __restrict__ refs, int n_pages,
                                                                 int32_t* __restrict__ status, int32_t* to, int32_t* src,
-                                                                int32_t* dst, int32_t* __restrict__ count) {
+                                                                int32_t* dst, int32_t* held, int32_t* __restrict__ count) {
+    __shared__ int below_of;
+    __shared__ int32_t before_of[kPer * kWavesPerGroup];
+    const uint32_t live0 = live_bits(refs, n_pages, 0);
+    const int chunks = chunks_of(n_pages);
     int live = 0;
-    for (int p0 = 0; p0 < n_pages; p0 += 4 * kThreads) {
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int p = p0 + 4 * threadIdx.x + i;
+    for (int c = 0; c < chunks; ++c) live += rank_bits(c ? live_bits(refs, n_pages, c) : live0, numbers_of(n_pages, c), before_of);
+    // live pages below page `live`: the others, and as many free pages, change places
+    if (threadIdx.x == 0) below_of = live;
+    __syncthreads();
+    int found = 0;
+    for (int c = 0; c < chunks; ++c) {
+        const uint32_t bits = c ? live_bits(refs, n_pages, c) : live0;
+        const int all = chunks == 1 ? 0 : rank_bits(bits, numbers_of(n_pages, c), before_of);
+        if (live / kSpan == c && live < n_pages) {
+            const int at = found + rank_of(bits, live % kSpan / kThreads, before_of);
+            if (live % kThreads == static_cast<int>(threadIdx.x)) below_of = at;
+        }
+        found += all;
+    }
+    __syncthreads();
+    const int below = below_of, moves = live - below;
+    found = 0;
+    for (int c = 0; c < chunks; ++c) {
+        const uint32_t bits = c ? live_bits(refs, n_pages, c) : live0;
+        const int all = chunks == 1 ? 0 : rank_bits(bits, numbers_of(n_pages, c), before_of);
+        for (int i = 0; i < numbers_of(n_pages, c); ++i) {
+            const int at = found + rank_of(bits, i, before_of);  // live pages before page p
+            const int64_t p = static_cast<int64_t>(c) * kSpan + i * kThreads + threadIdx.x;
+            const bool is_live = bits >> i & 1u;
             if (p < n_pages) {
-                n += refs[p] > 0;
-                to[p] = p;
+                if (is_live && p >= live) {
+                    src[at - below] = static_cast<int>(p);
+                    held[at - below] = refs[p];
+                } else {
+                    to[p] = static_cast<int>(p);
+                    if (!is_live && p < live) dst[p - at] = static_cast<int>(p);
+                }
             }
         }
-        int all;
-        scan(n, &all);
-        live += all;
+        found += all;
     }
-    const int holes = list_pages(refs, 0, live, IsFree(), dst, n_pages);
-    list_pages(refs, live, n_pages, IsLive(), src, n_pages);
-    __syncthreads();  // the lists are written
-    for (int i = threadIdx.x; i < holes; i += kThreads) {
-        to[src[i]] = dst[i];
-        refs[dst[i]] = refs[src[i]];
-        refs[src[i]] = 0;
+    __syncthreads();  // the lists are written, and the counts read
+    for (int i = threadIdx.x; i < moves; i += kThreads) {
+        const int s = src[i], d = dst[i];
+        to[s] = d;
+        refs[d] = held[i];
+        refs[s] = 0;
     }
     if (threadIdx.x == 0) {
-        *count = holes;
+        *count = moves;
         *status = live;
     }
 }
@@ -336,8 +403,9 @@ hipError_t launch_pages_free(const PageTable& p, const int32_t* seqs, int n, hip
 
 hipError_t launch_pages_compact(const PageTable& p, uint8_t* pool, int planes, int64_t page_bytes, int32_t* status,
                                 int32_t* work, hipStream_t stream) {
-    int32_t *to = work, *src = to + p.n_pages, *dst = src + p.n_pages, *count = dst + p.n_pages;
-    compact_plan_kernel<<<1, kThreads, 0, stream>>>(p.refs, p.n_pages, status, to, src, dst, count);
+    // a page moves to another: no more than half of them
+    int32_t *to = work, *src = to + p.n_pages, *held = src + (p.n_pages + 1) / 2, *dst = src + p.n_pages + 1, *count = dst + p.n_pages;
+    compact_plan_kernel<<<1, kThreads, 0, stream>>>(p.refs, p.n_pages, status, to, src, dst, held, count);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t pieces = (page_bytes + kPiece - 1) / kPiece;

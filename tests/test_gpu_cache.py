@@ -167,7 +167,9 @@ class Model:
 @pytest.mark.parametrize("pages,slots,width,page,size,steps", [
     (40, 12, 6, 16, 48, 60),          # runs out of pages often
     (300, 20, 9, 32, 16 * 1027, 60),  # page data that ends inside a 16 KB piece
-    (9000, 2100, 5, 16, 16, 30),      # more slots and pages than a workgroup takes at a time
+    (9000, 2100, 5, 16, 16, 30),      # more slots than a workgroup takes at a time
+    (16384, 2100, 5, 16, 16, 30),     # as many pages as it does
+    (40001, 2100, 30, 16, 16, 30),    # and more
 ])
 def test_page_calls(pk, pages, slots, width, page, size, steps):
     import torch
@@ -209,6 +211,24 @@ def test_page_calls(pk, pages, slots, width, page, size, steps):
     assert ("reserve", 0) in outcomes and ("fork", 0) in outcomes
     if pages == 40:
         assert ("reserve", 1) in outcomes
+
+
+@pytest.mark.parametrize("pages", [1, 15, 16, 17, 16384, 16385, 50000])
+@pytest.mark.parametrize("held", ["none", "all", "low", "high", "mixed"])
+def test_compact(pk, pages, held):
+    """Nothing to move, everything to move, and pools that end at a boundary."""
+    import torch
+    g = np.random.default_rng(pages)
+    refs = {"none": np.zeros(pages), "all": np.ones(pages), "low": np.arange(pages) < pages // 3, "high": np.arange(pages) >= pages - pages // 3,
+            "mixed": g.integers(0, 3, pages)}[held].astype(np.int32)
+    live = np.flatnonzero(refs)
+    m = Model(np.arange(pages, dtype=np.uint8).repeat(16).reshape(1, pages, 16).copy(), max(1, len(live)), 1, 16)
+    m.pool[0, :, :8] = np.arange(pages, dtype=np.int64).view(np.uint8).reshape(pages, 8)
+    m.refs, m.table = refs, (live[:, None] if len(live) else np.full((1, 1), -1)).astype(np.int32)
+    pool, table, d_refs = dev(m.pool), dev(m.table), dev(refs)
+    assert int(pk.apex4_pages_compact(pool, table, d_refs).item()) == m.compact() == len(live)
+    assert np.array_equal(table.cpu().numpy(), m.table) and np.array_equal(d_refs.cpu().numpy(), m.refs)
+    assert np.array_equal(pool.cpu().numpy()[:, :len(live)], m.pool[:, :len(live)])
 
 
 def test_copy_pages(pk):
