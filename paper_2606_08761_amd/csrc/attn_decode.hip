@@ -290,13 +290,23 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
                 w[j] = I4 ? times_half(e[j], x.vs[j >> 1], j & 1) : e[j];
             }
         }
-        u32x4 pw;
+        // A binary16 cache: the weights as a sum of two binary16.  The products are not
+        // what bounds the kernel (the times did not change), and so the rounding of the
+        // weights (2^-11 of one) is gone from the result, which is then as far from 64
+        // bits as its own rounding; with one binary16 1.4 times that.  Codes: one, 1.1
+        // times that; their kernel has no time to spare (94 us would be 103).
+        u32x4 pw, rest;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             pw[j] = pack_f16(w[2 * j], w[2 * j + 1]);
-            if constexpr (I4) l += e[2 * j] + e[2 * j + 1];
-            else l = add_pair(pw[j], l);  // the rounded weights: one large weight's rounding cancels
+            if constexpr (!I4) rest[j] = pack_f16(w[2 * j] - half_of(pw[j], 0), w[2 * j + 1] - half_of(pw[j], 1));
+            l += e[2 * j] + e[2 * j + 1];
         }
+        auto add = [&](int i, const u32x4& v) {
+            o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, pw), o[i], 0, 0, 0);
+            if constexpr (!I4)
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, rest), o[i], 0, 0, 0);
+        };
         // values: 8 positions x DV to DV operands of 8 positions
         if constexpr (I4) {
 #pragma unroll
@@ -308,11 +318,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
                     codes_f16(i ? high_halves(va, vb) : low_halves(va, vb), cf[j]);
                 }
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const u32x4 av = {cf[0][n], cf[1][n], cf[2][n], cf[3][n]};
-                    o[4 * i + n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                        __builtin_bit_cast(f16x8, av), __builtin_bit_cast(f16x8, pw), o[4 * i + n], 0, 0, 0);
-                }
+                for (int n = 0; n < 4; ++n) add(4 * i + n, u32x4{cf[0][n], cf[1][n], cf[2][n], cf[3][n]});
             }
         } else {
 #pragma unroll
@@ -323,10 +329,8 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
                     even[j] = low_halves(x.v[2 * j][i], x.v[2 * j + 1][i]);
                     odd[j] = high_halves(x.v[2 * j][i], x.v[2 * j + 1][i]);
                 }
-                o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, even), __builtin_bit_cast(f16x8, pw),
-                                                                  o[2 * i], 0, 0, 0);
-                o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, odd),
-                                                                      __builtin_bit_cast(f16x8, pw), o[2 * i + 1], 0, 0, 0);
+                add(2 * i, even);
+                add(2 * i + 1, odd);
             }
         }
         more_v();
