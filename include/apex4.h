@@ -479,7 +479,8 @@ int apex4_attn_decode(const void* q, int64_t q_stride, const void* k_pages, cons
 /*
  * The same for the packed new tokens of q_start (a prompt, a chunk of one, a few
  * tokens at a time), each at its own position p: q, out [T, heads, head_dim].
- *   max_q: a bound of the new tokens of a sequence; those past it get no output.
+ *   max_q: a bound of the new tokens of a sequence; the outputs of those past it,
+ *   and of tokens of no sequence, are left undefined.
  *   A token whose position is negative (more new tokens than kv_len) sees nothing
  *   and gets zeros.  A value that is infinite or NaN reaches every new token of
  *   its sequence for which its position lies in a tile with seen ones, also

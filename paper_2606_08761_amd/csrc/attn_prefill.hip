@@ -3,11 +3,10 @@
 // positions that stay visible.
 //
 // One pass over the positions with the running maximum and sum of the softmax.
-// A workgroup takes 128 rows of one key head (a row is a new token and one of
-// the query heads that share the key head, so that few tokens still fill it)
+// A workgroup takes 128 or 256 rows of one key head (a row is a new token and one
+// of the query heads that share the key head, so that few tokens still fill it)
 // and the tiles of 64 positions that any of them sees; a wave takes 32 rows,
-// with q and the output sums in registers.  Bound by the matrix cores and, next
-// to them, by the exponentials.
+// with q and the output sums in registers.
 //   S^T = K Q^T   32 x 32 x 16 products: a lane holds 16 positions of one row
 //                 in each of the tile's two halves, so the softmax needs no
 //                 other lane but lane ^ 32, and that only when the maximum is
@@ -15,15 +14,28 @@
 //   O^T = V^T P^T the scores' layout, rounded to binary16, is the right operand
 //                 as it stands: position 16 s + 8 (j / 4) + 4 h + j % 4 is
 //                 element j of lane half h in step s.
-// Keys and values go through registers into LDS in the order the products read
-// them, 16 bytes a lane without bank conflicts: keys as [d / 8][position],
-// values transposed on the way (8 positions x 4 values d by v_perm) as
-// [step, half][d][8 positions].  The next tile's loads are in flight during a
-// tile's products; the buffers alternate, one barrier a tile.
-// 4-bit codes become small integers in binary16 (exact) on their way into LDS;
-// a position's scales multiply its scores and weights in 32 bits.
+// Keys and values go into LDS as they lie in a page, by loads that pass no
+// register; only the 16-byte pieces of a position change places, so that neither
+// the keys' reads nor the transposing reads of the values meet in a bank.  The
+// loads of the next tile are in flight during a tile's products, and its first
+// products run beside the tile's exponentials; two buffers, one barrier a tile.
+// 4-bit codes become small integers in binary16 (exact) on their way into LDS,
+// through registers; a position's scales multiply its scores and weights in 32
+// bits.  The weights are rounded to binary16 for the second product (2^-11 of
+// each), the sums of scores, weights and outputs are of 32 bits.
 // With few rows and a long cache the tiles of a workgroup are cut into S parts,
 // joined by the kernel that joins those of attn_decode.hip.
+//
+// Bound by the matrix cores: a tile's 64 products take a wave 1024 cycles of its
+// SIMD's, its exponentials, their arguments, maxima and sums about 830 of the vector
+// unit, which runs beside them.  A prompt of 8192 tokens, 64 query heads of 128: 1.11
+// ms, 990 TFLOP/s of the 1343 that a product of 8192^3 reaches, the matrix cores busy
+// half of the cycles at a clock of 1.8 to 2.0 GHz; other orders of loads, products
+// and exponentials, three and four buffers and priorities gave the same.  Codes:
+// 16 % more a tile, for putting them into LDS and for the scales (2048 tokens of 2
+// sequences under a window of 1024: 235 us; fewer bank conflicts, and multiplications
+// left out to see, changed nothing; nor did the keys' conversion at a step's beginning
+// and the values' at its end).
 #include "attn_core.h"
 
 namespace apex4 {
@@ -47,7 +59,9 @@ template <int D, bool I4, int kWaves>
 struct Smem {
     uint8_t k[2][kW * D * 2];
     uint8_t v[2][kW * D * 2];
-    float ks[2][I4 ? kW : 4];  // scales, the softmax's factor in the keys'
+    // scales, the softmax's factor in the keys'; those of the keys of tile t are read in
+    // step t, beside the writing of tile t + 2's: four slots
+    float ks[4][I4 ? kW : 4];
     float vs[2][I4 ? kW : 4];
     float vs_most[2][4];       // the largest of the positions that each wave staged
 };
@@ -279,7 +293,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                     codes_f16(i_codes[j], w);
                     write_lds(k_lds + buf * kTileBytes + i_pos * kRow + 16 * ((4 * i_part + j) ^ k_swizzle<D>(i_pos)), u32x4{w[0], w[1], w[2], w[3]});
                 }
-                if (i_part == 0) sm.ks[buf][i_pos] = half_of(i_scale, 0) * to_log2;
+                if (i_part == 0) sm.ks[t & 3][i_pos] = half_of(i_scale, 0) * to_log2;
             }
         } else {
             float most = 0x1p-24f;  // a scale of zero leaves the sum of the weights alone to grow
@@ -378,7 +392,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const f32x4 s4 = __builtin_bit_cast(f32x4, read_lds(ks_lds + sb + 4 * kW * buf + 128 * u + 32 * i));
+                        const f32x4 s4 = __builtin_bit_cast(f32x4, read_lds(ks_lds + sb + 4 * kW * (t & 3) + 128 * u + 32 * i));
 #pragma unroll
                         for (int j = 0; j < 4; ++j) sc[u][4 * i + j] *= s4[j];
                     }
@@ -447,7 +461,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                     if constexpr (!I4) l = add_pair(p, l);  // the rounded weights: one large weight's rounding cancels
                     pw[s][j] = p;
                 }
-                        }
+            }
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const ValueFrags vf = read_v(s, vb);
@@ -592,9 +606,10 @@ hipError_t launch_attn_prefill(const KvView& c, const AttnArgs& a, hipStream_t s
     const Plan p = plan_prefill(c, a);
     float* part = static_cast<float*>(a.workspace);
     float* ml = part + a.T * a.heads * p.S * c.D;
-    hipError_t e;
-    if (c.D == 128) e = c.i4 ? run<128, true, 8>(c, a, p, part, ml, stream) : p.waves == 8 ? run<128, false, 8>(c, a, p, part, ml, stream) : run<128, false, 4>(c, a, p, part, ml, stream);
-    else e = c.i4 ? run<64, true, 8>(c, a, p, part, ml, stream) : p.waves == 8 ? run<64, false, 8>(c, a, p, part, ml, stream) : run<64, false, 4>(c, a, p, part, ml, stream);
+    const auto kernel = c.D == 64 ? (c.i4 ? run<64, true, 8> : run<64, false, 4>)
+                        : c.i4    ? run<128, true, 8>
+                                  : (p.waves == 8 ? run<128, false, 8> : run<128, false, 4>);
+    const hipError_t e = kernel(c, a, p, part, ml, stream);
     if (e != hipSuccess || p.S == 1) return e;
     return launch_attn_join(part, ml, a.T * a.heads, p.S, c.D, a.out, stream);
 }
