@@ -181,7 +181,6 @@ int apex4_attn_decode_workspace_size(int64_t B, int64_t width, int64_t max_len, 
     if ((rc = make_attn(a, c, nullptr, heads * head_dim, nullptr, B, 1, heads, window, sinks, 1.f, nullptr))) return rc;
     if ((rc = check_device())) return rc;
     return largest(c, a, B == 0, apex4::attn_decode_workspace, bytes);
-    return APEX4_OK;
 }
 
 int apex4_attn_decode(const void* q, int64_t q_stride, const void* k_pages, const void* v_pages, int64_t n_pages,
@@ -215,7 +214,6 @@ int apex4_attn_prefill_workspace_size(int64_t T, int64_t B, int64_t max_q, int64
     if ((rc = make_attn(a, c, nullptr, heads * head_dim, nullptr, T, max_q, heads, window, sinks, 1.f, nullptr))) return rc;
     if ((rc = check_device())) return rc;
     return largest(c, a, T == 0 || B == 0 || max_q == 0, apex4::attn_prefill_workspace, bytes);
-    return APEX4_OK;
 }
 
 int apex4_attn_prefill(const void* q, int64_t q_stride, const int32_t* q_start, int64_t T, int64_t max_q,

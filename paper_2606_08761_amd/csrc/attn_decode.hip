@@ -27,9 +27,21 @@
 // weights times scales, whatever the scales are, stay in binary16's range.
 //
 // Four waves (eight where the workgroups are few) share a range of positions and
-// add their sums through LDS; with
-// more than one range a sequence, a second kernel joins the ranges' sums in
-// order (the same bits every time).
+// add their sums through LDS; with more than one range a sequence, a second kernel
+// joins the ranges' sums in order (the same bits every time).
+//
+// Measured, 8 key heads of 128 and 64 query heads unless said otherwise; a kernel
+// that only reads reaches 5.1 TB/s over 0.5 GB and 5.7 over 2:
+//   one sequence of 131071, 537 MB           96 us, 5.6 TB/s, the join 4.8
+//   27 ragged sequences up to 8192, 502 MB  104 us, 4.8 TB/s, the join 4.8
+//   32 of them up to 16384, int4, 342 MB     75 us, 4.6 TB/s, the join 6.4
+//   16 under a window of 2048, 40 heads and key heads, 631 MB
+//                                           112 us, 5.6 TB/s, the join 4.6
+//   one sequence of 517 (one range)         9.4 us: 17 tiles of eight waves are
+//                                           three waits on memory and the merge
+// A launch of this size has about 10 us besides its bytes (first loads, last merge).
+// The codes' kernel issues 18 vector instructions a product, 45 % of what the SIMDs
+// issue in that time: there the bound is their latency between two tiles in flight.
 #include "attn_core.h"
 
 namespace apex4 {
@@ -372,7 +384,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
         }
     }
 
-    // the four waves' sums
+    // the waves' sums
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (g4 == 0) {

@@ -9,6 +9,11 @@
 // and ranks the pages it looks for by one scan (a cache of 288 GB has some ten
 // thousand pages); a chain of a few latencies.  The data then moves in one launch over
 // all planes, bound by HBM: 2 page_bytes a moved page and plane.
+//
+// Measured: the bookkeeping 8 to 10 us a call (32 forks of 63 pages, or 24 sequences
+// of up to 128, in pools of some thousand pages), freeing 3 to 5 us, and moving the
+// pages that such a batch leaves behind, 0.59 GB read and as much written in 8
+// planes of 32 KB pages, 227 us: 5.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
