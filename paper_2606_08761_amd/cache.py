@@ -88,20 +88,29 @@ def _starts(q_start, B):
     return _index(q_start, "q_start")
 
 
-def _output(out, shape, like):
+def _empty(like, shape, dtype, stream):
+    """Memory of the stream that the call runs on: what an earlier owner on another
+    stream still has under way does not reach it, nor this call its next owner."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with _torch().cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _output(out, shape, like, stream):
     if out is None:
-        return like.new_empty(shape, dtype=_torch().float16)
+        return _empty(like, shape, _torch().float16, stream)
     if tuple(out.shape) != tuple(shape):
         raise ValueError(f"the output must be {tuple(shape)}")
     return out
 
 
-def _workspace(workspace, need, like):
+def _workspace(workspace, need, like, stream):
     """(pointer, bytes): the caller's, or one made here where one is needed."""
     if workspace is None:
         if not need:
             return None, 0, None
-        workspace = like.new_empty((need,), dtype=_torch().uint8)
+        workspace = _empty(like, (need,), _torch().uint8, stream)
         return workspace.data_ptr(), need, workspace
     return _dev(workspace, _torch().uint8, "workspace"), workspace.numel(), workspace
 
@@ -134,8 +143,8 @@ def apex4_kv_gather(k_pages, v_pages, table, kv_len, T: int, kv_heads: int, head
     """The last q_start[b + 1] - q_start[b] tokens (None: one) of every sequence
     as float16: (k, v) [T, kv_heads, head_dim]."""
     torch = _torch()
-    k = _output(k, (T, kv_heads, head_dim), k_pages)
-    v = _output(v, (T, kv_heads, head_dim), k_pages)
+    k = _output(k, (T, kv_heads, head_dim), k_pages, stream)
+    v = _output(v, (T, kv_heads, head_dim), k_pages, stream)
     kpp, vpp, n = _planes(k_pages, v_pages, kv_heads, head_dim, page, cache)
     tp, width, lp, B = _tables(table, kv_len)
     rc = lib().apex4_kv_gather(kpp, vpp, n, tp, width, lp, B, kv_heads, head_dim, page, _kind(cache), _starts(q_start, B), T,
@@ -186,9 +195,9 @@ def apex4_attn_decode(q, k_pages, v_pages, table, kv_len, kv_heads: int, page: i
     if rows != B:
         raise ValueError("q must have one row a sequence")
     most = width * page if max_len is None else max_len
-    out = _output(out, (B, H, D), q)
+    out = _output(out, (B, H, D), q, stream)
     need = _decode_need(q.get_device(), B, width, most, H, kv_heads, D, page, window, sinks) if workspace is None else 0
-    wp, wn, held = _workspace(workspace, need, q)
+    wp, wn, held = _workspace(workspace, need, q, stream)
     rc = lib().apex4_attn_decode(qp, qs, kpp, vpp, n, tp, width, lp, B, most, H, kv_heads, D, page, _kind(cache), window,
                                  sinks, 1.0 / math.sqrt(D) if scale is None else scale, _ptr(out, torch.float16, "out"), wp,
                                  wn, _stream(q, stream))
@@ -210,10 +219,10 @@ def apex4_attn_prefill(q, q_start, k_pages, v_pages, table, kv_len, kv_heads: in
     sp = _starts(q_start, B)
     most = width * page if max_len is None else max_len
     most_q = T if max_q is None else max_q
-    out = _output(out, (T, H, D), q)
+    out = _output(out, (T, H, D), q, stream)
     need = (_prefill_need(q.get_device(), T, B, most_q, width, most, H, kv_heads, D, page, window, sinks)
             if workspace is None else 0)
-    wp, wn, held = _workspace(workspace, need, q)
+    wp, wn, held = _workspace(workspace, need, q, stream)
     rc = lib().apex4_attn_prefill(qp, qs, sp, T, most_q, kpp, vpp, n, tp, width, lp, B, most, H, kv_heads, D, page,
                                   _kind(cache), window, sinks, 1.0 / math.sqrt(D) if scale is None else scale,
                                   _ptr(out, torch.float16, "out"), wp, wn, _stream(q, stream))
@@ -243,12 +252,16 @@ def _pool(pool, refs):
     return _ptr(pool, torch.uint8, "pool"), pool.shape[0], pool.shape[2]
 
 
-def _status(status, like):
-    return like.new_empty((1,)) if status is None else status
+def _status(status, like, stream):
+    if status is None:
+        return _empty(like, (1,), _torch().int32, stream)
+    if status.numel() < 1:
+        raise ValueError("status must be [1]")
+    return status
 
 
-def _pages_work(workspace, n_pages, n, like):
-    return _workspace(workspace, 0 if workspace is not None else apex4_pages_workspace_size(n_pages, n), like)
+def _pages_work(workspace, n_pages, n, like, stream):
+    return _workspace(workspace, 0 if workspace is not None else apex4_pages_workspace_size(n_pages, n), like, stream)
 
 
 def _same_length(a, b, names):
@@ -263,8 +276,8 @@ def apex4_pages_reserve(table, kv_len, refs, seqs, new_len, page: int, status=No
     pages are too few, -1 where a length does not fit the table."""
     args = _state(table, kv_len, refs)
     n = _same_length(seqs, new_len, "seqs and new_len")
-    status = _status(status, table)
-    wp, wn, held = _pages_work(workspace, args[-1], n, table)
+    status = _status(status, table, stream)
+    wp, wn, held = _pages_work(workspace, args[-1], n, table, stream)
     rc = lib().apex4_pages_reserve(*args, _index(seqs, "seqs"), _index(new_len, "new_len"), n, page,
                                    _index(status, "status"), wp, wn, _stream(table, stream))
     _check("apex4_pages_reserve", rc)
@@ -278,8 +291,8 @@ def apex4_pages_fork(pool, table, kv_len, refs, parents, children, page: int, st
     args = _state(table, kv_len, refs)
     pp, planes, size = _pool(pool, refs)
     n = _same_length(parents, children, "parents and children")
-    status = _status(status, table)
-    wp, wn, held = _pages_work(workspace, args[-1], n, table)
+    status = _status(status, table, stream)
+    wp, wn, held = _pages_work(workspace, args[-1], n, table, stream)
     rc = lib().apex4_pages_fork(pp, planes, size, *args, _index(parents, "parents"), _index(children, "children"), n, page,
                                 _index(status, "status"), wp, wn, _stream(table, stream))
     _check("apex4_pages_fork", rc)
@@ -301,8 +314,8 @@ def apex4_pages_compact(pool, table, refs, status=None, workspace=None, stream=N
     if table.dim() != 2 or refs.dim() != 1:
         raise ValueError("table must be [slots, width] and refs [pages]")
     pp, planes, size = _pool(pool, refs)
-    status = _status(status, table)
-    wp, wn, held = _pages_work(workspace, refs.shape[0], 0, table)
+    status = _status(status, table, stream)
+    wp, wn, held = _pages_work(workspace, refs.shape[0], 0, table, stream)
     rc = lib().apex4_pages_compact(pp, planes, size, _index(table, "table"), table.shape[0], table.shape[1],
                                    _index(refs, "refs"), refs.shape[0], _index(status, "status"), wp, wn,
                                    _stream(table, stream))

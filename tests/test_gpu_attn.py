@@ -283,3 +283,25 @@ def test_side_stream_and_graph(pk):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, pk.apex4_attn_decode(q, kp, vp, table, lens, 2, 16))
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+def test_memory_made_for_another_stream(pk, cache):
+    """Output and workspace of a call on a stream that is not the current one: what
+    the current stream still does to freed memory does not reach them."""
+    import torch
+    c = paged.Case(67, [3000, 2100], [1, 1], 8, 2, 128, 16, cache)
+    q, kp, vp, table = dev(c.q), dev(c.k.raw), dev(c.v.raw), dev(c.table)
+    lens = dev(np.array(c.lens, np.int32))
+    need = pk.apex4_attn_decode_workspace_size(2, table.shape[1], c.width * 16, 8, 2, 128, 16)
+    assert need > 0
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    freed = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (q.numel() * 2, need)]
+    torch.cuda._sleep(20_000_000)
+    for x in freed:
+        x.fill_(255)  # NaN as binary16 and as float
+    del freed, x
+    y = pk.apex4_attn_decode(q, kp, vp, table, lens, 2, 16, cache=cache, stream=s)
+    torch.cuda.synchronize()
+    check(y, c)

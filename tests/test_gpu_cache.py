@@ -291,3 +291,12 @@ def test_a_sequences_life(pk):
         look()
         c.free([1, 2, 3, 4])
         assert int(c.refs.abs().sum()) == 0 and int(c.kv_len.sum()) == 0
+
+
+def test_an_empty_status_is_refused(pk):
+    import torch
+    c = pk.PagedKVCache(layers=1, pages=4, slots=2, kv_heads=1, head_dim=64)
+    none = torch.empty((0,), dtype=torch.int32, device="cuda")
+    for call in (lambda: c.reserve([0], [5], status=none), lambda: c.fork([0], [1], status=none), lambda: c.compact(status=none)):
+        with pytest.raises(ValueError):
+            call()
