@@ -28,10 +28,11 @@
 //
 // Bound by the matrix cores: a tile's 64 products take a wave 1024 cycles of its
 // SIMD's, its exponentials, their arguments, maxima and sums about 830 of the vector
-// unit, which runs beside them.  A prompt of 8192 tokens, 64 query heads of 128: 1.11
-// ms, 990 TFLOP/s of the 1343 that a product of 8192^3 reaches, the matrix cores busy
-// half of the cycles at a clock of 1.8 to 2.0 GHz; other orders of loads, products
-// and exponentials, three and four buffers and priorities gave the same.  Codes:
+// unit, which runs beside them.  A prompt of 8192 tokens, 64 query heads of 128: 1.08
+// ms, 1020 TFLOP/s of the 1343 that a product of 8192^3 reaches, at a clock that falls
+// with the load (all zeros, which cost less power: 0.85 ms).  No faster: three and
+// four buffers, two halves of the waves half a step apart, 64 rows a wave, fragments
+// read further ahead, wave priorities.  Codes:
 // 16 % more a tile, for putting them into LDS and for the scales (2048 tokens of 2
 // sequences under a window of 1024: 235 us; fewer bank conflicts, and multiplications
 // left out to see, changed nothing; nor did the keys' conversion at a step's beginning
@@ -43,7 +44,7 @@ namespace {
 
 using namespace attn;
 
-constexpr int kW = 64;            // positions of a tile
+constexpr int kShift = 6, kW = 1 << kShift;  // positions of a tile
 
 // Keys and values of a tile lie in LDS as they lie in a binary16 page, a row of D
 // values a position, but with the 16-byte pieces of a row exchanged (piece c at
@@ -193,10 +194,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     // positions that no row of the workgroup sees hold anything: their values,
     // times a weight of zero, must not count
     auto seen_by_some = [&](int t) { return t <= p_hi && (t >= tiles.lo || t < tiles.sinks); };
-    auto at_edge = [&](int t) {
-        const int at = tiles.start(t);
-        return at + kW > p_hi + 1 || (at < tiles.lo && at + kW > tiles.sinks);
-    };
+    // Which tiles have such positions (the last, and those at the end of the sinks and
+    // the window's start), and which are seen whole by every row: by numbers worked
+    // out once, for a step has no scalar instructions to spare.
+    const int edge = tiles.n_sink + ((p_hi + 1) >> kShift) - tiles.first;
+    auto at_edge = [&](int t) { return t >= edge || static_cast<uint32_t>(t - tiles.n_sink + 1) < 2u; };
+    const int whole_to = tiles.n_sink + ((p_lo + 1) >> kShift) - tiles.first;
+    const int whole_from = a.window ? tiles.n_sink + ((p_hi - a.window) >> kShift) + 1 - tiles.first : 0;
+    const int whole_sinks = a.window ? tiles.sinks >> kShift : 0;
+    auto whole = [&](int t) { return t < whole_to && (t >= whole_from || t < whole_sinks); };
     // Staging.  begin_k/v(t) sends the loads of tile t out, end_k/v(t, buf) has it
     // in LDS before the next barrier.
     // binary16: every 1 KB that a wave copies is kPos positions of 16 (one page)
@@ -371,20 +377,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
 
     // One tile, whose scores are in sc; the next one's products run into next
     // beside the exponentials.
+    // Sending the loads out takes some hundred scalar instructions: in the midst of the
+    // products they hide (a prompt of 8192 with 64 heads of 128: 1095 us after the third
+    // quarter, 1117 at the step's beginning).  Heads of 64, three workgroups a compute
+    // unit and shorter steps, want the loads early (ragged chunks: 96 us, 100 later), and
+    // so do codes, which the step itself waits for.
+    constexpr int kStage = I4 || D == 64 ? 0 : 3;
     Places next_v;  // tile t + 1's values
     Ids ids;        // of tile t + 2 (int4: of t + 1 where the thread stages values)
     auto step = [&](int t, f32x16 (&sc)[2], f32x16 (&next)[2], int buf) {
         const int at = tiles.start(t);
         const int staged = I4 && i_values ? t + 1 : t + 2;
-        const Places next_k = places(staged, ids);
-        if constexpr (I4) {
-            if (staged < t1) begin_codes(next_k);
-        } else {
-            if (t + 2 < t1) begin_copies(buf, next_k, c.k, k_lds, k_off);
-            if (t + 1 < t1) begin_copies(buf ^ 1, next_v, c.v, v_lds, v_off);
-            next_v = next_k;
-        }
-        ids = look_up(staged + 1);
+        auto stage = [&] {
+            const Places next_k = places(staged, ids);
+            if constexpr (I4) {
+                if (staged < t1) begin_codes(next_k);
+            } else {
+                if (t + 2 < t1) begin_copies(buf, next_k, c.k, k_lds, k_off);
+                if (t + 1 < t1) begin_copies(buf ^ 1, next_v, c.v, v_lds, v_off);
+                next_v = next_k;
+            }
+            ids = look_up(staged + 1);
+        };
+        if (kStage == 0 || idle) stage();
         if (!idle) {
             const uint32_t sb = 16 * (anew(tid) >> 5 & 1);
             if constexpr (I4) {
@@ -398,8 +413,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                     }
             }
             const float f_log2 = I4 ? 1.f : to_log2;
-            const bool full = at + kW - 1 <= p_lo && (a.window == 0 || at > p_hi - a.window || at + kW <= tiles.sinks);
-            if (!full) {
+            if (!whole(t)) {
                 // visible: t <= pos, and t > pos - window or t < sinks; as bounds of t less
                 // the lane's first position
                 const int p0 = at + 4 * (anew(tid) >> 5 & 1), last = pos - p0;
@@ -440,6 +454,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 add_scores(next, s, read_k(s, kb));
+                if (s + 1 == kStage) stage();
                 float e[8];
                 f32x4 sv[2];
                 if constexpr (I4) {
