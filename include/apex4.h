@@ -422,8 +422,8 @@ int apex4_w4a4_gemm_mx_ws(const uint8_t* A_6, const uint8_t* e_a,
  * width * page (or past max_len) and sequence numbers outside the table are never
  * used as addresses.  append leaves out tokens that have no page, gather returns
  * zeros for them, and attention to such positions is unspecified.
- * Limits: n_pages, max_len up to 2^30, width up to 2^20, B and T up to 2^24,
- * T heads up to 2^27.
+ * Limits: n_pages, max_len and the bytes of a page up to 2^30, width up to 2^20, B
+ * and T up to 2^24, T heads up to 2^27.
  */
 #define APEX4_KV_FP16 0
 #define APEX4_KV_INT4 1

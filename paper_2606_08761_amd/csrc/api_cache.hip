@@ -15,6 +15,7 @@ using apex4::KvView;
 using apex4::PageTable;
 
 constexpr int64_t kMaxPages = 1ll << 30, kMaxWidth = 1ll << 20, kMaxLen = 1ll << 30, kMaxCount = 1ll << 24;
+constexpr int64_t kMaxPageBytes = 1ll << 30;  // offsets inside a page are 32 bits
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 bool present(const void* p, int64_t n) { return p != nullptr || n == 0; }
@@ -29,7 +30,7 @@ int shift_of(int64_t page) {
 int check_geometry(int cache, int64_t kv_heads, int64_t D, int64_t page) {
     if (cache != APEX4_KV_FP16 && cache != APEX4_KV_INT4) return APEX4_ERR_SHAPE;
     if (kv_heads < 1 || kv_heads > 65536 || (D != 64 && D != 128) || shift_of(page) < 0) return APEX4_ERR_SHAPE;
-    return APEX4_OK;
+    return apex4::kv_page_bytes(cache == APEX4_KV_INT4, kv_heads, D, page) <= kMaxPageBytes ? APEX4_OK : APEX4_ERR_SHAPE;
 }
 
 // The cache's arguments; pointers and alignment are checked by the callers in
@@ -120,7 +121,7 @@ int make_table(PageTable& p, int32_t* table, int64_t slots, int64_t width, int32
 }
 
 int check_pool(const void* pool, int64_t planes, int64_t page_bytes) {
-    if (planes < 1 || planes > 65536 || page_bytes < 16 || page_bytes % 16 != 0 || page_bytes > (1ll << 30)) return APEX4_ERR_SHAPE;
+    if (planes < 1 || planes > 65536 || page_bytes < 16 || page_bytes % 16 != 0 || page_bytes > kMaxPageBytes) return APEX4_ERR_SHAPE;
     return aligned(pool, 16) ? APEX4_OK : APEX4_ERR_ALIGN;
 }
 

@@ -195,14 +195,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     // times a weight of zero, must not count
     auto seen_by_some = [&](int t) { return t <= p_hi && (t >= tiles.lo || t < tiles.sinks); };
     // Which tiles have such positions (the last, and those at the end of the sinks and
-    // the window's start), and which are seen whole by every row: by numbers worked
-    // out once, for a step has no scalar instructions to spare.
+    // the window's start), and which hold positions that some row does not see: by
+    // numbers worked out once, for a step has no scalar instructions to spare.
     const int edge = tiles.n_sink + ((p_hi + 1) >> kShift) - tiles.first;
     auto at_edge = [&](int t) { return t >= edge || static_cast<uint32_t>(t - tiles.n_sink + 1) < 2u; };
     const int whole_to = tiles.n_sink + ((p_lo + 1) >> kShift) - tiles.first;
     const int whole_from = a.window ? tiles.n_sink + ((p_hi - a.window) >> kShift) + 1 - tiles.first : 0;
     const int whole_sinks = a.window ? tiles.sinks >> kShift : 0;
-    auto whole = [&](int t) { return t < whole_to && (t >= whole_from || t < whole_sinks); };
+    auto late = [&](int t) { return t >= whole_to; };  // some of its positions are past some row
+    auto early = [&](int t) { return t < whole_from && t >= whole_sinks; };  // or before its window
     // Staging.  begin_k/v(t) sends the loads of tile t out, end_k/v(t, buf) has it
     // in LDS before the next barrier.
     // binary16: every 1 KB that a wave copies is kPos positions of 16 (one page)
@@ -235,8 +236,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
         int64_t at[kIds];
         int64_t scale;
     };
-    const __attribute__((address_space(4))) int32_t* table =
-        (const __attribute__((address_space(4))) int32_t*)(c.table + static_cast<int64_t>(b) * c.width);
+    typedef const __attribute__((address_space(4))) int32_t table_i32;
+    const __attribute__((address_space(4))) uint8_t* table =
+        (const __attribute__((address_space(4))) uint8_t*)(c.table + static_cast<int64_t>(b) * c.width);
+    const uint32_t page_bytes = static_cast<uint32_t>(c.page_bytes);  // at most 2^30
     auto first = [&](int i) { return I4 ? i_pos & (kW - 1) : first_of(i); };
     auto look_up = [&](int t) {
         const int at = tiles.start(t);
@@ -244,8 +247,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
 #pragma unroll
         for (int i = 0; i < kIds; ++i) {
             if (i && one_page) break;
-            const int p = (at + first(i)) >> c.page_shift;
-            r.page[i] = table[p < c.width ? p : c.width - 1];
+            const uint32_t p = static_cast<uint32_t>(at + first(i)) >> c.page_shift, most = c.width - 1;
+            r.page[i] = *reinterpret_cast<table_i32*>(table + 4 * (p < most ? p : most));  // below 2^22 bytes
         }
         return r;
     };
@@ -259,10 +262,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                 r.at[i] = r.at[0] + kPos * kWaves * kRow * i;
                 continue;
             }
-            const int p = static_cast<uint32_t>(ids.page[i]) < static_cast<uint32_t>(c.n_pages) ? ids.page[i] : 0;
-            const int x = static_cast<int>(head_at) + ((at + first(i)) & page_mask);  // below 2^26
-            r.at[i] = p * c.page_bytes + static_cast<int64_t>(x) * (I4 ? D / 2 : kRow);
-            if constexpr (I4) r.scale = p * c.page_bytes + scale_at + 2 * x;
+            const uint32_t p = static_cast<uint32_t>(ids.page[i]) < static_cast<uint32_t>(c.n_pages) ? ids.page[i] : 0;
+            const uint32_t x = static_cast<uint32_t>(head_at) + ((at + first(i)) & page_mask);
+            const uint64_t page = static_cast<uint64_t>(p) * page_bytes;
+            r.at[i] = page + x * (I4 ? D / 2 : kRow);
+            if constexpr (I4) r.scale = page + static_cast<uint32_t>(scale_at) + 2 * x;
         }
         return r;
     };
@@ -413,17 +417,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                     }
             }
             const float f_log2 = I4 ? 1.f : to_log2;
-            if (!whole(t)) {
-                // visible: t <= pos, and t > pos - window or t < sinks; as bounds of t less
-                // the lane's first position
-                const int p0 = at + 4 * (anew(tid) >> 5 & 1), last = pos - p0;
-                const int from = a.window ? last - a.window + 1 : -p0, first = a.sinks - p0;
+            // visible: t <= pos, and t > pos - window or t < sinks; as bounds of t less
+            // the lane's first position
+            if (late(t)) {
+                const int last = pos - at - 4 * (anew(tid) >> 5 & 1);
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         const int p = 32 * u + 8 * (j >> 2) + (j & 3);
-                        const bool seen = (p <= last) & ((p >= from) | (p < first));
+                        sc[u][j] = p <= last ? sc[u][j] : -INFINITY;
+                    }
+            }
+            if (early(t)) {
+                const int p0 = at + 4 * (anew(tid) >> 5 & 1), from = pos - a.window + 1 - p0, first = a.sinks - p0;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int p = 32 * u + 8 * (j >> 2) + (j & 3);
+                        const bool seen = (p >= from) | (p < first);
                         sc[u][j] = seen ? sc[u][j] : -INFINITY;
                     }
             }

@@ -155,3 +155,12 @@ def test_binding_refuses(L):
         pk.apex4_attn_decode(q, *planes, i, i[:, 0], 2, 16)
     with pytest.raises(TypeError):
         pk.apex4_kv_append(q, q, *planes, i, i[:, 0], 16)
+
+
+def test_pages_past_the_offsets_are_refused(L):
+    """A page's bytes fit the 32-bit offsets inside it: 2^30 at most."""
+    b = ctypes.c_int64(0)
+    assert L.apex4_kv_page_bytes(0, 4096, 128, 1024, ctypes.byref(b)) == 0 and b.value == 1 << 30
+    assert L.apex4_kv_page_bytes(0, 4097, 128, 1024, ctypes.byref(b)) == -2
+    assert L.apex4_kv_page_bytes(1, 16384, 128, 1024, ctypes.byref(b)) == -2
+    assert L.apex4_kv_append(*args(APPEND_ORDER, APPEND, kv_heads=8192, page=1024, k_stride=1 << 20, v_stride=1 << 20)) == -2
