@@ -461,7 +461,9 @@ int apex4_kv_gather(const void* k_pages, const void* v_pages, int64_t n_pages, c
  * tokens that stay visible).  A sequence without tokens gets zeros.  Positions
  * that are not seen may hold anything, NaN included.  Scores, weights' sums and
  * output sums are binary32; the weights are rounded to binary16 (the products'
- * operand), the result once.  scale: positive and finite.
+ * operand), the result once.  scale: positive and finite.  Scores scale q.k are taken
+ * up to a magnitude of 2^26 (a weight's exponent is one binary32 fma, whose error
+ * grows with the score's magnitude, and must stay within the weights' range).
  *   max_len: a bound of kv_len known on the host (shorter: less to launch);
  *   tokens past it are not seen.
  *   workspace: apex4_attn_decode_workspace_size bytes (NULL where that is 0);

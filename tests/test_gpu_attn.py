@@ -305,3 +305,19 @@ def test_memory_made_for_another_stream(pk, cache):
     y = pk.apex4_attn_decode(q, kp, vp, table, lens, 2, 16, cache=cache, stream=s)
     torch.cuda.synchronize()
     check(y, c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_of_large_magnitude(pk, cache, D):
+    """Scores of either sign of up to some 10^7, far past what an exponential holds."""
+    c = paged.Case(71, [1, 2, 40, 130, 700], [1] * 5, 8, 2, D, 16, cache, sd=3000.0)
+    c.q = (c.q * np.float16(2600.0)).astype(np.float16)
+    s = np.concatenate([(np.abs(np.einsum("hd,thd->ht", c.q[b].astype(np.float64), np.repeat(k, 4, axis=1))) * c.scale).ravel()
+                        for b, k in enumerate(c.K)])
+    assert 1e7 < s.max() < 2.0 ** 26
+    check(decode(pk, c), c)
+    check(prefill(pk, c), c)
+    n = paged.Case(73, [130, 700], [70, 33], 8, 2, D, 16, cache, sd=3000.0)
+    n.q = (n.q * np.float16(2600.0)).astype(np.float16)
+    check(prefill(pk, n), n)
