@@ -26,17 +26,17 @@
 // With few rows and a long cache the tiles of a workgroup are cut into S parts,
 // joined by the kernel that joins those of attn_decode.hip.
 //
-// Bound by the matrix cores: a tile's 64 products take a wave 1024 cycles of its
-// SIMD's, its exponentials, their arguments, maxima and sums about 830 of the vector
-// unit, which runs beside them.  A prompt of 8192 tokens, 64 query heads of 128: 1.08
-// ms, 1020 TFLOP/s of the 1343 that a product of 8192^3 reaches, at a clock that falls
-// with the load (all zeros, which cost less power: 0.85 ms).  No faster: three and
-// four buffers, two halves of the waves half a step apart, 64 rows a wave, fragments
-// read further ahead, wave priorities.  Codes:
-// 16 % more a tile, for putting them into LDS and for the scales (2048 tokens of 2
-// sequences under a window of 1024: 235 us; fewer bank conflicts, and multiplications
-// left out to see, changed nothing; nor did the keys' conversion at a step's beginning
-// and the values' at its end).
+// Bound by the matrix cores and, next to them, the vector units: a tile's 32 products
+// take a wave 1024 cycles of its SIMD's matrix core, its exponentials (16 cycles each),
+// their arguments, maxima and sums about 830 of the vector unit.  A prompt of 8192
+// tokens, 64 query heads of 128: 1.06 to 1.10 ms, 1000 to 1040 TFLOP/s of the 1343 that
+// a product of 8192^3 reaches, at a clock that falls with the load (queries of zero,
+// which cost less power: 0.85 ms).  No faster: three and four buffers, two halves of the
+// waves half a step apart, 64 rows a wave, fragments read further ahead, wave
+// priorities.  Codes: a fifth more a tile, for putting them into LDS and for the scales
+// (2048 tokens of 2 sequences under a window of 1024: 230 us); fewer bank conflicts,
+// multiplications left out to see, and the conversion elsewhere in the step changed
+// nothing.
 #include "attn_core.h"
 
 namespace apex4 {
