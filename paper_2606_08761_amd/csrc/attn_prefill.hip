@@ -34,7 +34,7 @@
 // which cost less power: 0.85 ms).  No faster: three and four buffers, two halves of the
 // waves half a step apart, 64 rows a wave, fragments read further ahead, wave
 // priorities.  Codes: a fifth more a tile, for putting them into LDS and for the scales
-// (2048 tokens of 2 sequences under a window of 1024: 230 us); fewer bank conflicts,
+// (2048 tokens of 2 sequences under a window of 1024: 226 us); fewer bank conflicts,
 // multiplications left out to see, and the conversion elsewhere in the step changed
 // nothing.
 #include "attn_core.h"
@@ -510,8 +510,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     f32x16 s0[2], s1[2];
     if (t0 < t1) {
         ids = look_up(t0);
-        next_v = places(t0, ids);
         if constexpr (I4) {
+            next_v = places(t0, ids);
             begin_codes(next_v);
             end_codes(t0, 0);
             if (!i_values && t0 + 1 < t1) {
@@ -520,12 +520,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
             }
             ids = look_up(i_values ? t0 + 1 : t0 + 2);
         } else {
-            ids = look_up(t0 + 1);
+            const Ids ids1 = look_up(t0 + 1), ids2 = look_up(t0 + 2);
+            next_v = places(t0, ids);
             begin_copies(0, next_v, c.k, k_lds, k_off);
             begin_copies(0, next_v, c.v, v_lds, v_off);
-            next_v = places(t0 + 1, ids);
+            next_v = places(t0 + 1, ids1);
             if (t0 + 1 < t1) begin_copies(1, next_v, c.k, k_lds, k_off);
-            ids = look_up(t0 + 2);
+            ids = ids2;
             landed();
             clear_unseen(t0, 0);
         }
@@ -540,28 +541,47 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     }
 
     l += __shfl_xor(l, 32, 64);
-    const Row x = row_of(anew(r32));
-    if (!x.valid) return;
-    const int64_t row = (static_cast<int64_t>(q0) + x.tok) * a.heads + x.head;
+    if (idle) return;
+    const int ln = anew(tid) & 63, r = ln & 31, h8 = ln >> 5;
+    const Row x = row_of(r);
+    const int row = (q0 + x.tok) * a.heads + x.head;  // below 2^27 where it is valid
     // the lane's rows of the sums are d = 32 i + 8 k + 4 half + y
-    const float f = S > 1 ? 1.f : l != 0.f ? 1.f / l : 0.f;
+    if (S == 1) {
+        // through LDS (the tiles are used, a wave has 32 rows of it), so that a row goes out
+        // in one piece.  (8 bytes a lane to 32 rows at a time: 241 us of the windowed case above,
+        // 226 so.)
+        const float f = l != 0.f ? 1.f / l : 0.f;
+        auto piece_of = [&](int r, int c) { return wave * 32 * kRow + r * kRow + 16 * (c ^ (D == 128 ? r & 15 : r >> 1 & 7)); };
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float v[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) v[y] = o[i][4 * k + y] * f;
+                *reinterpret_cast<u32x2*>(smem_raw + piece_of(r, 4 * i + k) + 8 * h8) =
+                    u32x2{pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+            }
+        const int mine = x.valid ? row : -1;
+#pragma unroll
+        for (int i = 0; i < kPieces / 2; ++i) {
+            const int to_r = 64 / kPieces * i + ln / kPieces, c = ln % kPieces, to = __shfl(mine, to_r, 64);
+            const u32x4 v = *reinterpret_cast<const u32x4*>(smem_raw + piece_of(to_r, c));
+            if (to >= 0) *reinterpret_cast<u32x4*>(a.out + static_cast<int64_t>(to) * D + 8 * c) = v;
+        }
+        return;
+    }
+    if (!x.valid) return;
+    const int64_t at = static_cast<int64_t>(row) * S + split;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float v[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) v[y] = o[i][4 * k + y] * f;
-            const int d = 32 * i + 8 * k + 4 * half;
-            if (S == 1) {
-                *reinterpret_cast<u32x2*>(a.out + row * D + d) = u32x2{pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
-            } else {
-                *reinterpret_cast<f32x4*>(part + (row * S + split) * D + d) = f32x4{v[0], v[1], v[2], v[3]};
-            }
-        }
-    if (S > 1 && half == 0) {
-        ml[(row * S + split) * 2] = m;
-        ml[(row * S + split) * 2 + 1] = l;
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<f32x4*>(part + at * D + 32 * i + 8 * k + 4 * h8) =
+                f32x4{o[i][4 * k], o[i][4 * k + 1], o[i][4 * k + 2], o[i][4 * k + 3]};
+    if (h8 == 0) {
+        ml[at * 2] = m;
+        ml[at * 2 + 1] = l;
     }
 }
 
