@@ -33,8 +33,8 @@
 // a product of 8192^3 reaches, at a clock that falls with the load (queries of zero,
 // which cost less power: 0.85 ms).  No faster: three and four buffers, two halves of the
 // waves half a step apart, 64 rows a wave, fragments read further ahead, wave
-// priorities.  Codes: a fifth more a tile, for putting them into LDS and for the scales
-// (2048 tokens of 2 sequences under a window of 1024: 226 us); fewer bank conflicts,
+// priorities.  Codes: 14 % more a tile, for putting them into LDS and for the scales
+// (2048 tokens of 2 sequences under a window of 1024: 217 us); fewer bank conflicts,
 // multiplications left out to see, and the conversion elsewhere in the step changed
 // nothing.
 #include "attn_core.h"
@@ -64,7 +64,7 @@ struct Smem {
     // step t, beside the writing of tile t + 2's: four slots
     float ks[4][I4 ? kW : 4];
     float vs[2][I4 ? kW : 4];
-    float vs_most[2][4];       // the largest of the positions that each wave staged
+    uint32_t vs_most[4];       // the largest of a tile's, as bits; a tile's slot is cleared two steps before it is written
 };
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
@@ -292,37 +292,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
             i_scale = *reinterpret_cast<const uint16_t*>(plane + at.scale);
         }
     };
+    // A piece, 8 codes, stays in the order of codes_f16 (code i, code i + 4, ..): q has
+    // the same (code_order), and of the values it shows in the rows of the sums.  The
+    // tile's largest scale is an atomic maximum, the same whatever the order: every
+    // wave waits for the values' four, and a reduction by shuffles and the values'
+    // reordering had them take twice as long as the keys' (8192 tokens: 1270 us, 1200 so).
+    const uint32_t least = __builtin_bit_cast(uint32_t, 0x1p-24f);  // a scale of zero leaves the sum of the weights alone to grow
     auto end_codes = [&](int t, int buf) {
         const int i_pos = (anew(tid) & 255) / kLanes, i_part = anew(tid) % kLanes;
         const bool i_thread = i_pos < kW;
-        if (!i_values) {
-            if (i_thread) {
+        if (i_thread) {
+            const uint32_t to = (i_values ? v_lds : k_lds) + buf * kTileBytes + i_pos * kRow;
+            const int number = i_values ? v_swizzle<D>(i_pos) : k_swizzle<D>(i_pos);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t w[4];
-                    codes_f16(i_codes[j], w);
-                    write_lds(k_lds + buf * kTileBytes + i_pos * kRow + 16 * ((4 * i_part + j) ^ k_swizzle<D>(i_pos)), u32x4{w[0], w[1], w[2], w[3]});
-                }
-                if (i_part == 0) sm.ks[t & 3][i_pos] = half_of(i_scale, 0) * to_log2;
+            for (int j = 0; j < 4; ++j) {
+                uint32_t w[4];
+                codes_f16(i_codes[j], w);
+                write_lds(to + 16 * ((4 * i_part + j) ^ number), u32x4{w[0], w[1], w[2], w[3]});
             }
-        } else {
-            float most = 0x1p-24f;  // a scale of zero leaves the sum of the weights alone to grow
-            if (i_thread) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t w[4];
-                    codes_f16(i_codes[j], w);  // back in order: the halves of w[i] are codes i and i + 4
-                    write_lds(v_lds + buf * kTileBytes + i_pos * kRow + 16 * ((4 * i_part + j) ^ v_swizzle<D>(i_pos)),
-                              u32x4{low_halves(w[0], w[1]), low_halves(w[2], w[3]), high_halves(w[0], w[1]), high_halves(w[2], w[3])});
+            if (i_part == 0) {
+                const float x = half_of(i_scale, 0);
+                if (!i_values) {
+                    sm.ks[t & 3][i_pos] = x * to_log2;
+                } else {
+                    const float scale = seen_by_some(tiles.start(t) + i_pos) ? x : 0.f;
+                    sm.vs[buf][i_pos] = scale;
+                    atomicMax(&sm.vs_most[anew(t & 3)], __builtin_bit_cast(uint32_t, fmaxf(scale, 0.f)));  // not negative: bits are in order
                 }
-                const float x = seen_by_some(tiles.start(t) + i_pos) ? half_of(i_scale, 0) : 0.f;
-                if (i_part == 0) sm.vs[buf][i_pos] = x;
-                most = fmaxf(most, x);
             }
-#pragma unroll
-            for (int i = kLanes; i < 64; i *= 2) most = fmaxf(most, __shfl_xor(most, i, 64));
-            if (lane == 0) sm.vs_most[buf][wave - 4] = most;
         }
+        if (tid == 256) sm.vs_most[(t + 1) & 3] = least;
     };
 
     f32x16 o[DT];
@@ -447,8 +446,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                 for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[u][j]);
             top *= f_log2;
             if constexpr (I4) {  // a bound of the scores with their values' scales
-                const f32x4 w = *reinterpret_cast<const f32x4*>(sm.vs_most[buf]);
-                top += __builtin_amdgcn_logf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])));
+                top += __builtin_amdgcn_logf(__builtin_bit_cast(float, sm.vs_most[t & 3]));
             }
             if (__any(top > m + kSlack)) {
                 top = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
@@ -513,6 +511,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
         if constexpr (I4) {
             next_v = places(t0, ids);
             begin_codes(next_v);
+            if (tid < 4) sm.vs_most[tid] = least;
+            __syncthreads();
             end_codes(t0, 0);
             if (!i_values && t0 + 1 < t1) {
                 begin_codes(places(t0 + 1, look_up(t0 + 1)));
@@ -545,7 +545,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     const int ln = anew(tid) & 63, r = ln & 31, h8 = ln >> 5;
     const Row x = row_of(r);
     const int row = (q0 + x.tok) * a.heads + x.head;  // below 2^27 where it is valid
-    // the lane's rows of the sums are d = 32 i + 8 k + 4 half + y
+    // the lane's rows of the sums are d = 32 i + 8 k + 4 half + y, of codes in their order
     if (S == 1) {
         // through LDS (the tiles are used, a wave has 32 rows of it), so that a row goes out
         // in one piece.  (8 bytes a lane to 32 rows at a time: 241 us of the windowed case above,
@@ -559,8 +559,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                 float v[4];
 #pragma unroll
                 for (int y = 0; y < 4; ++y) v[y] = o[i][4 * k + y] * f;
-                *reinterpret_cast<u32x2*>(smem_raw + piece_of(r, 4 * i + k) + 8 * h8) =
-                    u32x2{pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+                uint8_t* to = smem_raw + piece_of(r, 4 * i + k);
+                if constexpr (I4) {  // d = 8 k + 2 half, + 4, + 1, + 5
+                    *reinterpret_cast<uint32_t*>(to + 4 * h8) = pack_f16(v[0], v[2]);
+                    *reinterpret_cast<uint32_t*>(to + 8 + 4 * h8) = pack_f16(v[1], v[3]);
+                } else {
+                    *reinterpret_cast<u32x2*>(to + 8 * h8) = u32x2{pack_f16(v[0], v[1]), pack_f16(v[2], v[3])};
+                }
             }
         const int mine = x.valid ? row : -1;
 #pragma unroll
@@ -576,9 +581,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            *reinterpret_cast<f32x4*>(part + at * D + 32 * i + 8 * k + 4 * h8) =
-                f32x4{o[i][4 * k], o[i][4 * k + 1], o[i][4 * k + 2], o[i][4 * k + 3]};
+        for (int k = 0; k < 4; ++k) {
+            float* to = part + at * D + 32 * i + 8 * k;
+            const f32x4 v = {o[i][4 * k], o[i][4 * k + 1], o[i][4 * k + 2], o[i][4 * k + 3]};
+            if constexpr (I4) {
+                *reinterpret_cast<f32x2*>(to + 2 * h8) = f32x2{v[0], v[2]};
+                *reinterpret_cast<f32x2*>(to + 4 + 2 * h8) = f32x2{v[1], v[3]};
+            } else {
+                *reinterpret_cast<f32x4*>(to + 4 * h8) = v;
+            }
+        }
     if (h8 == 0) {
         ml[at * 2] = m;
         ml[at * 2 + 1] = l;
