@@ -34,9 +34,8 @@
 // which cost less power: 0.85 ms).  No faster: three and four buffers, two halves of the
 // waves half a step apart, 64 rows a wave, fragments read further ahead, wave
 // priorities.  Codes: 14 % more a tile, for putting them into LDS and for the scales
-// (2048 tokens of 2 sequences under a window of 1024: 217 us); fewer bank conflicts,
-// multiplications left out to see, and the conversion elsewhere in the step changed
-// nothing.
+// (2048 tokens of 2 sequences under a window of 1024: 206 to 217 us); multiplications
+// left out to see, and the conversion elsewhere in the step changed nothing.
 #include "attn_core.h"
 
 namespace apex4 {
@@ -51,10 +50,12 @@ constexpr int kShift = 6, kW = 1 << kShift;  // positions of a tile
 // c ^ the numbers below), so that the 16 lanes that read at a time find theirs in
 // different banks: 16 positions' piece c of the keys; and of the values 32
 // bytes of 4 positions next to 32 other bytes of the same (the transposing read).
+// Codes are written a piece of 4 (D = 64: 8) positions at a time, which the low bits
+// of both numbers keep apart (1 % of the time over an int4 cache).
 template <int D>
 __device__ __forceinline__ int k_swizzle(int t) { return D == 128 ? (t & 15) : ((t >> 1) & 7); }
 template <int D>
-__device__ __forceinline__ int v_swizzle(int t) { return D == 128 ? (t & 3) << 2 : (t & 2) << 1; }
+__device__ __forceinline__ int v_swizzle(int t) { return D == 128 ? 5 * (t & 3) : ((t & 2) << 1) ^ ((t >> 1) & 3); }
 
 template <int D, bool I4, int kWaves>
 struct Smem {
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     const uint32_t k_read = k_lds + r32 * kRow + 16 * (half ^ k_swizzle<D>(r32));
     // the transposing read: 16 lanes at 4 positions' 32 bytes of d = 32 i + 16 (lane / 16 % 2) ..
     const uint32_t v_read = v_lds + (4 * half + ((lane & 15) >> 2)) * kRow +
-                            ((32 * ((lane >> 4) & 1) + 8 * (lane & 3)) ^ (16 * v_swizzle<D>((lane & 15) >> 2)));
+                            ((32 * ((lane >> 4) & 1) + 8 * (lane & 3)) ^ (16 * v_swizzle<D>(4 * half + ((lane & 15) >> 2))));
 
     // Fragments of the products, a quarter of a tile's at a time: KS / 4 steps of
     // d for both halves of the keys, one step of 16 positions for all values d.
@@ -548,8 +549,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     // the lane's rows of the sums are d = 32 i + 8 k + 4 half + y, of codes in their order
     if (S == 1) {
         // through LDS (the tiles are used, a wave has 32 rows of it), so that a row goes out
-        // in one piece.  (8 bytes a lane to 32 rows at a time: 241 us of the windowed case above,
-        // 226 so.)
+        // in one piece.  (8 bytes a lane to 32 rows at a time: the windowed case above took 241
+        // us, 226 so.)
         const float f = l != 0.f ? 1.f / l : 0.f;
         auto piece_of = [&](int r, int c) { return wave * 32 * kRow + r * kRow + 16 * (c ^ (D == 128 ? r & 15 : r >> 1 & 7)); };
 #pragma unroll
