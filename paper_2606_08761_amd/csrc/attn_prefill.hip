@@ -604,9 +604,10 @@ struct Plan {
     int S;
 };
 
-// Eight waves (256 rows, half the staging a row; 3 % of a long prompt's time) where
-// that leaves four workgroups a compute unit of 32 tiles or more, and always for
-// codes; four otherwise: two workgroups a unit hide each other's beginnings.  The
+// Eight waves (256 rows, half the staging a row) where that leaves four workgroups a
+// compute unit of 12 tiles or more, and always for codes (8192 tokens 1154 -> 1111 us, a
+// window of 1024 179 -> 175); four otherwise: two workgroups a unit hide each other's
+// beginnings and even out the last round (4 x 1024 tokens, two a unit: 63 us, 68).  The
 // tiles are split where the workgroups number fewer than the compute units, into
 // parts of at least four tiles, as many as the units hold at once and no more (32
 // rows of 7954 positions: 4 parts 94 us, 5 parts 120).
@@ -621,7 +622,7 @@ Plan plan_prefill(const KvView& c, const AttnArgs& a) {
         const int64_t w = (static_cast<int64_t>(a.window) + tokens + kW - 2) / kW + 1 + (static_cast<int64_t>(a.sinks) + kW - 1) / kW;
         tiles = std::min(tiles, w);
     }
-    p.waves = c.i4 || (c.D == 128 && tiles >= 32 && heads * ((a.max_q * group + 255) / 256) >= 4 * cu) ? 8 : 4;
+    p.waves = c.i4 || (c.D == 128 && tiles >= 12 && heads * ((a.max_q * group + 255) / 256) >= 4 * cu) ? 8 : 4;
     const int64_t rows = 32 * p.waves;
     p.row_tiles = static_cast<int>((a.max_q * group + rows - 1) / rows);
     const int64_t units = heads * p.row_tiles;

@@ -321,3 +321,13 @@ def test_scores_of_large_magnitude(pk, cache, D):
     n = paged.Case(73, [130, 700], [70, 33], 8, 2, D, 16, cache, sd=3000.0)
     n.q = (n.q * np.float16(2600.0)).astype(np.float16)
     check(prefill(pk, n), n)
+
+
+@pytest.mark.parametrize("page,window,sinks", [(16, 0, 0), (64, 0, 0), (16, 800, 5), (128, 790, 0)])
+def test_prefill_of_many_workgroups(pk, page, window, sinks):
+    """The form with 256 rows a workgroup: 64 sequences x 8 key heads x 2 tiles of
+    rows, and more than 12 tiles of positions."""
+    lens = [1100, 900, 64, 1] + [3 + 7 * i % 60 for i in range(60)]
+    news = [40, 33, 64, 1] + [1 + i % 2 for i in range(60)]
+    c = paged.Case(83 + page, lens, news, 64, 8, 128, page, "fp16", window=window, sinks=sinks)
+    check(prefill(pk, c), c)
