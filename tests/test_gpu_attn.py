@@ -331,3 +331,19 @@ def test_prefill_of_many_workgroups(pk, page, window, sinks):
     news = [40, 33, 64, 1] + [1 + i % 2 for i in range(60)]
     c = paged.Case(83 + page, lens, news, 64, 8, 128, page, "fp16", window=window, sinks=sinks)
     check(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_many_rows_in_parts(pk, cache, D):
+    """The join that puts several rows in a workgroup: 40 sequences of 64 heads, their
+    length in several parts, most of which most sequences do not have."""
+    lens = [1700, 1400, 700, 0] + [1 + 11 * i % 90 for i in range(36)]
+    c = paged.Case(89 + D, lens, [1 if n else 0 for n in lens], 64, 8, D, 16, cache)
+    c.q = np.concatenate([c.q, np.ones((1, 64, D), np.float16)])[[int(c.start[b]) if n else -1 for b, n in enumerate(lens)]]
+    c.news = [1] * len(lens)
+    c.start, c.T = np.arange(len(lens) + 1, dtype=np.int32), len(lens)
+    assert pk.apex4_attn_decode_workspace_size(len(lens), c.width, c.width * 16, 64, 8, D, 16) > 0
+    y = decode(pk, c)
+    check(y, c)
+    assert (y[3] == 0).all()
