@@ -300,3 +300,38 @@ def test_an_empty_status_is_refused(pk):
     for call in (lambda: c.reserve([0], [5], status=none), lambda: c.fork([0], [1], status=none), lambda: c.compact(status=none)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D,H", [(64, 3), (128, 2)])
+def test_append_of_long_prompts(pk, cache, D, H):
+    """Enough tokens that a workgroup takes several, of more than one sequence: the
+    same bytes as token after token."""
+    import torch
+    lens = [3500, 1, 2, 1999, 0, 530, 3]
+    page, T = 32, sum(lens)
+    rows = [-(-n // page) for n in lens]
+    order = torch.randperm(sum(rows) + 2, generator=torch.Generator().manual_seed(D))
+    table = torch.full((len(lens), max(rows)), -1, dtype=torch.int32)
+    for b, n in enumerate(rows):
+        table[b, :n] = order[sum(rows[:b]):sum(rows[:b]) + n]
+    start = torch.tensor([sum(lens[:b]) for b in range(len(lens) + 1)], dtype=torch.int32).cuda()
+    table, kv_len = table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+    g = torch.Generator(device="cuda").manual_seed(D + 1)
+    k, v = (torch.randn((T, H, D), device="cuda", generator=g).to(torch.float16) for _ in range(2))
+    size = pk.apex4_kv_page_bytes(cache, H, D, page)
+    kp, vp, kq, vq = (torch.zeros((sum(rows) + 2, size), dtype=torch.uint8, device="cuda") for _ in range(4))
+    pk.apex4_kv_append(k, v, kp, vp, table, kv_len, page, q_start=start, cache=cache)
+    # one token at a time to each of up to 512 "sequences", which share their tables
+    at = torch.cat([torch.stack([torch.full((n,), b), torch.arange(1, n + 1)]) for b, n in enumerate(lens) if n], 1).cuda()
+    for i in range(0, T, 512):
+        b, n = at[0, i:i + 512], at[1, i:i + 512].to(torch.int32)
+        pk.apex4_kv_append(k[i:i + 512], v[i:i + 512], kq, vq, table[b].contiguous(), n, page, cache=cache)
+    assert torch.equal(kp, kq) and torch.equal(vp, vq) and bool(kp.any())
+    gk, gv = pk.apex4_kv_gather(kp, vp, table, kv_len, T, H, D, page, q_start=start, cache=cache)
+    for i in range(0, T, 512):
+        b, n = at[0, i:i + 512], at[1, i:i + 512].to(torch.int32)
+        a, c = pk.apex4_kv_gather(kp, vp, table[b].contiguous(), n, len(n), H, D, page, cache=cache)
+        assert torch.equal(a, gk[i:i + 512]) and torch.equal(c, gv[i:i + 512])
+    if cache == "fp16":
+        assert torch.equal(gk, k) and torch.equal(gv, v)
