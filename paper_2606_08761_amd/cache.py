@@ -105,6 +105,13 @@ def _output(out, shape, like, stream):
     return out
 
 
+def _output_like(out, q, stream):
+    """_output of q's shape; quicker where q has no gaps."""
+    if out is None and stream is None and q.is_contiguous():
+        return _torch().empty_like(q)
+    return _output(out, q.shape, q, stream)
+
+
 def _workspace(workspace, need, like, stream):
     """(pointer, bytes): the caller's, or one made here where one is needed."""
     if workspace is None:
@@ -195,7 +202,7 @@ def apex4_attn_decode(q, k_pages, v_pages, table, kv_len, kv_heads: int, page: i
     if rows != B:
         raise ValueError("q must have one row a sequence")
     most = width * page if max_len is None else max_len
-    out = _output(out, (B, H, D), q, stream)
+    out = _output_like(out, q, stream)
     need = _decode_need(q.get_device(), B, width, most, H, kv_heads, D, page, window, sinks) if workspace is None else 0
     wp, wn, held = _workspace(workspace, need, q, stream)
     rc = lib().apex4_attn_decode(qp, qs, kpp, vpp, n, tp, width, lp, B, most, H, kv_heads, D, page, _kind(cache), window,
@@ -219,7 +226,7 @@ def apex4_attn_prefill(q, q_start, k_pages, v_pages, table, kv_len, kv_heads: in
     sp = _starts(q_start, B)
     most = width * page if max_len is None else max_len
     most_q = T if max_q is None else max_q
-    out = _output(out, (T, H, D), q, stream)
+    out = _output_like(out, q, stream)
     need = (_prefill_need(q.get_device(), T, B, most_q, width, most, H, kv_heads, D, page, window, sinks)
             if workspace is None else 0)
     wp, wn, held = _workspace(workspace, need, q, stream)
