@@ -65,6 +65,7 @@ struct Smem {
     // step t, beside the writing of tile t + 2's: four slots
     float ks[4][I4 ? kW : 4];
     float vs[2][I4 ? kW : 4];
+    float vl[2][I4 ? kW : 4];  // log2 of the values', for a row's maximum
     uint32_t vs_most[4];       // the largest of a tile's, as bits; a tile's slot is cleared two steps before it is written
 };
 
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     const int64_t head_at = static_cast<int64_t>(h) << c.page_shift;
     const int64_t scale_at = (static_cast<int64_t>(c.kv_heads) << c.page_shift) * (D / 2);
     const uint32_t k_lds = lds_offset(sm.k), v_lds = lds_offset(sm.v);
-    const uint32_t ks_lds = lds_offset(sm.ks), vs_lds = lds_offset(sm.vs);
+    const uint32_t ks_lds = lds_offset(sm.ks), vs_lds = lds_offset(sm.vs), vl_lds = lds_offset(sm.vl);
 
     // positions that no row of the workgroup sees hold anything: their values,
     // times a weight of zero, must not count
@@ -318,6 +319,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                 } else {
                     const float scale = seen_by_some(tiles.start(t) + i_pos) ? x : 0.f;
                     sm.vs[buf][i_pos] = scale;
+                    sm.vl[buf][i_pos] = __builtin_amdgcn_logf(fmaxf(scale, 0x1p-24f));
                     atomicMax(&sm.vs_most[anew(t & 3)], __builtin_bit_cast(uint32_t, fmaxf(scale, 0.f)));  // not negative: bits are in order
                 }
             }
@@ -446,8 +448,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
 #pragma unroll
                 for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[u][j]);
             top *= f_log2;
-            if constexpr (I4) {  // a bound of the scores with their values' scales
+            if constexpr (I4) {
+                // A bound of the scores plus log2 of their values' scales; where it passes
+                // the slack, their maximum for each row.  The bound is none: its scale may
+                // be that of a position without weight, or of one that the row does not
+                // see, and under it the row's weights would fall below what binary16
+                // holds.  (The windowed case above 200 -> 206 us; in the same branch as
+                // the rescale 218, for the compiler then copies the output sums every tile;
+                // with the logarithms taken here 210.)
                 top += __builtin_amdgcn_logf(__builtin_bit_cast(float, sm.vs_most[t & 3]));
+                if (__any(top > m + kSlack)) {
+                    top = kNoMax;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const f32x4 sv = __builtin_bit_cast(f32x4, read_lds(vl_lds + sb + 4 * kW * buf + 32 * i));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            top = fmaxf(top, sc[i >> 2][4 * (i & 3) + j] + sv[j]);
+                    }
+                }
             }
             if (__any(top > m + kSlack)) {
                 top = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);

@@ -1,0 +1,86 @@
+"""Prompts of enough rows a key head that the kernel for many rows attends: 4-bit
+values of very different sizes, bounds that a call breaks, long flat tails, and
+the forms that only few-row calls reach elsewhere."""
+import numpy as np
+import pytest
+
+from tests import paged
+from tests.test_gpu_attn import check, dev, prefill
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def pk():
+    import paper_2606_08761_amd as pk
+    return pk
+
+
+def rewrite(c, b, t, k=None, v=None):
+    """Token t of sequence b gets other keys or values, [H, D]."""
+    for x, plane, keep in ((k, c.k, c.K), (v, c.v, c.V)):
+        if x is not None:
+            at = c.table[b, t // c.page], t % c.page
+            plane.put(*at, np.asarray(x, np.float16))
+            keep[b][t] = plane.get(*at)
+
+
+def check_contributions(y, c):
+    """As check(), with the term of the many tokens in proportion to what a token
+    contributes, not to the largest value seen: weights times values' scales are
+    rounded relative to the largest of them, 2^-25 of it at most below binary16's normal
+    range, and times a code of at most 8 (2^3); a value's scale is a seventh (2^-2.8) of
+    its largest entry, so 2^-24.8 of the largest weight times entry, a token."""
+    got = y.cpu().numpy().astype(np.float64)
+    group = c.Hq // c.H
+    for b, n in enumerate(c.lens):
+        for i in range(c.news[b]):
+            p = n - c.news[b] + i
+            t = np.array([t for t in range(p + 1) if paged.seen(p, t, c.window, c.sinks)])
+            for j in range(c.Hq):
+                K, V = c.K[b][t, j // group], c.V[b][t, j // group]
+                s = K @ c.q[c.start[b] + i, j].astype(np.float64) * c.scale
+                w = np.exp(s - s.max())
+                w /= w.sum()
+                out, mean, most = w @ V, w @ np.abs(V), (w * np.abs(V).max(axis=1)).max()
+                tol = 2.0 ** -10 * mean + 2.0 ** -11 * np.abs(out) + len(t) * 2.0 ** -24 * most + 2.0 ** -24
+                err = np.abs(got[c.start[b] + i, j] - out)
+                assert (err <= tol).all(), (b, i, j, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 0), (70, 3)])
+def test_int4_values_of_other_positions_do_not_cost_precision(pk, D, window, sinks):
+    """A value of thousands among ones of some hundredths: rows that do not see it (it
+    is later, or before their window), in its tile and in others, keep theirs."""
+    for far in (2, 40, 130, 195):
+        c = paged.Case(101 + far, [200], [200], 4, 1, D, 16, "int4", window=window, sinks=sinks, spoil=False)
+        g = np.random.default_rng(far)
+        for t in range(200):
+            rewrite(c, 0, t, v=g.standard_normal((1, D)) * (4000.0 if t == far else 0.02))
+        check_contributions(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_int4_large_values_of_no_weight_do_not_cost_precision(pk, D):
+    """Rows that see the large value, with a score that leaves it no weight: first
+    tokens with large values, a tile's only one, one a tile."""
+    for far in ([0], [100], [10, 74, 138, 199]):
+        c = paged.Case(113, [200], [40], 4, 1, D, 16, "int4", spoil=False)
+        g = np.random.default_rng(len(far))
+        c.q = np.abs(c.q)
+        for t in range(200):
+            big = t in far
+            rewrite(c, 0, t, k=np.full((1, D), -30.0) if big else None, v=g.standard_normal((1, D)) * (4000.0 if big else 0.02))
+        check_contributions(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("big", [1024.0, 2.0 ** -14])
+def test_int4_scales_far_apart_in_prompts(pk, D, big):
+    """Values of 2^-14 and of 2^10 in one prompt, and nothing but tiny ones."""
+    c = paged.Case(127, [200], [30], 4, 1, D, 16, "int4", spoil=False)
+    g = np.random.default_rng(3)
+    for t in range(200):
+        rewrite(c, 0, t, v=g.standard_normal((1, D)) * (big if t in (90, 91, 180) else 2.0 ** -14))
+    check_contributions(prefill(pk, c), c)
