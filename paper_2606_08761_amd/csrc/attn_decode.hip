@@ -81,7 +81,8 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
     // the sequence's rows of this key head: its new tokens times the heads that share it
     const int q0 = a.q_start ? a.q_start[b] : b;
     const int n = a.q_start ? new_tokens(a, b) : 1;
-    const uint32_t all_rows = n * group, row0 = rt * kRows;  // T heads and max_q heads are below 2^28
+    const int taken = min(n, static_cast<int>(a.max_q));  // past max_q tokens nothing is computed
+    const uint32_t all_rows = taken * group, row0 = rt * kRows;  // T heads and max_q heads are below 2^28
     if (row0 >= all_rows) return;
     const int rows = min(static_cast<int>(all_rows - row0), kRows);  // of this workgroup
     struct Row {
@@ -120,9 +121,9 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
             if constexpr (I4) qf[s] = code_order(qf[s]);
         }
     }
-    const int len = cached_tokens(c, b);
-    const int pos = len - n + tok;  // of the lane's row (negative: it sees nothing)
-    const Tiles<kTile> tiles(len - n, len - 1, a.window, a.sinks);
+    const int before = cached_tokens(c, b) - n, len = before + taken;  // positions that some row sees end at len
+    const int pos = before + tok;  // of the lane's row (negative: it sees nothing)
+    const Tiles<kTile> tiles(before, len - 1, a.window, a.sinks);
     const int t1 = min(t0 + range, tiles.count);
     if (t0 >= t1) {
         if (S > 1) {
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
         more_k();
         // positions that a row does not see: their scores do not count, and the values
         // of those that no row sees, whatever they are, are zero
-        const bool masked = at + kTile > len - n + 1 || (at < edge && at + kTile > tiles.sinks);
+        const bool masked = at + kTile > before + 1 || (at < edge && at + kTile > tiles.sinks);
         if (masked) {
             const int from = a.window ? pos - a.window + 1 : 0;
 #pragma unroll

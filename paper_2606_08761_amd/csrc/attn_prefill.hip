@@ -139,7 +139,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     }
     const uint32_t group = a.group;
 
-    const uint32_t rows = n * group;  // T heads and max_q heads are below 2^28
+    // past max_q tokens nothing is computed; T heads and max_q heads are below 2^28
+    const uint32_t rows = min(n, static_cast<int>(a.max_q)) * group;
     const int mt = static_cast<int>((rows + kRows - 1) / kRows) - 1 - from_last;
     if (mt < 0) return;
     const uint32_t R0 = mt * kRows;

@@ -84,3 +84,27 @@ def test_int4_scales_far_apart_in_prompts(pk, D, big):
     for t in range(200):
         rewrite(c, 0, t, v=g.standard_normal((1, D)) * (big if t in (90, 91, 180) else 2.0 ** -14))
     check_contributions(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D,Hq,H,lens,news,max_q,window,sinks", [
+    (128, 8, 1, [300, 40], [300, 40], 100, 0, 0),    # several tiles of rows, whole
+    (64, 8, 1, [300, 40], [300, 40], 33, 60, 4),
+    (128, 8, 1, [2500, 700], [300, 9], 20, 0, 0),    # cut along the positions
+    (64, 8, 1, [2500, 700], [300, 9], 20, 1200, 4),
+    (128, 4, 2, [2500, 90], [50, 3], 4, 0, 0),       # few rows
+    (64, 4, 2, [900, 90], [50, 3], 1, 100, 2),
+])
+def test_tokens_up_to_max_q_have_their_outputs(pk, cache, D, Hq, H, lens, news, max_q, window, sinks):
+    """More new tokens than the bound says: the first max_q of each sequence are
+    computed, at their own positions."""
+    import torch
+    c = paged.Case(157, lens, news, Hq, H, D, 16, cache, window=window, sinks=sinks)
+    need = pk.apex4_attn_prefill_workspace_size(c.T, len(lens), max_q, c.width, c.width * 16, Hq, H, D, 16, window, sinks)
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    out = torch.full((c.T, Hq, D), float("nan"), dtype=torch.float16, device="cuda")
+    y = prefill(pk, c, max_q=max_q, workspace=ws, out=out).cpu().numpy().astype(np.float64)
+    want, tol = c.expected()
+    for b, n in enumerate(news):
+        rows = slice(c.start[b], c.start[b] + min(n, max_q))
+        assert (np.abs(y[rows] - want[rows]) <= tol[rows]).all(), b
