@@ -343,9 +343,11 @@ def apex4_pages_copy(pool, src, dst, stream=None):
 
 class PagedKVCache:
     """The planes of all layers, the page tables of ``slots`` sequences and the
-    pages' reference counts.  Everything stays on the device: no call waits for
-    it, so a step can be captured into a HIP graph.  reserve and fork return
-    their outcome as a device tensor (``reserved(status)`` reads it).
+    pages' reference counts.  Everything stays on the device: with slots and lengths
+    given as device tensors no call waits for it, so a step can be captured into a
+    HIP graph; a list is copied there first, which waits for the stream's work and
+    cannot be captured.  reserve and fork return their outcome as a device tensor
+    (``reserved(status)`` reads it).
 
     pages: of each plane; page: tokens a page; max_len: tokens a sequence may
     reach."""
@@ -362,9 +364,14 @@ class PagedKVCache:
         self.refs = torch.zeros((pages,), dtype=torch.int32, device=device)
         self.planes = [(self.pool[2 * i], self.pool[2 * i + 1]) for i in range(layers)]
 
-    def _seqs(self, seqs):
+    def _seqs(self, seqs, stream=None):
+        """A list as a tensor of the stream that the call runs on: its memory goes
+        to no other call before that stream has read it."""
         torch = _torch()
-        return seqs if isinstance(seqs, torch.Tensor) else torch.tensor(seqs, dtype=torch.int32, device=self.table.device)
+        if isinstance(seqs, torch.Tensor):
+            return seqs
+        with torch.cuda.stream(stream):  # None: the current one
+            return torch.tensor(seqs, dtype=torch.int32, device=self.table.device)
 
     @staticmethod
     def reserved(status) -> bool:
@@ -372,14 +379,15 @@ class PagedKVCache:
         return int(status.item()) == 0
 
     def reserve(self, seqs, new_len, **kw):
-        return apex4_pages_reserve(self.table, self.kv_len, self.refs, self._seqs(seqs), self._seqs(new_len), self.page, **kw)
+        return apex4_pages_reserve(self.table, self.kv_len, self.refs, self._seqs(seqs, kw.get("stream")),
+                                   self._seqs(new_len, kw.get("stream")), self.page, **kw)
 
     def fork(self, parents, children, **kw):
-        return apex4_pages_fork(self.pool, self.table, self.kv_len, self.refs, self._seqs(parents), self._seqs(children),
-                                self.page, **kw)
+        return apex4_pages_fork(self.pool, self.table, self.kv_len, self.refs, self._seqs(parents, kw.get("stream")),
+                                self._seqs(children, kw.get("stream")), self.page, **kw)
 
     def free(self, seqs, **kw):
-        apex4_pages_free(self.table, self.kv_len, self.refs, self._seqs(seqs), **kw)
+        apex4_pages_free(self.table, self.kv_len, self.refs, self._seqs(seqs, kw.get("stream")), **kw)
 
     def compact(self, **kw):
         return apex4_pages_compact(self.pool, self.table, self.refs, **kw)

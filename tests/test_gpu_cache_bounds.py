@@ -1,0 +1,61 @@
+"""PagedKVCache and the page calls where a call's bounds meet: lengths past max_len
+that the table still holds, more pages asked for than there are, lists on other
+streams."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def pk():
+    import paper_2606_08761_amd as pk
+    return pk
+
+
+def test_lists_belong_to_the_stream_of_the_call(pk, monkeypatch):
+    """The memory of a list's tensor goes to no call on another stream: the current
+    one's next small tensors are not made of it."""
+    import torch
+
+    from paper_2606_08761_amd import cache
+    c = pk.PagedKVCache(layers=1, pages=64, slots=16, kv_heads=1, head_dim=64, page=16, max_len=64)
+    made = []
+
+    def watched(name, at):
+        call = getattr(cache, name)
+
+        def run(*args, **kw):
+            made.extend(args[i].data_ptr() for i in at)
+            return call(*args, **kw)
+        monkeypatch.setattr(cache, name, run)
+
+    watched("apex4_pages_reserve", (3, 4))
+    watched("apex4_pages_fork", (4, 5))
+    watched("apex4_pages_free", (3,))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    others = []
+
+    def then():
+        torch.cuda._sleep(200_000)
+        others.extend(torch.full((1,), 7, dtype=torch.int32, device="cuda") for _ in range(8))
+        assert not set(made) & {x.data_ptr() for x in others}
+
+    for i in range(6):
+        status = c.reserve([i], [20 + i], stream=s)
+        then()
+        s.synchronize()
+        assert c.reserved(status)
+    for i in range(6):
+        status = c.fork([i], [6 + i], stream=s)
+        then()
+        s.synchronize()
+        assert c.reserved(status)
+    assert c.kv_len.tolist() == [*range(20, 26), *range(20, 26), 0, 0, 0, 0]
+    for i in range(0, 12, 2):
+        c.free([i], stream=s)
+        then()
+    s.synchronize()
+    assert c.kv_len.tolist() == [0 if i % 2 == 0 else 20 + i % 6 for i in range(12)] + [0] * 4
+    assert len(made) == 6 * 2 + 6 * 2 + 6
