@@ -26,9 +26,13 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // zero, not NaN, where every score so far is masked (s = -inf).
 constexpr float kNoMax = -1e30f;
 // Scores may pass the running maximum by this much (in units of log2) before
-// the sums are rescaled: the weights stay below 2^8, exact enough in binary16,
-// and after the first tiles a rescale is rare.
+// the sums are rescaled: after the first tiles a rescale is rare.  The weights of
+// decoding stay below 2^8.  Those of prefill, whose sums run over a whole length, are
+// scaled by 2^kHeadroom and stay below 2^15: binary16 then holds them to 2^-32 of the
+// largest one, and a long tail of small weights, rounded the same way each, keeps its
+// share (without it 40000 of 2^-25 vanished: 1.2e-3 of the result).
 constexpr float kSlack = 8.f;
+constexpr float kHeadroom = 7.f;
 constexpr float kMostWeight = 256.f;
 constexpr float kMostSum = 0x1p60f;
 

@@ -448,7 +448,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[u][j]);
-            top *= f_log2;
+            // how far the row's largest weight would be above 1, in units of log2: of scores
+            // of any magnitude (differences are taken first, or inside one fma)
+            float rise, most_vl = 0.f;
             if constexpr (I4) {
                 // A bound of the scores plus log2 of their values' scales; where it passes
                 // the slack, their maximum for each row.  The bound is none: its scale may
@@ -457,19 +459,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                 // holds.  (The windowed case above 200 -> 206 us; in the same branch as
                 // the rescale 218, for the compiler then copies the output sums every tile;
                 // with the logarithms taken here 210.)
-                top += __builtin_amdgcn_logf(__builtin_bit_cast(float, sm.vs_most[t & 3]));
-                if (__any(top > m + kSlack)) {
-                    top = kNoMax;
+                most_vl = __builtin_amdgcn_logf(__builtin_bit_cast(float, sm.vs_most[t & 3]));
+                rise = (top - m) + most_vl;
+                if (__any(rise > kHeadroom + kSlack)) {
+                    most_vl = kNoMax;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const f32x4 sv = __builtin_bit_cast(f32x4, read_lds(vl_lds + sb + 4 * kW * buf + 32 * i));
+                        const f32x4 vl = __builtin_bit_cast(f32x4, read_lds(vl_lds + sb + 4 * kW * buf + 32 * i));
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            top = fmaxf(top, sc[i >> 2][4 * (i & 3) + j] + sv[j]);
+                            most_vl = fmaxf(most_vl, (sc[i >> 2][4 * (i & 3) + j] - top) + vl[j]);
                     }
+                    rise = (top - m) + most_vl;
                 }
+            } else {
+                rise = fmaf(top, f_log2, -m);
             }
-            if (__any(top > m + kSlack)) {
+            if (__any(rise > kHeadroom + kSlack)) {
+                top = I4 ? top + (most_vl - kHeadroom) : fmaf(top, f_log2, -kHeadroom);
                 top = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
                 const float f = exp2_fast(m - top);
                 l *= f;
@@ -481,6 +488,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
             }
             // the next tile's products (past the last tile: of whatever lies there, and
             // not used) a quarter at a time beside a quarter of the exponentials
+            // A tile's weights are summed first: added one by one to the sum of a long
+            // length, small ones would all be rounded the same way.
+            float sum = 0.f;
             u32x4 pw[4];
             const uint32_t kb = anew(k_read + (buf ^ 1) * kTileBytes), vb = anew(v_read + buf * kTileBytes);
 #pragma unroll
@@ -498,17 +508,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                     const float x = sc[s >> 1][8 * (s & 1) + j];
                     e[j] = exp2_fast(I4 ? x - m : fmaf(x, f_log2, -m));
                     if constexpr (I4) {
-                        l += e[j];
+                        sum += e[j];
                         e[j] *= sv[j >> 2][j & 3];
                     }
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t p = pack_f16(e[2 * j], e[2 * j + 1]);
-                    if constexpr (!I4) l = add_pair(p, l);  // the rounded weights: one large weight's rounding cancels
+                    if constexpr (!I4) sum = add_pair(p, sum);  // the rounded weights: one large weight's rounding cancels
                     pw[s][j] = p;
                 }
             }
+            l += sum;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const ValueFrags vf = read_v(s, vb);

@@ -108,3 +108,37 @@ def test_tokens_up_to_max_q_have_their_outputs(pk, cache, D, Hq, H, lens, news, 
     for b, n in enumerate(news):
         rows = slice(c.start[b], c.start[b] + min(n, max_q))
         assert (np.abs(y[rows] - want[rows]) <= tol[rows]).all(), b
+
+
+@pytest.mark.parametrize("cache,n", [("fp16", 40000), ("int4", 100000)])
+@pytest.mark.parametrize("below", [25.02, 22.3])
+def test_long_flat_tails_keep_their_share(pk, cache, n, below):
+    """One token of weight 1 and n - 1 of 2^-below: alone they are next to binary16's
+    smallest numbers, together they are a part in some hundreds of the result."""
+    import torch
+    H, group, D, page, T = 8, 8, 64, 64, 512
+    pages = n // page + 1
+    planes = [torch.zeros((pages, pk.apex4_kv_page_bytes(cache, H, D, page)), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    k = torch.zeros((n, H, D), dtype=torch.float16, device="cuda")
+    v = torch.ones((n, H, D), dtype=torch.float16, device="cuda")
+    k[0, :, 0] = below * np.log(2.0)
+    v[0] = -1.0
+    kv_len = torch.tensor([n], dtype=torch.int32, device="cuda")
+    pk.apex4_kv_append(k, v, *planes, table, kv_len, page, q_start=torch.tensor([0, n], dtype=torch.int32, device="cuda"), cache=cache)
+    q = torch.zeros((T, H * group, D), dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 1.0
+    start = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    # whole lengths: the tiles of rows fill the compute units
+    y = pk.apex4_attn_prefill(q, start, *planes, table, kv_len, H, page, max_q=T, cache=cache, scale=1.0).double()
+    a, b = pk.apex4_kv_gather(*planes, table, kv_len, n, H, D, page, q_start=torch.tensor([0, n], dtype=torch.int32, device="cuda"), cache=cache)
+    score, first, rest = a[0, 0, 0].double(), b[0, 0, 0].double(), b[1, 0, 0].double()
+    share = torch.arange(n - T, n, device="cuda", dtype=torch.float64) * torch.exp(-score)
+    want = ((first + share * rest) / (1 + share))[:, None, None]
+    mean = ((first.abs() + share * rest.abs()) / (1 + share))[:, None, None]
+    # the weight of the first is exact; a tail's weight, all equal, may be rounded the same
+    # way every time: 2^-11 of it, or, below the normal range, 2^-31 of the largest one, each;
+    # 2^-11 and the sums' 32 bits for the rest
+    tol = 2.0 ** -11 * want.abs() + 2.0 ** -11 * (share[:, None, None] * 2) + n * 2.0 ** -31 * 2 + 2.0 ** -14 * mean
+    err = (y - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
