@@ -350,16 +350,17 @@ class PagedKVCache:
     (``reserved(status)`` reads it).
 
     pages: of each plane; page: tokens a page; max_len: tokens a sequence may
-    reach."""
+    reach, to the end of the page that holds the last (kept so as ``max_len``)."""
 
     def __init__(self, layers: int, pages: int, slots: int, kv_heads: int, head_dim: int = 128, page: int = 16,
                  max_len: int = 4096, cache: str = "fp16", device="cuda"):
         torch = _torch()
         size = apex4_kv_page_bytes(cache, kv_heads, head_dim, page)
         self.layers, self.kv_heads, self.head_dim, self.page, self.cache = layers, kv_heads, head_dim, page, cache
-        self.max_len = max_len
+        width = -(-max_len // page)
+        self.max_len = width * page  # what reserve gives, and so what attention has to see
         self.pool = torch.zeros((2 * layers, pages, size), dtype=torch.uint8, device=device)
-        self.table = torch.full((slots, -(-max_len // page)), -1, dtype=torch.int32, device=device)
+        self.table = torch.full((slots, width), -1, dtype=torch.int32, device=device)
         self.kv_len = torch.zeros((slots,), dtype=torch.int32, device=device)
         self.refs = torch.zeros((pages,), dtype=torch.int32, device=device)
         self.planes = [(self.pool[2 * i], self.pool[2 * i + 1]) for i in range(layers)]

@@ -59,3 +59,24 @@ def test_lists_belong_to_the_stream_of_the_call(pk, monkeypatch):
     s.synchronize()
     assert c.kv_len.tolist() == [0 if i % 2 == 0 else 20 + i % 6 for i in range(12)] + [0] * 4
     assert len(made) == 6 * 2 + 6 * 2 + 6
+
+
+@pytest.mark.parametrize("kind", ["fp16", "int4"])
+def test_lengths_up_to_the_tables_end_are_seen(pk, kind):
+    """max_len inside a page: what reserve gives, attention sees."""
+    import torch
+    c = pk.PagedKVCache(layers=1, pages=8, slots=2, kv_heads=2, head_dim=64, page=16, max_len=20, cache=kind)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    n = 30
+    assert c.reserved(c.reserve([1], [n]))
+    assert not c.reserved(c.reserve([0], [33]))  # does not fit the table
+    k, v = (torch.randn((n, 2, 64), device="cuda", generator=g).to(torch.float16) for _ in range(2))
+    q = torch.randn((n, 4, 64), device="cuda", generator=g).to(torch.float16)
+    start = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    b = c.batch([1])
+    c.append(0, k, v, b, start)
+    args = (*c.planes[0], *b, 2, 16)
+    assert torch.equal(c.decode(0, q[-1:], b), pk.apex4_attn_decode(q[-1:], *args, cache=kind))
+    assert torch.equal(c.prefill(0, q, b, start, n), pk.apex4_attn_prefill(q, start, *args, max_q=n, cache=kind))
+    assert torch.equal(c.prefill(0, q[-2:], b, torch.tensor([0, 2], dtype=torch.int32, device="cuda"), 2),
+                       pk.apex4_attn_prefill(q[-2:], torch.tensor([0, 2], dtype=torch.int32, device="cuda"), *args, max_q=2, cache=kind))
