@@ -419,8 +419,8 @@ int apex4_w4a4_gemm_mx_ws(const uint8_t* A_6, const uint8_t* e_a,
  *
  * int32 buffers need 4-byte alignment, all others 16-byte alignment.  Values in
  * device memory cannot be validated: page ids outside [0, n_pages), lengths past
- * width * page (or past max_len) and sequence numbers outside the table are never
- * used as addresses.  append leaves out tokens that have no page, gather returns
+ * width * page (or past max_len), starts outside [0, T] and sequence numbers outside
+ * the table are never used as addresses.  append leaves out tokens that have no page, gather returns
  * zeros for them, and attention to such positions is unspecified.
  * Limits: n_pages, max_len and the bytes of a page up to 2^30, width up to 2^20, B
  * and T up to 2^24, T heads up to 2^27.

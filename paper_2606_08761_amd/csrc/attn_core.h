@@ -47,10 +47,11 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     return __builtin_bit_cast(uint32_t, r);
 }
 
-// New tokens of sequence b of the packed ones.
+// New tokens of sequence b of the packed ones: those of rows q_start[b] .. that are
+// among the T, none where the start is not.  (So that no row number overflows.)
 __device__ __forceinline__ int new_tokens(const AttnArgs& a, int b) {
-    const int n = a.q_start[b + 1] - a.q_start[b];
-    return n < 0 ? 0 : n < a.T ? n : static_cast<int>(a.T);
+    const int64_t first = a.q_start[b], n = a.q_start[b + 1] - first, left = a.T - first;
+    return static_cast<int>(first < 0 || n < 0 || left < 0 ? 0 : n < left ? n : left);
 }
 
 // Tiles of W positions that rows at positions p_lo .. p_hi see (causal, a

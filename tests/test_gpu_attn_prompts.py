@@ -142,3 +142,24 @@ def test_long_flat_tails_keep_their_share(pk, cache, n, below):
     tol = 2.0 ** -11 * want.abs() + 2.0 ** -11 * (share[:, None, None] * 2) + n * 2.0 ** -31 * 2 + 2.0 ** -14 * mean
     err = (y - want).abs()
     assert bool((err <= tol).all()), float((err / tol).max())
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D,Hq,max_q", [(64, 8, 90), (128, 8, 90), (128, 4, 2)])
+def test_starts_out_of_range_are_no_rows(pk, cache, D, Hq, max_q):
+    """Starts of sequences that are no row numbers (a broken q_start) read and write
+    nothing there; the sequences before them have their outputs."""
+    import torch
+    c = paged.Case(163, [300, 200, 50, 90, 70], [40, 20, 10, 10, 10], Hq, 2, D, 16, cache)
+    out = torch.full((c.T, Hq, D), 7.0, dtype=torch.float16, device="cuda")
+    big = 2 ** 31 - 1
+    for rest in ([60, big, big - 3, 90], [60, -5, -2 ** 31, 90], [60, big, -1, big], [60, 2 ** 24, 2 ** 30, c.T + 1]):
+        out.fill_(7.0)
+        start = np.array([0, 40] + rest, np.int64).astype(np.int32)
+        pk.apex4_attn_prefill(dev(c.q), dev(start), dev(c.k.raw), dev(c.v.raw), dev(c.table), dev(np.array(c.lens, np.int32)),
+                              2, 16, max_q=max_q, cache=cache, out=out)
+        got, (want, tol) = out.cpu().numpy().astype(np.float64), c.expected()
+        n = min(max_q, 40)
+        assert (np.abs(got[:n] - want[:n]) <= tol[:n]).all()
+        n = min(max_q, 20)
+        assert (np.abs(got[40:40 + n] - want[40:40 + n]) <= tol[40:40 + n]).all()
