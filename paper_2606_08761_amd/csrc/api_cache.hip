@@ -64,7 +64,7 @@ int check_view_pointers(const KvView& c) {
 
 // A row of `heads` heads every `stride` elements.
 int check_rows(int64_t T, int64_t heads, int64_t D, int64_t stride) {
-    if (T < 0 || T * heads > 0x7FFFFFFFll / 16) return APEX4_ERR_SHAPE;
+    if (T < 0 || T > kMaxCount || T * heads > 0x7FFFFFFFll / 16) return APEX4_ERR_SHAPE;  // heads <= 65536: no wrap
     if (stride < heads * D || stride % 8 != 0 || stride > (1ll << 40)) return APEX4_ERR_SHAPE;
     return APEX4_OK;
 }
@@ -72,7 +72,7 @@ int check_rows(int64_t T, int64_t heads, int64_t D, int64_t stride) {
 int make_attn(AttnArgs& a, const KvView& c, const void* q, int64_t q_stride, const int32_t* q_start, int64_t T,
               int64_t max_q, int64_t heads, int64_t window, int64_t sinks, float scale, void* out) {
     if (heads < 1 || heads > 65536 || heads % c.kv_heads != 0) return APEX4_ERR_SHAPE;
-    if (T < 0 || T > kMaxCount || max_q < 0 || max_q > kMaxCount) return APEX4_ERR_SHAPE;
+    if (max_q < 0 || max_q > kMaxCount) return APEX4_ERR_SHAPE;
     const int rc = check_rows(T, heads, c.D, q_stride);
     if (rc) return rc;
     if (window < 0 || sinks < 0 || !(scale > 0.f) || scale > 3.4e38f) return APEX4_ERR_SHAPE;
