@@ -14,7 +14,7 @@ using apex4::AttnArgs;
 using apex4::KvView;
 using apex4::PageTable;
 
-constexpr int64_t kMaxPages = 1ll << 30, kMaxWidth = 1ll << 20, kMaxLen = 1ll << 30, kMaxCount = 1ll << 24;
+constexpr int64_t kMaxPages = 1ll << 30, kMaxWidth = 1ll << 20, kMaxLen = 1ll << 30, kMaxCount = 1ll << 24, kMaxRows = 1ll << 27;
 constexpr int64_t kMaxPageBytes = 1ll << 30;  // offsets inside a page are 32 bits
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -64,7 +64,7 @@ int check_view_pointers(const KvView& c) {
 
 // A row of `heads` heads every `stride` elements.
 int check_rows(int64_t T, int64_t heads, int64_t D, int64_t stride) {
-    if (T < 0 || T > kMaxCount || T * heads > 0x7FFFFFFFll / 16) return APEX4_ERR_SHAPE;  // heads <= 65536: no wrap
+    if (T < 0 || T > kMaxCount || T * heads > kMaxRows) return APEX4_ERR_SHAPE;  // heads <= 65536: no wrap
     if (stride < heads * D || stride % 8 != 0 || stride > (1ll << 40)) return APEX4_ERR_SHAPE;
     return APEX4_OK;
 }
