@@ -209,7 +209,8 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(int32_t* __restrict__ ta
         if (i < n) dst[i] = one ? need + before : -1;
         need += all;
     }
-    const int found = need > n_pages ? 0 : list_free(refs, n_pages, live0, before_of, free_list, need);
+    // (the list has room for as many as there are pages; all free ones are counted then)
+    const int found = list_free(refs, n_pages, live0, before_of, free_list, min(need, n_pages));
     const bool enough = found >= need;
     if (threadIdx.x == 0) *status = enough ? 0 : need - found;
     __syncthreads();  // the lists are written, and no count changes before they are

@@ -80,3 +80,16 @@ def test_lengths_up_to_the_tables_end_are_seen(pk, kind):
     assert torch.equal(c.prefill(0, q, b, start, n), pk.apex4_attn_prefill(q, start, *args, max_q=n, cache=kind))
     assert torch.equal(c.prefill(0, q[-2:], b, torch.tensor([0, 2], dtype=torch.int32, device="cuda"), 2),
                        pk.apex4_attn_prefill(q[-2:], torch.tensor([0, 2], dtype=torch.int32, device="cuda"), *args, max_q=2, cache=kind))
+
+
+@pytest.mark.parametrize("pages,children", [(4, 6), (4, 3), (4, 4), (3, 2000)])
+def test_fork_counts_the_pages_that_are_missing(pk, pages, children):
+    """Also where the children outnumber the pool's pages."""
+    import torch
+    c = pk.PagedKVCache(layers=1, pages=pages, slots=children + 1, kv_heads=1, head_dim=64, page=16, max_len=64)
+    assert c.reserved(c.reserve([0], [5]))
+    before = [x.clone() for x in (c.table, c.kv_len, c.refs)]
+    missing = max(0, children - (pages - 1))
+    assert int(c.fork([0] * children, list(range(1, children + 1))).item()) == missing
+    if missing:  # nothing has changed
+        assert all(torch.equal(a, b) for a, b in zip(before, (c.table, c.kv_len, c.refs)))
