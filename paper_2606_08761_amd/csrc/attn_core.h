@@ -47,6 +47,16 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     return __builtin_bit_cast(uint32_t, r);
 }
 
+// Workgroups of a launch: HIP takes less than 2^32 threads along a grid's first
+// dimension, so more than 2^22 workgroups (of up to 512 threads) take two.  What is past the
+// last one has to return.
+inline dim3 grid_of(int64_t blocks) {
+    constexpr int64_t kRow = 1 << 22;
+    return blocks <= kRow ? dim3(static_cast<unsigned>(blocks))
+                          : dim3(static_cast<unsigned>(kRow), static_cast<unsigned>((blocks + kRow - 1) / kRow));
+}
+__device__ __forceinline__ uint32_t workgroup_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 // New tokens of sequence b of the packed ones: those of rows q_start[b] .. that are
 // among the T, none where the start is not.  (So that no row number overflows.)
 __device__ __forceinline__ int new_tokens(const AttnArgs& a, int b) {

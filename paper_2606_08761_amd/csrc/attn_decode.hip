@@ -69,14 +69,15 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
     // Workgroups go to the 8 XCDs in turn.  Every group of 8 is rotated by its
     // number, so that no XCD gets the same heads or ranges of every sequence, which
     // differ in length; the later ranges, missing from short sequences, come last.
-    uint32_t id = blockIdx.x;
-    if ((id | 7) < gridDim.x) id = (id & ~7u) | ((id + (id >> 3)) & 7u);
+    uint32_t id = workgroup_number();
+    if ((id | 7) < gridDim.x * gridDim.y) id = (id & ~7u) | ((id + (id >> 3)) & 7u);
     const int h = static_cast<int>(id % c.kv_heads);
     id /= c.kv_heads;
     const int rt = static_cast<int>(id % row_tiles);
     id /= row_tiles;
     const int b = static_cast<int>(id % c.B);
     const int split = static_cast<int>(id / c.B);
+    if (split >= S) return;
     const uint32_t group = a.group;
     // the sequence's rows of this key head: its new tokens times the heads that share it
     const int q0 = a.q_start ? a.q_start[b] : b;
@@ -453,17 +454,19 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
 // slices of the parts, added in a fixed order.  With many parts a row's columns
 // go to several workgroups (64 rows of 256 parts: 13.9 -> 5 us).
 template <int D, int C>
-__global__ __launch_bounds__(256) void attn_join_kernel(const float* __restrict__ part, const float* __restrict__ ml, int S,
-                                                        uint16_t* __restrict__ out) {
+__global__ __launch_bounds__(256) void attn_join_kernel(const float* __restrict__ part, const float* __restrict__ ml,
+                                                        int64_t rows, int S, uint16_t* __restrict__ out) {
     constexpr int N = 256 / C, kFactors = 1024;
     __shared__ float top_of[4];
     __shared__ int last_of[4];
     __shared__ float factor[kFactors];
     __shared__ float sum_of[4];
     __shared__ __align__(16) f32x4 sums[N][C];
-    const int64_t row = blockIdx.x / (D / 4 / C);
+    const uint32_t id = workgroup_number();
+    const int64_t row = id / (D / 4 / C);
+    if (row >= rows) return;
     const int tid = threadIdx.x, wave = tid >> 6;
-    const int col = static_cast<int>(blockIdx.x % (D / 4 / C)) * C + tid % C, slice = tid / C;
+    const int col = static_cast<int>(id % (D / 4 / C)) * C + tid % C, slice = tid / C;
     const float* mlr = ml + row * S * 2;
     const float* p = part + row * S * D + 4 * col;
     float top = kNoMax;
@@ -530,7 +533,7 @@ template <int D>
 __global__ __launch_bounds__(256) void attn_join_few_kernel(const float* __restrict__ part, const float* __restrict__ ml,
                                                             int64_t rows, int S, uint16_t* __restrict__ out) {
     constexpr int C = D / 4;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / C) + threadIdx.x / C;
+    const int64_t row = static_cast<int64_t>(workgroup_number()) * (256 / C) + threadIdx.x / C;
     const int col = threadIdx.x % C;
     if (row >= rows) return;
     const float* mlr = ml + row * S * 2;
@@ -606,15 +609,15 @@ hipError_t launch_attn_join(const float* part, const float* ml, int64_t rows, in
                             hipStream_t stream) {
     if (S <= kFewParts && rows >= 8 * device_cu_count()) {
         const int64_t n = 1024 / D;  // rows of a workgroup
-        const unsigned blocks = static_cast<unsigned>((rows + n - 1) / n);
-        if (D == 128) attn_join_few_kernel<128><<<blocks, 256, 0, stream>>>(part, ml, rows, S, out);
-        else attn_join_few_kernel<64><<<blocks, 256, 0, stream>>>(part, ml, rows, S, out);
+        const dim3 grid = grid_of((rows + n - 1) / n);
+        if (D == 128) attn_join_few_kernel<128><<<grid, 256, 0, stream>>>(part, ml, rows, S, out);
+        else attn_join_few_kernel<64><<<grid, 256, 0, stream>>>(part, ml, rows, S, out);
         return hipGetLastError();
     }
     // 32 parts or more, and rows too few to fill the compute units twice
     const bool wide = S >= 32 && rows < 2 * device_cu_count();
     auto run = [&](auto kernel, int per_row) {
-        kernel<<<static_cast<unsigned>(rows * per_row), 256, 0, stream>>>(part, ml, S, out);
+        kernel<<<grid_of(rows * per_row), 256, 0, stream>>>(part, ml, rows, S, out);
     };
     if (D == 128) wide ? run(attn_join_kernel<128, 8>, 4) : run(attn_join_kernel<128, 32>, 1);
     else wide ? run(attn_join_kernel<64, 8>, 2) : run(attn_join_kernel<64, 16>, 1);
@@ -626,7 +629,7 @@ hipError_t launch_attn_decode(const KvView& c, const AttnArgs& a, hipStream_t st
     float* part = static_cast<float*>(a.workspace);
     float* ml = part + a.T * a.heads * p.S * c.D;
     auto run = [&](auto kernel) {
-        kernel<<<static_cast<unsigned>(blocks_of(c, p)), 64 * p.waves, 0, stream>>>(c, a, p.S, p.range, p.row_tiles, part, ml);
+        kernel<<<grid_of(blocks_of(c, p)), 64 * p.waves, 0, stream>>>(c, a, p.S, p.range, p.row_tiles, part, ml);
     };
     auto pick = [&](auto few, auto many) { p.waves == 8 ? run(few) : run(many); };
     if (c.D == 128) {

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     Smem<D, I4, kWaves>& sm = *reinterpret_cast<Smem<D, I4, kWaves>*>(smem_raw);
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r32 = lane & 31, half = lane >> 5;
-    uint32_t id = blockIdx.x;
+    uint32_t id = workgroup_number();
     const int h = static_cast<int>(id % c.kv_heads);  // workgroups of one key head on one XCD's L2 where the heads allow it
     id /= c.kv_heads;
     const int split = static_cast<int>(id % S);
@@ -121,6 +121,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
     // rows, which see the most: what starts late is short.  (In the order given, six
     // ragged chunks took 137 us instead of 96.)
     int b = static_cast<int>(id / row_tiles);
+    if (b >= c.B) return;
     const int from_last = static_cast<int>(id) - b * row_tiles;
     int q0, n, len;
     {
@@ -681,7 +682,7 @@ hipError_t run(const KvView& c, const AttnArgs& a, const Plan& p, float* part, f
     constexpr int lds = sizeof(Smem<D, I4, kWaves>);
     const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(attn_prefill_kernel<D, I4, kWaves>), lds, done);
     if (e != hipSuccess) return e;
-    attn_prefill_kernel<D, I4, kWaves><<<static_cast<unsigned>(blocks_of(c, p)), 64 * kWaves, lds, stream>>>(c, a, p.S, p.row_tiles, part, ml);
+    attn_prefill_kernel<D, I4, kWaves><<<grid_of(blocks_of(c, p)), 64 * kWaves, lds, stream>>>(c, a, p.S, p.row_tiles, part, ml);
     return hipGetLastError();
 }
 

@@ -163,3 +163,43 @@ def test_starts_out_of_range_are_no_rows(pk, cache, D, Hq, max_q):
         assert (np.abs(got[:n] - want[:n]) <= tol[:n]).all()
         n = min(max_q, 20)
         assert (np.abs(got[40:40 + n] - want[40:40 + n]) <= tol[40:40 + n]).all()
+
+
+def one_page_each(B, Hq, H, D, page, seed):
+    """B sequences of up to a page: device tensors, and (out, tolerance) in 64 bits."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    planes = [torch.randn((B, H * page * D), device="cuda", generator=g).to(torch.float16).view(torch.uint8) for _ in range(2)]
+    q = torch.randn((B, Hq, D), device="cuda", generator=g).to(torch.float16)
+    ids = torch.randperm(B, device="cuda", generator=g).to(torch.int32)
+    lens = torch.randint(1, 17, (B,), device="cuda", generator=g).to(torch.int32)
+    k, v = (p.view(torch.float16).view(B, H, page, D)[ids.long(), :, :16].double().cpu().numpy() for p in planes)
+    x = np.matmul(q.double().cpu().numpy().reshape(B, H, Hq // H, D), k.swapaxes(2, 3)) / np.sqrt(D)
+    seen = np.arange(16) < lens.cpu().numpy()[:, None]
+    x = np.where(seen[:, None, None], x, -np.inf)
+    w = np.exp(x - x.max(axis=-1, keepdims=True))
+    w /= w.sum(axis=-1, keepdims=True)
+    out, mean = (np.matmul(w, a).reshape(B, Hq, D) for a in (v, np.abs(v)))
+    # as in paged.tolerance, with at most 16 tokens of values under 8
+    return q, planes, ids, lens, out, 2.0 ** -10 * mean + 2.0 ** -11 * np.abs(out) + 16 * 2.0 ** -24 * 8 + 2.0 ** -24
+
+
+def test_more_workgroups_than_one_dimension_of_a_grid_holds(pk):
+    """8192 sequences and max_q no better known than as all tokens: 2^24 workgroups
+    of 256 threads, nearly all without rows."""
+    import torch
+    q, planes, ids, lens, out, tol = one_page_each(8192, 32, 2, 64, 16, 7)
+    start = torch.arange(8193, device="cuda", dtype=torch.int32)
+    y = pk.apex4_attn_prefill(q, start, *planes, ids[:, None].contiguous(), lens, 2, 16)
+    assert (np.abs(y.cpu().numpy().astype(np.float64) - out) <= tol).all()
+
+
+def test_more_parts_than_one_dimension_of_a_grid_holds(pk):
+    """As many workgroups for single tokens, whose tables could hold 2^18 positions."""
+    import torch
+    B, H, width = 8192, 8, 256
+    q, planes, ids, lens, out, tol = one_page_each(B, H, H, 64, 1024, 11)
+    table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+    table[:, 0] = ids
+    y = pk.apex4_attn_decode(q, *planes, table, lens, H, 1024)
+    assert (np.abs(y.cpu().numpy().astype(np.float64) - out) <= tol).all()
