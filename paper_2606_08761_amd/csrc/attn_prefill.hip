@@ -76,14 +76,19 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
 
 // 16 bytes a lane from base + off straight into LDS at `to` + 16 lane.  The
 // compiler does not see these loads: landed() waits for all of them.  (The wait
-// states let M0, and a base that came out of a vector instruction, settle.)
+// states let M0, and a base that came out of a vector instruction, settle.)  M0 is
+// among the clobbers, so that no setting of the compiler's own is taken to outlive the
+// statement; it warns that it reserves the register, and so has none to save.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy_to_lds(uint32_t to, uint32_t off, const uint8_t* base) {
     const uint64_t at = reinterpret_cast<uint64_t>(base);
     const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off),
                  "s"(static_cast<uint64_t>(hi) << 32 | lo)
-                 : "memory");
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // 4 positions' value d for the lane's d: lanes 4 j + i of 16 point at 4 values
