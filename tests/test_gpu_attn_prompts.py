@@ -203,3 +203,77 @@ def test_more_parts_than_one_dimension_of_a_grid_holds(pk):
     table[:, 0] = ids
     y = pk.apex4_attn_decode(q, *planes, table, lens, H, 1024)
     assert (np.abs(y.cpu().numpy().astype(np.float64) - out) <= tol).all()
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("zeros", ["all", "values", "keys", "first", "last"])
+def test_zero_tokens_in_prompts(pk, cache, D, zeros):
+    """Keys or values of nothing but zeros (scales of zero), everywhere or beside
+    ordinary ones; scores far above those of the tokens with values."""
+    n = 300
+    c = paged.Case(131, [n], [24], 4, 1, D, 16, cache, spoil=False)
+    c.q *= np.float16(8)  # scores of some tens
+    zero = np.zeros((1, D))
+    for t in range(n):
+        some = zeros in ("all", "values") or (zeros == "first" and t < 100) or (zeros == "last" and t >= 250)
+        rewrite(c, 0, t, k=zero if zeros in ("all", "keys") else None, v=zero if some else None)
+    check(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("slope", [0.4, -0.4])
+def test_growing_scores_in_prompts(pk, cache, slope):
+    """Scores that rise along the sequence, so that the running maximum is raised
+    again and again, or fall, so that weights vanish."""
+    c = paged.Case(137, [700], [24], 4, 1, 64, 16, cache, spoil=False)
+    c.q[:] = 1.0
+    for t in range(700):
+        rewrite(c, 0, t, k=np.full((1, 64), slope * (t - 350) / 8.0))
+    check(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D,page,window,sinks", [(128, 64, 0, 0), (64, 16, 0, 0), (64, 16, 3000, 5), (128, 32, 1500, 70)])
+def test_prompts_cut_along_the_positions(pk, cache, D, page, window, sinks):
+    """Few tiles of rows and a long cache: parts, joined; with a window, parts that
+    some of the rows do not reach."""
+    c = paged.Case(139, [4100, 900], [20, 12], 8, 1, D, page, cache, window=window, sinks=sinks)
+    assert pk.apex4_attn_prefill_workspace_size(c.T, 2, 20, c.width, c.width * page, 8, 1, D, page, window, sinks) > 0
+    check(prefill(pk, c), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+def test_prompts_on_pages_past_32_bits(pk, cache):
+    """Pages past 4 GiB of a plane."""
+    import torch
+    c = paged.Case(149, [100, 40], [20, 17], 32, 8, 128, 16, cache)
+    size, used = c.k.raw.shape[1], c.k.raw.shape[0]
+    pages = (5 << 30) // size
+    planes = []
+    for raw in (c.k.raw, c.v.raw):
+        p = torch.zeros((pages, size), dtype=torch.uint8, device="cuda")
+        p[pages - used:] = dev(raw)
+        planes.append(p)
+    table = dev(np.where(c.table >= 0, c.table + pages - used, c.table).astype(np.int32))
+    check(pk.apex4_attn_prefill(dev(c.q), dev(c.start), *planes, table, dev(np.array(c.lens, np.int32)), 8, 16, max_q=20,
+                                cache=cache), c)
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("page", [16, 64])
+def test_prompts_beside_ids_and_lengths_out_of_range(pk, cache, page):
+    """Page ids outside the pool and lengths past the table are never addresses:
+    the sequences beside them are right."""
+    c = paged.Case(151, [200, 90, 140], [30, 25, 40], 8, 2, 64, page, cache)
+    t = c.table.copy()
+    t[1] = -1
+    t[1, :2] = [1 << 30, -5]
+    t[1, -1] = c.k.raw.shape[0]
+    y = pk.apex4_attn_prefill(dev(c.q), dev(c.start), dev(c.k.raw), dev(c.v.raw), dev(t), dev(np.array([200, 1 << 29, 140], np.int32)),
+                              2, page, max_q=40, cache=cache)
+    got = y.cpu().numpy().astype(np.float64)
+    want, tol = c.expected()
+    for b in (0, 2):
+        rows = slice(c.start[b], c.start[b + 1])
+        assert (np.abs(got[rows] - want[rows]) <= tol[rows]).all()

@@ -1,7 +1,6 @@
 """PagedKVCache and the page calls where a call's bounds meet: lengths past max_len
 that the table still holds, more pages asked for than there are, lists on other
 streams."""
-import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
