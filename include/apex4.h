@@ -460,8 +460,10 @@ int apex4_kv_gather(const void* k_pages, const void* v_pages, int64_t n_pages, c
  * with window > 0, t > p - window or t < sinks (a sliding window, and first
  * tokens that stay visible).  A sequence without tokens gets zeros.  Positions
  * that are not seen may hold anything, NaN included.  Scores, weights' sums and
- * output sums are binary32; the weights are rounded to binary16 (the products'
- * operand), the result once.  scale: positive and finite.  Scores scale q.k are taken
+ * output sums are binary32.  The weights (times the values' scales, of codes) are the
+ * products' operand in binary16: over a binary16 cache as a sum of two, which leaves
+ * the result its own rounding, over codes as one.  The result is rounded once.
+ * scale: positive and finite.  Scores scale q.k are taken
  * up to a magnitude of 2^26 (a weight's exponent is one binary32 fma, whose error
  * grows with the score's magnitude, and must stay within the weights' range).
  *   max_len: a bound of kv_len known on the host (shorter: less to launch);
@@ -483,6 +485,7 @@ int apex4_attn_decode(const void* q, int64_t q_stride, const void* k_pages, cons
  * tokens at a time), each at its own position p: q, out [T, heads, head_dim].
  *   max_q: a bound of the new tokens of a sequence; the outputs of those past it,
  *   and of tokens of no sequence, are left undefined.
+ *   The weights are one binary16 operand over either cache.
  *   A token whose position is negative (more new tokens than kv_len) sees nothing
  *   and gets zeros.  A value that is infinite or NaN reaches every new token of
  *   its sequence for which its position lies in a tile with seen ones, also
@@ -507,15 +510,18 @@ int apex4_attn_prefill(const void* q, int64_t q_stride, const int32_t* q_start, 
  * status (int32) receives the outcome on the device.  workspace:
  * apex4_pages_workspace_size(n_pages, n) bytes.
  *
+ * A slot's kv_len is what was reserved for it, written or not; no call shortens it.
+ *
  * reserve: gives slot seqs[i] the pages for new_len[i] tokens, in the order of
  *   the list, and sets its kv_len (a smaller new_len changes nothing).  All or
  *   nothing: status 0, or > 0 where free pages are too few, or -1 where a length
  *   does not fit the table.
  * fork: slot children[i] (empty) continues parents[i] (and is not a parent in
  *   the same call): it shares the full pages, and gets a page of its own, with the
- *   data copied, for the tokens of a partly filled last one, so that appending
- *   never writes to a shared page.  All or nothing: status 0, or the number of
- *   missing pages.
+ *   data copied, for the tokens of a partly filled last one, so that appending past
+ *   kv_len never writes to a shared page.  Tokens below it are shared: a parent that
+ *   reserved ahead is forked once those are written, or parent and child both write
+ *   them to the same pages.  All or nothing: status 0, or the number of missing pages.
  * free: gives back the slots' pages and empties them.
  * compact: moves pages so that the live ones are 0 .. live - 1 (those past that
  *   number, in ascending order, to the free ones below it) and updates table and

@@ -279,7 +279,7 @@ def _same_length(a, b, names):
 
 def apex4_pages_reserve(table, kv_len, refs, seqs, new_len, page: int, status=None, workspace=None, stream=None):
     """Pages for new_len tokens of each of the slots seqs (all or nothing), and
-    their kv_len.  Returns status, int32 [1] on the device: 0, > 0 where free
+    their kv_len, which counts them whether they are written or not.  Returns status, int32 [1] on the device: 0, > 0 where free
     pages are too few, -1 where a length does not fit the table."""
     args = _state(table, kv_len, refs)
     n = _same_length(seqs, new_len, "seqs and new_len")
@@ -293,7 +293,8 @@ def apex4_pages_reserve(table, kv_len, refs, seqs, new_len, page: int, status=No
 
 def apex4_pages_fork(pool, table, kv_len, refs, parents, children, page: int, status=None, workspace=None, stream=None):
     """The (empty) slots children continue parents: full pages shared, a partly
-    filled last one copied.  Returns status, int32 [1]: 0, or the pages missing
+    filled last one copied.  All of a parent's kv_len is taken as written: tokens that
+    it only reserved would be written to shared pages by both.  Returns status, int32 [1]: 0, or the pages missing
     (then nothing has changed)."""
     args = _state(table, kv_len, refs)
     pp, planes, size = _pool(pool, refs)

@@ -29,13 +29,15 @@
 // Bound by the matrix cores and, next to them, the vector units: a tile's 32 products
 // take a wave 1024 cycles of its SIMD's matrix core, its exponentials (16 cycles each),
 // their arguments, maxima and sums about 830 of the vector unit.  A prompt of 8192
-// tokens, 64 query heads of 128: 1.06 to 1.10 ms, 1000 to 1040 TFLOP/s of the 1343 that
+// tokens, 64 query heads of 128: 1.04 to 1.10 ms, 1000 to 1055 TFLOP/s of the 1343 that
 // a product of 8192^3 reaches, at a clock that falls with the load (queries of zero,
 // which cost less power: 0.85 ms).  No faster: three and four buffers, two halves of the
 // waves half a step apart, 64 rows a wave, fragments read further ahead, wave
-// priorities.  Codes: 14 % more a tile, for putting them into LDS and for the scales
-// (2048 tokens of 2 sequences under a window of 1024: 206 to 217 us); multiplications
-// left out to see, and the conversion elsewhere in the step changed nothing.
+// priorities.  Codes: some 16 % more a tile, for putting them into LDS and for the scales
+// (the prompt 1.24 ms; 2048 new tokens of 2 sequences of 8192 under a window of 1024: 207
+// us, binary16 178); multiplications left out to see, and the conversion elsewhere in
+// the step changed nothing.  Heads of 64: the prompt 0.61 ms, codes 0.97; the window 99
+// and 160 us.
 #include "attn_core.h"
 
 namespace apex4 {
@@ -642,9 +644,10 @@ struct Plan {
 };
 
 // Eight waves (256 rows, half the staging a row) where that leaves four workgroups a
-// compute unit of 12 tiles or more, and always for codes (8192 tokens 1154 -> 1111 us, a
-// window of 1024 179 -> 175); four otherwise: two workgroups a unit hide each other's
-// beginnings and even out the last round (4 x 1024 tokens, two a unit: 63 us, 68).  The
+// compute unit of 12 tiles or more, and always for codes (64 query heads of 128 over 8
+// key heads: 8192 tokens 1082 -> 1044 us, 2 x 2048 tokens of 8192 under a window of 1024
+// 183 -> 177); four otherwise: two workgroups a unit hide each other's beginnings and
+// even out the last round (4 x 1024 tokens, two a unit: 63 us, 68).  The
 // tiles are split where the workgroups number fewer than the compute units, into
 // parts of at least four tiles, as many as the units hold at once and no more (32
 // rows of 7954 positions: 4 parts 94 us, 5 parts 120).
@@ -671,10 +674,19 @@ Plan plan_prefill(const KvView& c, const AttnArgs& a) {
 }
 
 // Rows (new tokens times the heads that share a key head) up to which the decode
-// kernel, 16 at a time, is the faster one.  14 sequences of 7954 with 8 key heads of
-// 128: binary16 16 rows 92 us against 119, 32 rows 137 against 119 (it reads the
-// cache twice); int4 32 rows 56 against 130, 64 rows 89 against 138 (the codes are
-// made binary16 in LDS by a workgroup whose products are few).
+// kernel, 16 at a time, is the faster one.  It reads the cache once for every 16 rows
+// (from the L2 after the first), this one once, but this one makes codes binary16 in
+// LDS by a workgroup whose products are few.  The decode kernel's time against this
+// one's in us, 14 sequences of 7954 | 14 of 600 | 64 of 600; 8 key heads, 64 query heads
+// unless 32 of each are said:
+//   binary16, D = 128, 16 rows   94, 96 | 12, 17 | 27, 32     32 of each 360, 344 | 24, 28 | 121, 137
+//                      32 rows  141, 97 | 15, 17 | 49, 33                523, 344 | 45, 28 | 186, 143
+//             D = 64,  16 rows   42, 43 |  8, 14 | 17, 20                187, 158 | 15, 17 |  56,  71
+//                      32 rows   76, 45 |  9, 13 | 27, 21                268, 158 | 25, 18 |  94,  74
+//   int4,     D = 128, 64 rows   82, 109 | 13, 19 | 36, 50               291, 394 | 30, 46 | 113, 189
+//                     128 rows  154, 115 | 21, 25 | 62, 54               526, 407 | 53, 49 | 221, 212
+//             D = 64,  64 rows   53, 99  |  9, 18 | 24, 44               186, 356 | 22, 39 |  79, 169
+//                     128 rows   94, 101 | 14, 22 | 42, 46               345, 356 | 38, 42 | 154, 174
 bool few_rows(const KvView& c, const AttnArgs& a) { return a.max_q * (a.heads / c.kv_heads) <= (c.i4 ? 64 : 16); }
 
 int64_t blocks_of(const KvView& c, const Plan& p) {

@@ -8,9 +8,10 @@
 // sequence is a search in q_start): that chain of loads, not the bytes, bounds a
 // workgroup of few tokens, and long prompts take 8 tokens a workgroup.
 //
-// Measured, 8 heads of 128: 16 tokens 2.7 us either way (a launch and that chain);
-// ragged prompts, 8958 tokens, into an int4 cache 14.6 us (37 MB read, 10 written: 3.2
-// TB/s, bound by the conversion and the chain), back 12.6 us (3.7 TB/s).
+// Measured, 8 heads of 128: 16 tokens 2.8 us either way (a launch and that chain);
+// ragged prompts, 8958 tokens, into an int4 cache 14.4 us (37 MB read, 10 written: 3.2
+// TB/s, with the vector units 0.42 busy: neither is full, the chain comes before the
+// bytes), back 12.8 us (3.8 TB/s); binary16 there and back 30.4 us (4.8 TB/s).
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
