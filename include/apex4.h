@@ -485,7 +485,9 @@ int apex4_attn_decode(const void* q, int64_t q_stride, const void* k_pages, cons
  * tokens at a time), each at its own position p: q, out [T, heads, head_dim].
  *   max_q: a bound of the new tokens of a sequence; the outputs of those past it,
  *   and of tokens of no sequence, are left undefined.
- *   The weights are one binary16 operand over either cache.
+ *   The weights are one binary16 operand over either cache.  A token's output does
+ *   not depend on the values of later tokens, bit for bit, but for infinite and NaN
+ *   ones (below).
  *   A token whose position is negative (more new tokens than kv_len) sees nothing
  *   and gets zeros.  A value that is infinite or NaN reaches every new token of
  *   its sequence for which its position lies in a tile with seen ones, also

@@ -25,14 +25,16 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // A running maximum that no finite score is below, and that leaves 2^(s - m)
 // zero, not NaN, where every score so far is masked (s = -inf).
 constexpr float kNoMax = -1e30f;
-// Scores may pass the running maximum by this much (in units of log2) before
-// the sums are rescaled: after the first tiles a rescale is rare.  The weights of
-// decoding stay below 2^8.  Those of prefill, whose sums run over a whole length, are
-// scaled by 2^kHeadroom and stay below 2^15: binary16 then holds them to 2^-32 of the
-// largest one, and a long tail of small weights, rounded the same way each, keeps its
-// share (without it 40000 of 2^-25 vanished: 1.2e-3 of the result).
-constexpr float kSlack = 8.f;
-constexpr float kHeadroom = 7.f;
+// The weights of prefill, whose sums run over a whole length, are scaled by 2^kHeadroom
+// when the running maximum is raised, and it is raised again where one passes it by kSlack
+// more (in units of log2), just inside binary16's range: after the first tiles a rescale is
+// rare (a slack of 8 takes 5 % more time under a window over codes).  Binary16 holds
+// the weights to 2^-31 of the largest one, so that a long tail of small weights, rounded
+// the same way each, keeps its share (without the headroom 40000 of 2^-25 vanished:
+// 1.2e-3 of the result).
+constexpr float kHeadroom = 6.f;
+constexpr float kSlack = 9.875f;
+// Decoding, at most 512 positions a wave: weights below 2^8.
 constexpr float kMostWeight = 256.f;
 constexpr float kMostSum = 0x1p60f;
 

@@ -282,7 +282,8 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
             top = fmaxf(top, w[j]);
             if constexpr (I4) sum_top = fmaxf(sum_top, e[j]);  // a scale of zero leaves the sum alone to grow
         }
-        if (__any(top > kMostWeight || (I4 && sum_top > kMostSum))) {
+        // (only of the rows that need it: what a row gives does not depend on the others)
+        if (const uint64_t over = __ballot(top > kMostWeight || (I4 && sum_top > kMostSum))) {
             top = kNoMax;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 4 ? 3 : 2) void attn_decode_
             }
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            top = fmaxf(top, m);
+            top = (over >> r16 & 0x0001000100010001ull) ? fmaxf(top, m) : m;
             const float f = exp2_fast(m - top);
             l *= f;
             m = top;

@@ -464,9 +464,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
                 // the slack, their maximum for each row.  The bound is none: its scale may
                 // be that of a position without weight, or of one that the row does not
                 // see, and under it the row's weights would fall below what binary16
-                // holds.  (The windowed case above 200 -> 206 us; in the same branch as
-                // the rescale 218, for the compiler then copies the output sums every tile;
-                // with the logarithms taken here 210.)
+                // holds.  (The windowed case above 203 -> 207 us; in the same branch as
+                // the rescale 12 more, for the compiler then copies the output sums every
+                // tile; with the logarithms taken here 4 more.)
                 most_vl = __builtin_amdgcn_logf(__builtin_bit_cast(float, sm.vs_most[t & 3]));
                 rise = (top - m) + most_vl;
                 if (__any(rise > kHeadroom + kSlack)) {
@@ -483,9 +483,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_prefill_kernel(KvView c, 
             } else {
                 rise = fmaf(top, f_log2, -m);
             }
-            if (__any(rise > kHeadroom + kSlack)) {
+            // Only the rows that need it are raised: what a row gives does not depend on
+            // what others of its wave see.
+            if (const uint64_t over = __ballot(rise > kHeadroom + kSlack)) {
                 top = I4 ? top + (most_vl - kHeadroom) : fmaf(top, f_log2, -kHeadroom);
                 top = fmaxf(fmaxf(top, __shfl_xor(top, 32, 64)), m);
+                top = (over >> (anew(tid) & 31) & 0x100000001ull) ? top : m;
                 const float f = exp2_fast(m - top);
                 l *= f;
                 m = top;

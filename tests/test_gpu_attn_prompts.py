@@ -277,3 +277,23 @@ def test_prompts_beside_ids_and_lengths_out_of_range(pk, cache, page):
     for b in (0, 2):
         rows = slice(c.start[b], c.start[b + 1])
         assert (np.abs(got[rows] - want[rows]) <= tol[rows]).all()
+
+
+@pytest.mark.parametrize("cache", ["fp16", "int4"])
+@pytest.mark.parametrize("D,Hq,lens,news,at", [
+    (64, 4, [150, 90], [150, 40], 100), (128, 4, [150, 90], [150, 40], 100),  # many rows
+    (64, 4, [150, 90], [4, 3], 148), (128, 4, [150, 90], [4, 3], 148),        # few
+    (64, 4, [700, 90], [4, 3], 698), (128, 4, [700, 90], [4, 3], 698),
+])
+def test_later_tokens_leave_earlier_rows_their_bits(pk, cache, D, Hq, lens, news, at):
+    """Also a token that raises the running maximum of the rows that see it."""
+    import torch
+    c = paged.Case(167, lens, news, Hq, 2, D, 16, cache, spoil=False)
+    a = prefill(pk, c)
+    first = at - (lens[0] - news[0])  # the first new token that sees it
+    for k, v in ((40.0, 3.0), (-40.0, 500.0)):
+        rewrite(c, 0, at, k=c.K[0][at] * k, v=c.V[0][at] * v)
+        b = prefill(pk, c)
+        assert torch.equal(a[:first], b[:first]) and torch.equal(a[news[0]:], b[news[0]:])
+        assert not torch.equal(a[first:news[0]], b[first:news[0]])
+    check(b, c)
