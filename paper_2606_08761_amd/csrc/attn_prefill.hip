@@ -34,8 +34,8 @@
 // which cost less power: 0.85 ms).  No faster: three and four buffers, two halves of the
 // waves half a step apart, 64 rows a wave, fragments read further ahead, wave
 // priorities.  Codes: some 16 % more a tile, for putting them into LDS and for the scales
-// (the prompt 1.24 ms; 2048 new tokens of 2 sequences of 8192 under a window of 1024: 207
-// us, binary16 178); multiplications left out to see, and the conversion elsewhere in
+// (the prompt 1.24 to 1.26 ms; 2048 new tokens of 2 sequences of 8192 under a window of 1024: 207
+// us, binary16 177); multiplications left out to see, and the conversion elsewhere in
 // the step changed nothing.  Heads of 64: the prompt 0.61 ms, codes 0.97; the window 99
 // and 160 us.
 #include "attn_core.h"
