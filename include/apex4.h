@@ -441,6 +441,45 @@ int apex4_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
                     void* stream);
 
 /*
+ * Rotary positions.  Of every head of a token at position p, the first rot values are
+ * rot / 2 pairs, and pair j turns by p freq[j] whole turns (not radians):
+ *   (a, b) -> mag (a cos - b sin, b cos + a sin).
+ * APEX4_ROPE_HALF: the pairs are (j, j + rot / 2); APEX4_ROPE_INTERLEAVED: (2 j, 2 j + 1).
+ * The values from rot on are copied.
+ *   freq [rot / 2] binary64 (device, 8-byte aligned): how contexts are stretched is in
+ *   these numbers (apex4_rope_freq of the Python binding makes them);
+ *   mag: positive and finite.
+ *   positions [T] int32 (device), any values: a negative one turns back.
+ * Angles are binary64, turned values binary32, rounded once to binary16.
+ *
+ * apex4_rope: T rows of heads * head_dim binary16, x_stride and out_stride elements
+ *   apart (multiples of 8; the heads of a fused projection's queries and keys are one
+ *   call).  out is x itself with the same stride, or overlaps it nowhere.
+ *   head_dim: a multiple of 8, 8 to 512; rot even, 2 to head_dim; heads up to 65536, T
+ *   up to 2^24, T heads up to 2^27.  Fastest where head_dim is a multiple of 16 and rot
+ *   one of 16 (half) or 8 (interleaved).
+ */
+#define APEX4_ROPE_HALF 0
+#define APEX4_ROPE_INTERLEAVED 1
+int apex4_rope(const void* x, int64_t x_stride, const int32_t* positions, int64_t T, int64_t heads, int64_t head_dim,
+               const double* freq, int64_t rot, int layout, float mag, void* out, int64_t out_stride, void* stream);
+
+/*
+ * apex4_kv_append with rotary positions on the way, in one launch: the keys are
+ * turned (and rounded to binary16) before they are stored, the values are stored as
+ * they are, and the queries are turned into q_out [T, heads, head_dim].  Cache and
+ * q_out end up as after apex4_rope of queries and keys and apex4_kv_append, bit for bit.
+ *   positions [T] int32, or NULL: each new token's own position in its sequence.
+ *   heads == 0: no queries (q and q_out may be NULL).  q_out overlaps no input.
+ * Rows of q_out behind the last sequence's are left as they were.
+ */
+int apex4_kv_append_rope(const void* q, int64_t q_stride, int64_t heads, void* q_out, const void* k, int64_t k_stride,
+                         const void* v, int64_t v_stride, const int32_t* q_start, int64_t T, const int32_t* positions,
+                         const double* freq, int64_t rot, int layout, float mag, void* k_pages, void* v_pages,
+                         int64_t n_pages, const int32_t* table, int64_t width, const int32_t* kv_len, int64_t B,
+                         int64_t kv_heads, int64_t head_dim, int64_t page, int cache, void* stream);
+
+/*
  * Reads the last n tokens of every sequence (n = q_start[b + 1] - q_start[b]) as
  * binary16 into k, v [T, kv_heads, head_dim]; from an int4 cache, code times
  * scale rounded once.

@@ -43,7 +43,8 @@ EXPORTED = ("apex4_quantize_act", "apex4_w4a4_gemm", "apex4_w4a4_gemm_groupsums"
             "apex4_w4a4_linear_tiled", "apex4_w4a4_linear_ws", "apex4_kv_page_bytes", "apex4_kv_append",
             "apex4_kv_gather", "apex4_attn_decode_workspace_size", "apex4_attn_decode",
             "apex4_attn_prefill_workspace_size", "apex4_attn_prefill", "apex4_pages_workspace_size",
-            "apex4_pages_reserve", "apex4_pages_fork", "apex4_pages_free", "apex4_pages_compact", "apex4_pages_copy")
+            "apex4_pages_reserve", "apex4_pages_fork", "apex4_pages_free", "apex4_pages_compact", "apex4_pages_copy",
+            "apex4_rope", "apex4_kv_append_rope")
 
 _lib = None
 
@@ -99,6 +100,8 @@ def lib() -> ctypes.CDLL:
     L.apex4_pages_free.argtypes = [P, I, I, P, P, I, P, I, P]
     L.apex4_pages_compact.argtypes = [P, I, I, P, I, I, P, I, P, P, I, P]
     L.apex4_pages_copy.argtypes = [P, I, I, I, P, P, I, P]
+    L.apex4_rope.argtypes = [P, I, P, I, I, I, P, I, C, F, P, I, P]
+    L.apex4_kv_append_rope.argtypes = [P, I, I, P, P, I, P, I, P, I, P, P, I, C, F, P, P, I, P, I, P, I, I, I, I, C, P]
     for f in EXPORTED:
         getattr(L, f).restype = ctypes.c_int
     L.apex4_status_string.argtypes = [ctypes.c_int]
@@ -587,7 +590,8 @@ class W4A4Linear:
         return Y
 
 
-from .cache import (KV_CACHES, PagedKVCache, apex4_attn_decode, apex4_attn_decode_workspace_size,  # noqa: E402,F401
-                    apex4_attn_prefill, apex4_attn_prefill_workspace_size, apex4_kv_append, apex4_kv_gather,
-                    apex4_kv_page_bytes, apex4_pages_compact, apex4_pages_copy, apex4_pages_fork, apex4_pages_free,
-                    apex4_pages_reserve, apex4_pages_workspace_size)
+from .cache import (KV_CACHES, ROPE_LAYOUTS, PagedKVCache, apex4_attn_decode,  # noqa: E402,F401
+                    apex4_attn_decode_workspace_size, apex4_attn_prefill, apex4_attn_prefill_workspace_size, apex4_kv_append,
+                    apex4_kv_append_rope, apex4_kv_gather, apex4_kv_page_bytes, apex4_pages_compact,
+                    apex4_pages_copy, apex4_pages_fork, apex4_pages_free, apex4_pages_reserve, apex4_pages_workspace_size)
+from .rotary import apex4_rope, apex4_rope_freq  # noqa: E402,F401

@@ -10,6 +10,7 @@ Table, lengths and sequence numbers are int32 tensors on the device.
     c.reserve(seqs, new_len)                      # pages for what comes
     b = c.batch(seqs)                             # their rows of the table, their lengths
     c.append(layer, k, v, b, q_start)             # the new tokens' keys and values
+    q = c.append_rope(layer, q, k, v, b, freq, q_start)  # or: with rotary positions, q's too
     y = c.prefill(layer, q, b, q_start, max_q)    # a prompt's attention
     y = c.decode(layer, q, b)                     # one new token a sequence
 """
@@ -22,6 +23,7 @@ import math
 from . import Apex4Error, _check, _dev, _stream, _torch, lib
 
 KV_CACHES = {"fp16": 0, "int4": 1}
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 
 
 def _kind(cache):
@@ -29,6 +31,20 @@ def _kind(cache):
         return KV_CACHES[cache]
     except KeyError:
         raise ValueError("cache must be 'fp16' or 'int4'") from None
+
+
+def _layout(layout):
+    try:
+        return ROPE_LAYOUTS[layout]
+    except KeyError:
+        raise ValueError("layout must be 'half' or 'interleaved'") from None
+
+
+def _one_device(t, *others):
+    """The tensors of a call (or None) lie on the current device, where it launches."""
+    i = t.get_device()
+    if i != _torch().cuda.current_device() or any(o is not None and o.get_device() != i for o in others):
+        raise ValueError("all tensors of a call must be on the current device")
 
 
 def _ptr(t, dtype, name):
@@ -59,6 +75,14 @@ def _rows(t, name):
     if (one != 1 and D > 1) or (head != D and H > 1):
         raise ValueError(f"the heads of {name}'s rows must be contiguous")
     return t.data_ptr(), row if T > 1 else H * D
+
+
+def _freq(freq):
+    """Pointer of freq [rot / 2], and rot."""
+    p = _ptr(freq, _torch().float64, "freq")
+    if freq.dim() != 1:
+        raise ValueError("freq must be [rot / 2]")
+    return p, 2 * freq.shape[0]
 
 
 def _planes(k_pages, v_pages, kv_heads, head_dim, page, cache):
@@ -143,6 +167,38 @@ def apex4_kv_append(k, v, k_pages, v_pages, table, kv_len, page: int, q_start=No
     rc = lib().apex4_kv_append(kp, ks, vp, vs, _starts(q_start, B), T, kpp, vpp, n, tp, width, lp, B, H, D, page,
                                _kind(cache), _stream(k, stream))
     _check("apex4_kv_append", rc)
+
+
+def apex4_kv_append_rope(q, k, v, k_pages, v_pages, table, kv_len, page: int, freq, layout: str = "half", scale: float = 1.0,
+                         q_start=None, positions=None, cache: str = "fp16", out=None, stream=None):
+    """apex4_kv_append with the keys turned by their positions (None: their places in
+    the sequences), freq and scale as apex4_rope.  q [T, heads, head_dim] (or None) is
+    turned too, into ``out`` [T, heads, head_dim] (made here when None), which is returned."""
+    torch = _torch()
+    (T, H, D) = k.shape
+    if v.shape != k.shape:
+        raise ValueError("k and v must have one shape")
+    kp, ks = _rows(k, "k")
+    vp, vs = _rows(v, "v")
+    fp, rot = _freq(freq)
+    qp, qs, heads, op = None, 0, 0, None
+    if q is not None:
+        qp, qs = _rows(q, "q")
+        if q.shape[0] != T or q.shape[2] != D:
+            raise ValueError("q must be [T, heads, head_dim], as k")
+        heads = q.shape[1]
+        out = _output(out, q.shape, q, stream)
+        op = _ptr(out, torch.float16, "out")
+    if positions is not None and tuple(positions.shape) != (T,):
+        raise ValueError("positions must be [T]")
+    kpp, vpp, n = _planes(k_pages, v_pages, H, D, page, cache)
+    tp, width, lp, B = _tables(table, kv_len)
+    _one_device(k, v, q, out, k_pages, v_pages, table, kv_len, freq, q_start, positions)
+    rc = lib().apex4_kv_append_rope(qp, qs, heads, op, kp, ks, vp, vs, _starts(q_start, B), T,
+                                    None if positions is None else _index(positions, "positions"), fp, rot, _layout(layout),
+                                    scale, kpp, vpp, n, tp, width, lp, B, H, D, page, _kind(cache), _stream(k, stream))
+    _check("apex4_kv_append_rope", rc)
+    return out
 
 
 def apex4_kv_gather(k_pages, v_pages, table, kv_len, T: int, kv_heads: int, head_dim: int, page: int, q_start=None,
@@ -401,6 +457,9 @@ class PagedKVCache:
 
     def append(self, layer, k, v, batch, q_start=None, **kw):
         apex4_kv_append(k, v, *self.planes[layer], *batch, self.page, q_start=q_start, cache=self.cache, **kw)
+
+    def append_rope(self, layer, q, k, v, batch, freq, q_start=None, **kw):
+        return apex4_kv_append_rope(q, k, v, *self.planes[layer], *batch, self.page, freq, q_start=q_start, cache=self.cache, **kw)
 
     def gather(self, layer, T, batch, q_start=None, **kw):
         return apex4_kv_gather(*self.planes[layer], *batch, T, self.kv_heads, self.head_dim, self.page, q_start=q_start,

@@ -194,6 +194,31 @@ hipError_t launch_kv_append(const KvView& c, const uint16_t* k, int64_t k_stride
 hipError_t launch_kv_gather(const KvView& c, uint16_t* k, uint16_t* v, const int32_t* q_start, int64_t T,
                             hipStream_t stream);
 
+// Rotary positions: pair j < rot / 2 of a head turns by position * freq[j] whole
+// turns, and is multiplied by mag (rope_core.h).
+struct Rotary {
+    const double* freq = nullptr;  // [rot / 2]
+    double mag = 1.0;
+    int rot = 0;
+    bool interleaved = false;
+};
+// Rows of heads * D binary16 into out (x itself, or no part of it).
+hipError_t launch_rope(const uint16_t* x, int64_t x_stride, const int32_t* positions, int64_t T, int heads, int D, const Rotary& r,
+                       uint16_t* out, int64_t out_stride, hipStream_t stream);
+// The append with the keys turned on the way, and the queries (heads > 0) into
+// rows of their own.  positions: nullptr for the places in the sequences.
+struct RopeRows {
+    const uint16_t* q = nullptr;
+    const uint16_t* k = nullptr;
+    const uint16_t* v = nullptr;
+    uint16_t* q_out = nullptr;        // [T, heads, D]
+    int64_t q_stride = 0, k_stride = 0, v_stride = 0;
+    int heads = 0;
+    const int32_t* positions = nullptr;
+};
+hipError_t launch_kv_append_rope(const KvView& c, const RopeRows& a, const int32_t* q_start, int64_t T, const Rotary& r,
+                                 hipStream_t stream);
+
 // Attention over the cache.  q rows are heads * D binary16, q_stride elements
 // apart; out is [T, heads, D].  One new token a sequence (T = B), or the packed
 // tokens of q_start, at most max_q a sequence.

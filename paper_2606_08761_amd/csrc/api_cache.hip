@@ -13,6 +13,7 @@ namespace {
 using apex4::AttnArgs;
 using apex4::KvView;
 using apex4::PageTable;
+using apex4::Rotary;
 
 constexpr int64_t kMaxPages = 1ll << 30, kMaxWidth = 1ll << 20, kMaxLen = 1ll << 30, kMaxCount = 1ll << 24, kMaxRows = 1ll << 27;
 constexpr int64_t kMaxPageBytes = 1ll << 30;  // offsets inside a page are 32 bits
@@ -66,6 +67,17 @@ int check_view_pointers(const KvView& c) {
 int check_rows(int64_t T, int64_t heads, int64_t D, int64_t stride) {
     if (T < 0 || T > kMaxCount || T * heads > kMaxRows) return APEX4_ERR_SHAPE;  // heads <= 65536: no wrap
     if (stride < heads * D || stride % 8 != 0 || stride > (1ll << 40)) return APEX4_ERR_SHAPE;
+    return APEX4_OK;
+}
+
+int make_rotary(Rotary& r, const double* freq, int64_t D, int64_t rot, int layout, float mag) {
+    if (rot < 2 || rot > D || rot % 2 != 0) return APEX4_ERR_SHAPE;
+    if (layout != APEX4_ROPE_HALF && layout != APEX4_ROPE_INTERLEAVED) return APEX4_ERR_SHAPE;
+    if (!(mag > 0.f) || mag > 3.4e38f) return APEX4_ERR_SHAPE;
+    r.freq = freq;
+    r.mag = mag;
+    r.rot = static_cast<int>(rot);
+    r.interleaved = layout == APEX4_ROPE_INTERLEAVED;
     return APEX4_OK;
 }
 
@@ -154,6 +166,58 @@ int apex4_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
     if (T == 0) return APEX4_OK;
     return status_of(apex4::launch_kv_append(c, static_cast<const uint16_t*>(k), k_stride, static_cast<const uint16_t*>(v),
                                              v_stride, q_start, T, static_cast<hipStream_t>(stream)));
+}
+
+int apex4_rope(const void* x, int64_t x_stride, const int32_t* positions, int64_t T, int64_t heads, int64_t head_dim,
+               const double* freq, int64_t rot, int layout, float mag, void* out, int64_t out_stride, void* stream) {
+    if (!present(x, T) || !present(positions, T) || !freq || !present(out, T)) return APEX4_ERR_NULL;
+    Rotary r;
+    if (heads < 1 || heads > 65536 || head_dim < 8 || head_dim > 512 || head_dim % 8 != 0) return APEX4_ERR_SHAPE;
+    int rc = make_rotary(r, freq, head_dim, rot, layout, mag);
+    if (rc) return rc;
+    if ((rc = check_rows(T, heads, head_dim, x_stride)) || (rc = check_rows(T, heads, head_dim, out_stride))) return rc;
+    if (T > 1 && x == out && x_stride != out_stride) return APEX4_ERR_SHAPE;
+    if (!aligned(x, 16) || !aligned(positions, 4) || !aligned(freq, 8) || !aligned(out, 16)) return APEX4_ERR_ALIGN;
+    if ((rc = check_device())) return rc;
+    if (T == 0) return APEX4_OK;
+    return status_of(apex4::launch_rope(static_cast<const uint16_t*>(x), x_stride, positions, T, static_cast<int>(heads),
+                                        static_cast<int>(head_dim), r, static_cast<uint16_t*>(out), out_stride,
+                                        static_cast<hipStream_t>(stream)));
+}
+
+int apex4_kv_append_rope(const void* q, int64_t q_stride, int64_t heads, void* q_out, const void* k, int64_t k_stride,
+                         const void* v, int64_t v_stride, const int32_t* q_start, int64_t T, const int32_t* positions,
+                         const double* freq, int64_t rot, int layout, float mag, void* k_pages, void* v_pages,
+                         int64_t n_pages, const int32_t* table, int64_t width, const int32_t* kv_len, int64_t B,
+                         int64_t kv_heads, int64_t head_dim, int64_t page, int cache, void* stream) {
+    const int64_t queries = heads == 0 ? 0 : T;
+    if (!present(q, queries) || !present(q_out, queries) || !present(k, T) || !present(v, T) || !freq || !k_pages || !v_pages ||
+        !present(table, B) || !present(kv_len, B))
+        return APEX4_ERR_NULL;
+    KvView c;
+    Rotary r;
+    int rc = make_view(c, k_pages, v_pages, n_pages, table, width, kv_len, B, kMaxLen, kv_heads, head_dim, page, cache);
+    if (rc || (rc = make_rotary(r, freq, head_dim, rot, layout, mag))) return rc;
+    if (heads < 0 || heads > 65536) return APEX4_ERR_SHAPE;
+    if (heads && (rc = check_rows(T, heads, head_dim, q_stride))) return rc;
+    if ((rc = check_rows(T, kv_heads, head_dim, k_stride)) || (rc = check_rows(T, kv_heads, head_dim, v_stride))) return rc;
+    if (T > 0 && (q_start ? B < 1 : T != B)) return APEX4_ERR_SHAPE;
+    if (heads && q == q_out && T > 0) return APEX4_ERR_SHAPE;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(q_start, 4) || !aligned(positions, 4) || !aligned(freq, 8)) return APEX4_ERR_ALIGN;
+    if (heads && (!aligned(q, 16) || !aligned(q_out, 16))) return APEX4_ERR_ALIGN;
+    if ((rc = check_view_pointers(c)) || (rc = check_device())) return rc;
+    if (T == 0) return APEX4_OK;
+    apex4::RopeRows a;
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.heads = static_cast<int>(heads);
+    a.positions = positions;
+    return status_of(apex4::launch_kv_append_rope(c, a, q_start, T, r, static_cast<hipStream_t>(stream)));
 }
 
 int apex4_kv_gather(const void* k_pages, const void* v_pages, int64_t n_pages, const int32_t* table, int64_t width,

@@ -12,12 +12,20 @@
 // ragged prompts, 8958 tokens, into an int4 cache 14.4 us (37 MB read, 10 written: 3.2
 // TB/s, with the vector units 0.42 busy: neither is full, the chain comes before the
 // bytes), back 12.8 us (3.8 TB/s); binary16 there and back 30.4 us (4.8 TB/s).
+//
+// With rotary positions on the way (kv_append_rope_kernel) a lane moves the 16 values
+// of one (token, head) that hold both of every pair, and blockIdx.y 2 turns the queries
+// into a buffer of their own: one launch for what stands between a layer's projection
+// and its attention.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "apex4_internal.h"
 #include "kv_cache.h"
 #include "quant_core.h"
+#include "rope_core.h"
 
 namespace apex4 {
 namespace {
@@ -152,6 +160,106 @@ __global__ __launch_bounds__(kThreads) void kv_gather_kernel(KvView c, uint16_t*
         });
 }
 
+// The place of new token i, its position, and whether it is a sequence's.
+struct Spot {
+    Place place;
+    int pos;
+    bool live;
+};
+__device__ __forceinline__ Spot spot_of(const KvView& c, const int32_t* q_start, int64_t T, int64_t i) {
+    Spot s = {{-1, 0}, 0, false};
+    if (i >= T) return s;
+    const int b = sequence_of(q_start, c.B, static_cast<int>(i));
+    const int64_t end = q_start ? q_start[b + 1] : i + 1;
+    if (i >= end) return s;
+    const int64_t pos = c.kv_len[b] - end + i;
+    s.pos = static_cast<int>(pos);
+    s.live = true;
+    if (pos < 0) return s;
+    s.place.page = page_of(c, b, pos);
+    s.place.at = static_cast<int>(pos) & ((1 << c.page_shift) - 1);
+    return s;
+}
+
+// blockIdx.y: 0 keys, 1 values (not turned), 2 queries (into rows of their own).  A
+// key is turned and rounded to binary16 before it is stored or quantized: what the
+// two calls, one after the other, would give, bit for bit.
+template <int D, bool I4, int FORM>
+__global__ __launch_bounds__(kThreads) void kv_append_rope_kernel(KvView c, RopeRows a, const int32_t* __restrict__ q_start,
+                                                                  int64_t T, Rotary r, int per) {
+    constexpr int L = D / 16, U = 4;
+    __shared__ Spot spots[kMost];
+    __shared__ float2 turns[kMost * D / 2];
+    const int64_t i0 = static_cast<int64_t>(blockIdx.x) * per;
+    const int tokens = static_cast<int>(T - i0 < per ? T - i0 : per);
+    const bool turned = blockIdx.y != 1, cached = blockIdx.y != 2;
+    const int heads = cached ? c.kv_heads : a.heads, pairs = r.rot / 2;
+    const uint16_t* src = blockIdx.y == 0 ? a.k : blockIdx.y == 1 ? a.v : a.q;
+    const int64_t stride = blockIdx.y == 0 ? a.k_stride : blockIdx.y == 1 ? a.v_stride : a.q_stride;
+    uint8_t* plane = const_cast<uint8_t*>(blockIdx.y ? c.v : c.k);
+    if (static_cast<int>(threadIdx.x) < tokens) spots[threadIdx.x] = spot_of(c, q_start, T, i0 + threadIdx.x);
+    __syncthreads();
+    if (turned) {
+        for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
+            const int t = i / pairs;
+            turns[i] = rope::turn_of(r, a.positions ? a.positions[i0 + t] : spots[t].pos, i - t * pairs);
+        }
+        __syncthreads();
+    }
+    const int l = threadIdx.x % L, rows = tokens * heads;
+    const int2 at = FORM == rope::kSingles ? make_int2(2 * l, 2 * l + 1) : rope::pieces_of<FORM>(r, l);
+    for (int row0 = threadIdx.x / L; row0 < rows; row0 += U * (kThreads / L)) {  // whole rows of lanes
+        u32x4 x[U], y[U];
+        int tok[U], head[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = row0 + u * (kThreads / L);
+            tok[u] = row / heads;
+            head[u] = row - tok[u] * heads;
+            if (row < rows) {
+                const uint16_t* from = src + (i0 + tok[u]) * stride + head[u] * D;
+                if (FORM == rope::kSingles && turned) {
+                    x[u] = rope::turned_piece(r, from, at.x, turns + tok[u] * pairs);
+                    y[u] = rope::turned_piece(r, from, at.y, turns + tok[u] * pairs);
+                } else {
+                    x[u] = *reinterpret_cast<const u32x4*>(from + 8 * at.x);
+                    y[u] = *reinterpret_cast<const u32x4*>(from + 8 * at.y);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (row0 + u * (kThreads / L) >= rows) break;
+            if constexpr (FORM != rope::kSingles)
+                if (turned) rope::turn_pieces<FORM>(r, l, turns + tok[u] * pairs, x[u], y[u]);
+            const Spot& s = spots[tok[u]];
+            if (!cached) {
+                uint16_t* to = a.q_out + ((i0 + tok[u]) * heads + head[u]) * D;
+                if (s.live) {
+                    *reinterpret_cast<u32x4*>(to + 8 * at.x) = x[u];
+                    *reinterpret_cast<u32x4*>(to + 8 * at.y) = y[u];
+                }
+            } else if constexpr (I4) {
+                const uint4 p = make_uint4(x[u][0], x[u][1], x[u][2], x[u][3]), q = make_uint4(y[u][0], y[u][1], y[u][2], y[u][3]);
+                const uint32_t mp = absmax8_bits(p), mq = absmax8_bits(q);
+                uint16_t bits;
+                const float sc = scale_of(group_max<L>(mp > mq ? mp : mq), &bits);
+                const uint32_t cp = pack8(p, sc, inv_of(sc)), cq = pack8(q, sc, inv_of(sc));
+                if (s.place.page >= 0) {
+                    uint8_t* to = plane + row_at<D, true>(c, s.place, head[u]);
+                    *reinterpret_cast<uint32_t*>(to + 4 * at.x) = cp;
+                    *reinterpret_cast<uint32_t*>(to + 4 * at.y) = cq;
+                    if (l == 0) *reinterpret_cast<uint16_t*>(plane + scale_at<D>(c, s.place, head[u])) = bits;
+                }
+            } else if (s.place.page >= 0) {
+                uint8_t* to = plane + row_at<D, false>(c, s.place, head[u]);
+                *reinterpret_cast<u32x4*>(to + 16 * at.x) = x[u];
+                *reinterpret_cast<u32x4*>(to + 16 * at.y) = y[u];
+            }
+        }
+    }
+}
+
 // Tokens of a workgroup: one while that leaves the compute units with few
 // workgroups each, then up to kMost.
 int tokens_per_group(int64_t T) {
@@ -168,6 +276,28 @@ hipError_t launch_kv_append(const KvView& c, const uint16_t* k, int64_t k_stride
     auto run = [&](auto kernel) { kernel<<<grid_of(T, per), kThreads, 0, stream>>>(c, k, k_stride, v, v_stride, q_start, T, per); };
     if (c.D == 128) c.i4 ? run(kv_append_kernel<128, true>) : run(kv_append_kernel<128, false>);
     else c.i4 ? run(kv_append_kernel<64, true>) : run(kv_append_kernel<64, false>);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_append_rope(const KvView& c, const RopeRows& a, const int32_t* q_start, int64_t T, const Rotary& r,
+                                 hipStream_t stream) {
+    const int per = tokens_per_group(T);
+    dim3 grid = grid_of(T, per);
+    grid.y = a.heads ? 3 : 2;
+    auto run = [&](auto kernel) { kernel<<<grid, kThreads, 0, stream>>>(c, a, q_start, T, r, per); };
+    auto form = [&](auto d, auto i4) {
+        constexpr int D = decltype(d)::value;
+        constexpr bool I4 = decltype(i4)::value;
+        switch (rope::form_of(r, D)) {
+            case rope::kHalves: run(kv_append_rope_kernel<D, I4, rope::kHalves>); break;
+            case rope::kNeighbours: run(kv_append_rope_kernel<D, I4, rope::kNeighbours>); break;
+            default: run(kv_append_rope_kernel<D, I4, rope::kSingles>);
+        }
+    };
+    using std::integral_constant;
+    using std::bool_constant;
+    if (c.D == 128) c.i4 ? form(integral_constant<int, 128>(), bool_constant<true>()) : form(integral_constant<int, 128>(), bool_constant<false>());
+    else c.i4 ? form(integral_constant<int, 64>(), bool_constant<true>()) : form(integral_constant<int, 64>(), bool_constant<false>());
     return hipGetLastError();
 }
 
