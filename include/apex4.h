@@ -400,6 +400,30 @@ int apex4_w4a4_gemm_mx_ws(const uint8_t* A_6, const uint8_t* e_a,
                           void* Y, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * Linears in 8 bits, for layers that 4 bits are too few for: one scale a token (row of
+ * A) and one a channel (row of W).  Not the paper's method; its W4A4 linears stand beside them.
+ *
+ * apex4_quantize_act8: x [M, K] binary16 -> A_8 [M, K] int8 codes and s_a [M] binary32:
+ *   s = the binary32 nearest to max|x| / 127, codes = clamp(round-half-even(x / s), -127,
+ *   127), taken on the exact quotient; a row whose s is zero gets zero codes, and one that
+ *   holds an infinity or a NaN gets a scale that is one and zero codes.  Deterministic.
+ *   The same call quantizes weights ([N, K] -> W_8, s_w).
+ * apex4_w8a8_gemm: Y[m,n] = binary16(s_a[m] s_w[n] sum_k A_8[m,k] W_8[n,k]), the sum
+ *   exact (int32), the products binary32, rounded once more to binary16.  A row's bits do
+ *   not depend on the other rows.
+ * apex4_w8a8_linear: both, Y bit for bit as after the two calls.  A_8_work [M, K] and
+ *   s_a_work [M] are scratch (a single token is quantized on the way and leaves them alone).
+ *
+ * All buffers device memory, 16-byte aligned.  M >= 0, N >= 1, K % 32 == 0, 32 <= K <
+ * 131072; each operand's codes under 4 GiB (M K and N K below 2^32).
+ */
+int apex4_quantize_act8(const void* x, int64_t M, int64_t K, int8_t* A_8, float* s_a, void* stream);
+int apex4_w8a8_gemm(const int8_t* A_8, const float* s_a, const int8_t* W_8, const float* s_w, int64_t M, int64_t N, int64_t K,
+                    void* Y, void* stream);
+int apex4_w8a8_linear(const void* x, const int8_t* W_8, const float* s_w, int64_t M, int64_t N, int64_t K, void* Y,
+                      int8_t* A_8_work, float* s_a_work, void* stream);
+
+/*
  * Paged key-value cache and the attention that reads it: what stands between a
  * decoder layer's qkv projection and its output projection.
  *

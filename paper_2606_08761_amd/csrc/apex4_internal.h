@@ -170,6 +170,18 @@ hipError_t launch_gemm_mx_splitk(const uint8_t* A6, const uint8_t* ea, const uin
                                  int64_t M, int64_t N, int64_t K, int64_t G, uint16_t* Y, float* part,
                                  hipStream_t stream);
 
+// 8-bit codes with a scale a token and a scale a channel: the quantizer, and the GEMM on
+// tiles, or for few rows with the weights streamed once (a single token quantized on the
+// way, where it fits).  All give the same bits: the sums are exact.
+hipError_t launch_quantize8(const uint16_t* x, int64_t M, int64_t K, int8_t* q, float* s, hipStream_t stream);
+hipError_t launch_w8a8_tiles(const int8_t* A, const float* sa, const int8_t* W, const float* sw, int M, int N, int K, uint16_t* Y,
+                             hipStream_t stream);
+bool w8a8_rows_fits(int64_t M, int64_t N);
+hipError_t launch_w8a8_rows(const int8_t* A, const float* sa, const int8_t* W, const float* sw, int M, int N, int K, uint16_t* Y,
+                            hipStream_t stream);
+bool w8a8_fused_fits(int64_t M, int64_t K);
+hipError_t launch_w8a8_fused(const uint16_t* x, const int8_t* W, const float* sw, int N, int K, uint16_t* Y, hipStream_t stream);
+
 // A paged key-value cache as the kernels see it (layout: kv_cache.h).
 struct KvView {
     const uint8_t* k = nullptr;       // planes of the keys and of the values
