@@ -609,6 +609,37 @@ int apex4_pages_compact(void* pool, int64_t planes, int64_t page_bytes, int32_t*
 int apex4_pages_copy(void* pool, int64_t planes, int64_t page_bytes, int64_t n_pages, const int32_t* src, const int32_t* dst,
                      int64_t n, void* stream);
 
+/*
+ * Sampling: a token for each of B rows of V logits (APEX4_LOGITS_FP16: binary16, _FP32:
+ * binary32), `stride` elements apart, from one random number u a row.
+ *   A row's order is by falling logits, equal ones by rising index; w = exp((x - max) /
+ *   temperature).  Kept are
+ *     top_k > 0: the first top_k of that order;
+ *     top_p < 1: of these the shortest beginning that holds top_p of their sum;
+ *     min_p > 0: those with w >= min_p;
+ *   and always the first.  The token is the first, by index, whose running sum of kept w
+ *   passes u times their sum (u below 0: 0; from 1 on: the last kept one), and its
+ *   probability w / sum.  A temperature that is not above 0, top_k 1, top_p not above 0
+ *   and min_p above 1 leave the first alone (probability 1); a top_p or min_p that is NaN
+ *   is off.
+ *   A logit of -infinity or NaN is never chosen; a row of nothing else gives -1 (and
+ *   probability 0).  Infinite logits share all of the weight.
+ *   temperature, top_k, top_p, min_p: [B] on the device, or NULL: the value beside it
+ *   for every row.  u [B] binary32.
+ *   tokens [B] int32, probs [B] binary32 or NULL (outputs).
+ * Weights are binary64 and summed exactly, in units of 2^-45 of the largest: the outcome
+ * is a function of the row and its settings alone.  Logits below 2^-46 of the largest
+ * weight count as never chosen.
+ * logits 16-byte aligned, the others 4-byte; the aligned 16-byte pieces that hold a row's
+ * logits are read whole.  B up to 2^21, V up to 2^18.
+ */
+#define APEX4_LOGITS_FP16 0
+#define APEX4_LOGITS_FP32 1
+int apex4_sample(const void* logits, int type, int64_t stride, int64_t B, int64_t V, const float* u,
+                 const float* temperature, float temperature_all, const int32_t* top_k, int64_t top_k_all,
+                 const float* top_p, float top_p_all, const float* min_p, float min_p_all, int32_t* tokens, float* probs,
+                 void* stream);
+
 /* Static description of a status code (never NULL). */
 const char* apex4_status_string(int status);
 

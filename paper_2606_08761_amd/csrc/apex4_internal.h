@@ -182,6 +182,24 @@ hipError_t launch_w8a8_rows(const int8_t* A, const float* sa, const int8_t* W, c
 bool w8a8_fused_fits(int64_t M, int64_t K);
 hipError_t launch_w8a8_fused(const uint16_t* x, const int8_t* W, const float* sw, int N, int K, uint16_t* Y, hipStream_t stream);
 
+// Sampling: B rows of V logits (binary16 or binary32), `stride` elements apart.  Settings
+// of a row, or one for all where the pointer is nullptr.
+struct SampleArgs {
+    const void* logits = nullptr;
+    const float* u = nullptr;            // [B]
+    const float* temperature = nullptr;  // [B] each
+    const int32_t* top_k = nullptr;
+    const float* top_p = nullptr;
+    const float* min_p = nullptr;
+    int32_t* tokens = nullptr;           // [B]
+    float* probs = nullptr;              // [B] or nullptr
+    int64_t stride = 0;
+    int V = 0;
+    int top_k_all = 0;
+    float temperature_all = 1.f, top_p_all = 1.f, min_p_all = 0.f;
+};
+hipError_t launch_sample(const SampleArgs& a, int64_t B, bool f16, hipStream_t stream);
+
 // A paged key-value cache as the kernels see it (layout: kv_cache.h).
 struct KvView {
     const uint8_t* k = nullptr;       // planes of the keys and of the values

@@ -1,0 +1,674 @@
+// Sampling: a token for every row of logits from one given random number.
+//
+// In the order of falling logits (equal ones by index, lowest first) w = 2^((x - max) c),
+// c = log2(e) / temperature; top-k keeps the first k; top-p of those the shortest
+// beginning that holds p of their sum; min-p those with w >= min_p.  All three keep a
+// beginning of that order, so one border does: a logit, and an index among those equal to
+// it.  The token is the first, by index, whose running sum of kept weights passes u times
+// their sum.
+//
+// Weights are computed in binary64 and held as whole numbers of 2^-45 of the largest
+// one: their sums are exact in any order, so that no result depends on which thread was
+// first, and a border moves by 2^-45 of a weight at most.  (In binary32 one row in some
+// hundred of a flat distribution over 10^5 tokens would get another token.)  A logit 46
+// octaves below the largest weighs nothing.
+//
+// A workgroup takes a row; rows of up to 128 KB stay in LDS, longer ones are read again,
+// through a ring in LDS that keeps four loads a wave in flight and no registers.  Passes
+// over the row:
+//   1  the largest logit;
+//   2  only for top-k or top-p: counts and sums by buckets of 1/16 octave below it; a scan
+//      gives the bucket of the border;
+//   3  the logits down to that bucket into a list, if it holds them; then all that follows
+//      goes over the list.  If not, the bucket's own go there, and the weights before it
+//      are summed by the waves' parts of the row.  The range of the bucket's logits is
+//      split into 1024 until one value is left, and for equal ones their indexes, 256 and
+//      then 1 at a time (where the list does not even hold the bucket, over the row);
+//   4  the token: by indexes in the list, or by the waves' parts of the row, then the
+//      logits of the part that holds it.
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "apex4_internal.h"
+
+namespace apex4 {
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned long long u64;
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kBuckets = 736;          // 1/16 octave each
+constexpr int kStageBytes = 128 << 10; // of a row in LDS
+constexpr int kLdsBytes = 160 << 10, kMostList = 9216;
+constexpr int kDepth = 4, kRingBytes = kWaves * kDepth * 1024;
+constexpr int kSteps = 64;             // table of 2^(i / 64)
+constexpr double kMagic = 0x1.8p52;    // added to a number below 2^51: its nearest whole one in the low bits
+constexpr float kNothing = -__builtin_inff();
+
+struct Shared {
+    u64 bucket_w[kBuckets];
+    u64 bin_w[1024];
+    double table[kSteps];
+    uint32_t bucket_n[kBuckets];
+    uint32_t bin_n[1024];
+    u64 wave_w[kWaves];
+    u64 part_w[kWaves];   // of the waves' parts of the row
+    uint32_t wave_n[kWaves];
+    float wave_max[kWaves];
+    // the border's bin: what lies before it and in it
+    u64 before_w, in_w;
+    uint32_t before_n, in_n;
+    int bin;
+    uint32_t listed, low, high, first;
+};
+
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);  // -0 as 0
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+__device__ __forceinline__ u32x4 read_lds(uint32_t at) {
+    return *(const __attribute__((address_space(3))) u32x4*)static_cast<uintptr_t>(at);
+}
+// 16 bytes a lane from base + off straight into LDS at `to` + 16 lane.  The compiler does
+// not see these loads: landed_but() waits for all but the last N of the wave's (and for its
+// reads of LDS).  The wait states let M0, and a base that came out of a vector
+// instruction, settle.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy_to_lds(uint32_t to, uint32_t off, const uint8_t* base) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off),
+                 "s"(static_cast<uint64_t>(hi) << 32 | lo)
+                 : "memory", "m0");
+}
+#pragma clang diagnostic pop
+template <int N>
+__device__ __forceinline__ void landed_but() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
+
+// What the passes need to know of a row.
+template <bool F16, bool STAGED>
+struct Row {
+    static constexpr int kVec = F16 ? 8 : 4;  // logits of 16 bytes, a piece
+    const uint8_t* base;   // 16-byte aligned, at or before the first logit
+    u32x4* staged;
+    uint32_t ring;         // the ring's place in LDS
+    const double* table;
+    int skip, V, pieces;   // logits between base and the first; pieces that hold the row
+    bool infinite;         // the largest logit is infinite: its like count as 0, the others as nothing
+    float half, c32;
+    double max, c64;
+
+    static constexpr uint32_t kNone = F16 ? 0xFC00FC00u : 0xFF800000u;  // -infinity
+    // A piece as it was read, with -infinity for what is not of the row.
+    __device__ __forceinline__ u32x4 trimmed(u32x4 v, int piece) const {
+        if ((piece == 0 && skip) || piece == pieces - 1) {
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                const int i = piece * kVec + j - skip;
+                if (i >= 0 && i < V) continue;
+                if constexpr (F16) v[j >> 1] = j & 1 ? (v[j >> 1] & 0xFFFFu) | (kNone & 0xFFFF0000u) : (v[j >> 1] & 0xFFFF0000u) | (kNone & 0xFFFFu);
+                else v[j] = kNone;
+            }
+        }
+        return v;
+    }
+    __device__ __forceinline__ static float raw(const u32x4& v, int j) {
+        if constexpr (F16) return __half2float(__ushort_as_half(static_cast<unsigned short>(j & 1 ? v[j >> 1] >> 16 : v[j >> 1] & 0xFFFFu)));
+        else return __uint_as_float(v[j]);
+    }
+    __device__ __forceinline__ float finite(float x) const { return infinite ? (x == -kNothing ? 0.f : kNothing) : x; }
+    // Logit i of the row.
+    __device__ __forceinline__ float at(int i) const {
+        const void* p = STAGED ? static_cast<const void*>(staged) : base;
+        if constexpr (F16) return finite(__half2float(__ushort_as_half(static_cast<const uint16_t*>(p)[i + skip])));
+        else return finite(static_cast<const float*>(p)[i + skip]);
+    }
+    // f(logits, index of the first) for the thread's pieces; wave w has the w-th part() of them,
+    // all its lanes together (a lane without a piece has -infinity).
+    template <class F>
+    __device__ __forceinline__ void each_piece(F f) const {
+        const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = threadIdx.x & 63;
+        const int begin = wave * part(), n = (min(pieces, begin + part()) - begin + 63) / 64;
+        const uint32_t slots = ring + wave * (kDepth * 1024);
+        auto fetch = [&](int it) {
+            const int i = min(begin + 64 * it + lane, pieces - 1);
+            copy_to_lds(slots + it % kDepth * 1024, static_cast<uint32_t>(i) * 16u, base);
+        };
+        if constexpr (!STAGED)
+            for (int it = 0; it < kDepth && it < n; ++it) fetch(it);
+        for (int it = 0; it < n; ++it) {
+            const int i = begin + 64 * it + lane;
+            u32x4 v;
+            if constexpr (STAGED) {
+                v = staged[min(i, pieces - 1)];
+            } else {
+                if (it + kDepth <= n) landed_but<kDepth - 1>();
+                else landed_but<0>();
+                v = trimmed(read_lds(slots + it % kDepth * 1024 + lane * 16), min(i, pieces - 1));
+                landed_but<kDepth - 1>();  // it is read before its place is loaded again
+                if (it + kDepth < n) fetch(it + kDepth);
+            }
+            if (i >= min(pieces, begin + part())) v = u32x4{kNone, kNone, kNone, kNone};
+            float x[kVec];
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) x[j] = finite(raw(v, j));
+            f(x, i * kVec - skip);
+        }
+    }
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+        each_piece([&](const float(&x)[kVec], int i) {
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) f(x[j], i + j);
+        });
+    }
+    __device__ __forceinline__ int part() const { return (pieces + kWaves - 1) / kWaves; }
+
+    // 1/16 octaves below the largest: rises as x falls (halves, whose difference cannot
+    // overflow).  NaN and -infinity are not below kBuckets: they are not live.
+    __device__ __forceinline__ float below(float x) const { return fmaf(-0.5f, x, half) * c32; }
+    __device__ __forceinline__ static bool live(float y) { return y < static_cast<float>(kBuckets); }
+    // 2^45 2^y for y = (x - max) c, not below -60, in binary64: y 64 = k + f, |f| <= 1/2, a power of two,
+    // the table's 2^(k % 64 / 64), and e^(f ln 2 / 64) by its series, whose terms from the
+    // third on (2^-25 and less) need binary32 alone.
+    __device__ __forceinline__ double weight(float x) const {
+        const double y = (static_cast<double>(x) - max) * c64, t = y + kMagic, f = y - (t - kMagic);
+        const int k = static_cast<int>(__double_as_longlong(t));
+        constexpr double l = 0.69314718055994530942 / kSteps;
+        const float g = static_cast<float>(f);
+        const float tail = g * g * g * static_cast<float>(l * l * l / 6) *
+                           fmaf(g, fmaf(g, static_cast<float>(l * l / 20), static_cast<float>(l / 4)), 1.f);
+        const double p = fma(f, fma(f, l * l / 2, l), static_cast<double>(tail));
+        const double a = table[k & (kSteps - 1)];
+        const double b = __longlong_as_double(__double_as_longlong(a) + (static_cast<long long>((k >> 6) + 45) << 52));
+        return fma(b, p, b);
+    }
+    __device__ __forceinline__ static u64 whole(double w) {  // 0 .. 2^45
+        return static_cast<u64>(__double_as_longlong(w + 0x1p52)) & 0x000FFFFFFFFFFFFFull;
+    }
+};
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_before(uint32_t v) {
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xF, false));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void add_before(uint32_t& n, u64& w) {
+    const uint32_t lo = from_before<CTRL, ROWS>(static_cast<uint32_t>(w)), hi = from_before<CTRL, ROWS>(static_cast<uint32_t>(w >> 32));
+    n += from_before<CTRL, ROWS>(n);
+    w += static_cast<u64>(hi) << 32 | lo;
+}
+// Running sums over the wave's lanes, the lane's own included: by 1, 2, 4 and 8 lanes
+// inside rows of 16, then the rows' last lanes into the rows behind them.
+__device__ __forceinline__ void wave_scan(uint32_t& n, u64& w) {
+    add_before<0x111, 0xF>(n, w);
+    add_before<0x112, 0xF>(n, w);
+    add_before<0x114, 0xF>(n, w);
+    add_before<0x118, 0xF>(n, w);
+    add_before<0x142, 0xA>(n, w);
+    add_before<0x143, 0xC>(n, w);
+}
+
+// The workgroup's sums, to every thread.  Begins with a barrier.
+__device__ __forceinline__ void group_sum(Shared& sm, uint32_t& n, u64& w) {
+    wave_scan(n, w);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) {
+        sm.wave_n[threadIdx.x >> 6] = n;
+        sm.wave_w[threadIdx.x >> 6] = w;
+    }
+    __syncthreads();
+    n = 0;
+    w = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        n += sm.wave_n[i];
+        w += sm.wave_w[i];
+    }
+}
+
+// What a border is looked for by: the k-th, the first whose running sum reaches `share`, or
+// the first whose running sum passes `goal`.
+struct Target {
+    enum Kind { kCount, kShare, kPass } kind;
+    uint32_t k;
+    double share;
+    u64 goal;
+    __device__ __forceinline__ bool reached(uint32_t n, u64 w) const {
+        return kind == kCount ? n >= k : kind == kShare ? static_cast<double>(w) >= share : w > goal;
+    }
+};
+
+// Of 1024 bins, a thread with (n, w) of each, the one in which what comes after (base_n,
+// base_w) reaches the target: to sm.bin, before_*, in_*.  Ends in a barrier.
+__device__ __forceinline__ void find_bin(Shared& sm, uint32_t n, u64 w, uint32_t base_n, u64 base_w, const Target& target) {
+    const int wave = threadIdx.x >> 6;
+    uint32_t sn = n;
+    u64 sw = w;
+    wave_scan(sn, sw);
+    if ((threadIdx.x & 63) == 63) {
+        sm.wave_n[wave] = sn;
+        sm.wave_w[wave] = sw;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+        if (i < wave) {
+            base_n += sm.wave_n[i];
+            base_w += sm.wave_w[i];
+        }
+    const uint32_t after_n = base_n + sn, first_n = after_n - n;
+    const u64 after_w = base_w + sw, first_w = after_w - w;
+    if (!target.reached(first_n, first_w) && target.reached(after_n, after_w)) {
+        sm.bin = threadIdx.x;
+        sm.before_n = first_n;
+        sm.before_w = first_w;
+        sm.in_n = n;
+        sm.in_w = w;
+    }
+    __syncthreads();
+}
+
+// Kept are logits above `key`, and those equal to it up to index `last`; their sum.
+struct Border {
+    uint32_t key;
+    int last;
+    u64 sum;
+};
+
+// What the list holds: nothing, the bucket of the border, or all down to it.
+enum Held : int { kNoList, kBucket, kAll };
+
+// A border's search.  The list is filled by the first (held < 0); the second one's border is
+// not behind the first's.  parts: the waves' sums of the kept weights before the bucket are
+// left in sm.part_w (min-p's `least` included) where the list holds the bucket alone.
+template <class R>
+__device__ Border search(Shared& sm, const R& row, u64* list, uint32_t room, const Target& target, bool weigh, bool parts, double least,
+                         int& held, uint32_t& listed) {
+    const int tid = threadIdx.x;
+    find_bin(sm, tid < kBuckets ? sm.bucket_n[tid] : 0u, tid < kBuckets ? sm.bucket_w[tid] : 0ull, 0u, 0ull, target);
+    const int bucket = sm.bin;
+    uint32_t before_n = sm.before_n;
+    const uint32_t members = sm.in_n;
+    u64 before_w = sm.before_w;
+    const float top = static_cast<float>(bucket), end = static_cast<float>(bucket + 1);  // 1/16 octaves
+    if (tid == 0) {
+        sm.low = 0xFFFFFFFFu;
+        sm.high = 0u;
+    }
+    uint32_t low = 0xFFFFFFFFu, high = 0u;
+    auto member = [&](float x) {
+        low = min(low, ordered(x));
+        high = max(high, ordered(x));
+    };
+    if (held != kAll) {
+        held = before_n + members <= room ? kAll : members <= room ? kBucket : kNoList;
+        listed = held == kAll ? before_n + members : members;
+        if (tid == 0) sm.listed = 0u;
+        __syncthreads();
+        // a piece's logits that `wanted` has a bit of, into the list, one count for a wave
+        auto append = [&](uint32_t wanted, const float(&x)[R::kVec], int i) {
+            uint32_t n = __builtin_popcount(wanted), own = n;
+            u64 none = 0;
+            wave_scan(n, none);
+            uint32_t at = 0;
+            if ((tid & 63) == 63) at = atomicAdd(&sm.listed, n);
+            at = __builtin_amdgcn_readlane(at, 63) + n - own;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j)
+                if (wanted >> j & 1 && at < room) list[at++] = static_cast<u64>(ordered(x[j])) << 32 | static_cast<uint32_t>(i + j);
+        };
+        u64 sum = 0;
+        if (held == kAll) {
+            row.each_piece([&](const float(&x)[R::kVec], int i) {
+                uint32_t wanted = 0;
+#pragma unroll
+                for (int j = 0; j < R::kVec; ++j) wanted |= row.below(x[j]) < end ? 1u << j : 0u;
+                if (__any(wanted)) append(wanted, x, i);
+            });
+        } else if (held == kBucket) {
+            row.each_piece([&](const float(&x)[R::kVec], int i) {
+                uint32_t wanted = 0;
+#pragma unroll
+                for (int j = 0; j < R::kVec; ++j) {
+                    const float y = row.below(x[j]);
+                    wanted |= y >= top && y < end ? 1u << j : 0u;
+                    if (parts && y < top) {
+                        const double w = row.weight(x[j]);
+                        if (w >= least) sum += R::whole(w);
+                    }
+                }
+                if (__any(wanted)) append(wanted, x, i);
+            });
+        } else {
+            row.each([&](float x, int) {
+                const float y = row.below(x);
+                if (y >= top && y < end) member(x);
+            });
+        }
+        uint32_t none = 0;
+        wave_scan(none, sum);
+        if ((tid & 63) == 63) sm.part_w[tid >> 6] = sum;
+    }
+    __syncthreads();
+    if (held != kNoList) {
+        for (uint32_t i = tid; i < listed; i += kThreads) {
+            const float x = unordered(static_cast<uint32_t>(list[i] >> 32)), y = row.below(x);
+            if (y >= top && y < end) member(x);
+        }
+    }
+    if (high) {
+        atomicMin(&sm.low, low);
+        atomicMax(&sm.high, high);
+    }
+    __syncthreads();
+    low = sm.low;
+    high = sm.high;
+    // f(key, index): the bucket's are all the logits from low to high
+    auto each = [&](auto f) {
+        if (held != kNoList) {
+            for (uint32_t i = tid; i < listed; i += kThreads) f(static_cast<uint32_t>(list[i] >> 32), static_cast<int>(list[i] & 0xFFFFFFFFu));
+        } else {
+            row.each([&](float x, int i) { f(ordered(x), i); });
+        }
+    };
+    Border b;
+    for (;;) {
+        const uint32_t range = high - low;
+        const int shift = range < 1024u ? 0 : 22 - __builtin_clz(range);
+        sm.bin_n[tid] = 0u;
+        sm.bin_w[tid] = 0ull;
+        __syncthreads();
+        each([&](uint32_t key, int) {
+            if (key < low || key > high) return;
+            const uint32_t bin = (high - key) >> shift;
+            atomicAdd(&sm.bin_n[bin], 1u);
+            if (weigh) atomicAdd(&sm.bin_w[bin], R::whole(row.weight(unordered(key))));
+        });
+        __syncthreads();
+        find_bin(sm, sm.bin_n[tid], sm.bin_w[tid], before_n, before_w, target);
+        before_n = sm.before_n;
+        before_w = sm.before_w;
+        const uint32_t first = high - (static_cast<uint32_t>(sm.bin) << shift);
+        if (shift == 0) {
+            b.key = first;
+            break;
+        }
+        const uint32_t span = (1u << shift) - 1u;
+        low = first - low > span ? first - span : low;
+        high = first;
+        __syncthreads();  // sm's fields are read
+    }
+    // of the equal ones, the first `take` by index
+    const uint32_t equal = sm.in_n;
+    const u64 w = weigh ? R::whole(row.weight(unordered(b.key))) : 0ull;
+    uint32_t take = equal;
+    if (target.kind == Target::kCount) {
+        take = target.k - before_n;
+    } else {
+        const double t = ceil((target.share - static_cast<double>(before_w)) / static_cast<double>(w));
+        take = t < 1.0 ? 1u : t > equal ? equal : static_cast<uint32_t>(t);
+        while (take > 1 && target.reached(0, before_w + (take - 1) * w)) --take;
+        while (take < equal && !target.reached(0, before_w + take * w)) ++take;
+    }
+    b.sum = before_w + take * w;
+    b.last = row.V;
+    if (take < equal) {
+        int first = 0;
+        uint32_t done = 0;
+        const Target nth = {Target::kCount, take, 0.0, 0ull};
+        for (int shift = 8; shift >= 0; shift -= 8) {  // V <= 2^18
+            __syncthreads();
+            sm.bin_n[tid] = 0u;
+            __syncthreads();
+            each([&](uint32_t key, int i) {
+                const int bin = (i - first) >> shift;
+                if (key == b.key && bin >= 0 && bin < 1024) atomicAdd(&sm.bin_n[bin], 1u);
+            });
+            __syncthreads();
+            find_bin(sm, sm.bin_n[tid], 0ull, done, 0ull, nth);
+            done = sm.before_n;
+            first += sm.bin << shift;
+        }
+        b.last = first;
+    }
+    __syncthreads();
+    return b;
+}
+
+// The largest whole number that is not above u total (total >= 1), and below total.
+__device__ __forceinline__ u64 share_of(float u, u64 total) {
+    if (!(u > 0.f)) return 0ull;
+    if (u >= 1.f) return total - 1;
+    int e;
+    const u64 f = static_cast<u64>(ldexpf(frexpf(u, &e), 24));  // u = f 2^(e - 24)
+    const int shift = 24 - e;
+    return shift < 128 ? static_cast<u64>(static_cast<unsigned __int128>(f) * total >> shift) : 0ull;
+}
+
+template <bool F16, bool STAGED>
+__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t room, int list_at) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    Shared& sm = *reinterpret_cast<Shared*>(smem);
+    u64* list = reinterpret_cast<u64*>(smem + list_at);
+    using R = Row<F16, STAGED>;
+    constexpr int kSize = F16 ? 2 : 4;
+
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int64_t b = blockIdx.x;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(a.logits) + static_cast<uintptr_t>(b * a.stride) * kSize;
+    R row;
+    row.base = reinterpret_cast<const uint8_t*>(at & ~static_cast<uintptr_t>(15));
+    row.staged = reinterpret_cast<u32x4*>(smem + (sizeof(Shared) + 15) / 16 * 16);
+    row.ring = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_u8*)(smem + (sizeof(Shared) + 15) / 16 * 16)));
+    row.table = sm.table;
+    row.skip = static_cast<int>(at & 15) / kSize;
+    row.V = a.V;
+    row.pieces = (row.skip + a.V + R::kVec - 1) / R::kVec;
+    row.infinite = false;
+
+    const float t = a.temperature ? a.temperature[b] : a.temperature_all, p = a.top_p ? a.top_p[b] : a.top_p_all;
+    const float least = a.min_p ? a.min_p[b] : a.min_p_all, u = a.u[b];
+    const int k = a.top_k ? a.top_k[b] : a.top_k_all;
+
+    // 1: the largest logit
+    float m = kNothing;
+    auto larger = [&](float x) { m = x > m ? x : m; };
+    if constexpr (STAGED) {
+        const int part = row.part(), end = min(row.pieces, (wave + 1) * part);
+        for (int i = wave * part + lane; i < end; i += 64) {
+            const u32x4 v = row.trimmed(reinterpret_cast<const u32x4*>(row.base)[i], i);
+            row.staged[i] = v;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j) larger(R::raw(v, j));
+        }
+    } else {
+        row.each([&](float x, int) { larger(x); });
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) larger(__shfl_xor(m, d, 64));
+    if (lane == 0) sm.wave_max[wave] = m;
+    if (tid == 0) sm.first = 0xFFFFFFFFu;
+    if (tid < kBuckets) {
+        sm.bucket_n[tid] = 0u;
+        sm.bucket_w[tid] = 0ull;
+    }
+    if (tid < kSteps) sm.table[tid] = exp2(tid * (1.0 / kSteps));
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) larger(sm.wave_max[i]);
+    if (m == kNothing) {  // nothing can be chosen
+        if (tid == 0) {
+            a.tokens[b] = -1;
+            if (a.probs) a.probs[b] = 0.f;
+        }
+        return;
+    }
+    row.infinite = m == -kNothing;
+    if (row.infinite) m = 0.f;
+    // settings that leave the first alone: the largest logit, the lowest index of equal ones
+    if (!(t > 0.f) || k == 1 || p <= 0.f || least > 1.f) {
+        uint32_t first = 0xFFFFFFFFu;
+        row.each([&](float x, int i) {
+            if (x == m) first = min(first, static_cast<uint32_t>(i));
+        });
+        if (first != 0xFFFFFFFFu) atomicMin(&sm.first, first);
+        __syncthreads();
+        if (tid == 0) {
+            a.tokens[b] = static_cast<int>(sm.first);
+            if (a.probs) a.probs[b] = 1.f;
+        }
+        return;
+    }
+    const double c = 1.4426950408889634074 / static_cast<double>(t);
+    row.max = m;
+    row.half = 0.5f * m;
+    row.c64 = kSteps * c;
+    row.c32 = fminf(static_cast<float>(32.0 * c), 3.4e38f);  // 0 times it is 0
+
+    // 2, 3: the border
+    const bool by_k = k > 1 && k < a.V, by_p = p < 1.f;
+    const double floor_w = least > 0.f ? 0x1p45 * static_cast<double>(least) : 0.0;
+    Border border = {0u, a.V, 0ull};
+    int held = -1;
+    uint32_t listed = 0;
+    if (by_k || by_p) {
+        row.each([&](float x, int) {
+            const float y = row.below(x);
+            if (!R::live(y)) return;
+            atomicAdd(&sm.bucket_n[static_cast<int>(y)], 1u);
+            if (by_p) atomicAdd(&sm.bucket_w[static_cast<int>(y)], R::whole(row.weight(x)));
+        });
+        __syncthreads();
+        uint32_t n = tid < kBuckets ? sm.bucket_n[tid] : 0u;
+        u64 w = tid < kBuckets ? sm.bucket_w[tid] : 0ull;
+        group_sum(sm, n, w);
+        __syncthreads();
+        border.sum = w;
+        if (by_k && static_cast<uint32_t>(k) < n)
+            border = search(sm, row, list, room, Target{Target::kCount, static_cast<uint32_t>(k), 0.0, 0ull}, by_p, !by_p, floor_w, held, listed);
+        if (by_p)
+            border = search(sm, row, list, room, Target{Target::kShare, 0u, static_cast<double>(p) * static_cast<double>(border.sum), 0ull}, true, true,
+                            floor_w, held, listed);
+    }
+
+    // 4: the token.  The weight of a logit if it is kept, or 0: above `low`, and not one of
+    // those equal to the border's that come after its last.
+    // Where no border is, what is 50 octaves below the largest (rounded anyhow: 46 to 60
+    // would do) stays out, and what is no number.
+    const float dead = fminf(m - static_cast<float>(50.0 / c), unordered(ordered(m) - 1u));
+    const float low = border.key ? unordered(border.key - 1u) : dead;
+    const float tied = border.last < a.V ? unordered(border.key) : __builtin_nanf("");
+    auto kept = [&](float x, int i) -> u64 {
+        if (!(x > low) || (x == tied && i > border.last)) return 0ull;
+        const double w = row.weight(x);
+        return w >= floor_w ? R::whole(w) : 0ull;
+    };
+    auto done = [&](int i, float x, u64 total) {
+        a.tokens[b] = i;
+        if (a.probs) a.probs[b] = static_cast<float>(row.weight(x) / static_cast<double>(total));
+    };
+    if (held == kAll) {
+        // by indexes, 256 at a time, then 1
+        int first = 0;
+        u64 total = 0, passed = 0;
+        Target target = {Target::kPass, 0u, 0.0, 0ull};
+        for (int shift = 8; shift >= 0; shift -= 8) {
+            sm.bin_w[tid] = 0ull;
+            __syncthreads();
+            u64 sum = 0;
+            for (uint32_t e = tid; e < listed; e += kThreads) {
+                const uint32_t key = static_cast<uint32_t>(list[e] >> 32);
+                const int i = static_cast<int>(list[e] & 0xFFFFFFFFu), bin = (i - first) >> shift;
+                if (bin < 0 || bin >= 1024) continue;
+                const u64 w = kept(unordered(key), i);
+                if (w) atomicAdd(&sm.bin_w[bin], w);
+                sum += w;
+            }
+            if (shift) {
+                uint32_t none = 0;
+                total = sum;
+                group_sum(sm, none, total);
+                target.goal = share_of(u, total);
+            }
+            __syncthreads();
+            find_bin(sm, 0u, sm.bin_w[tid], 0u, passed, target);
+            passed = sm.before_w;
+            first += sm.bin << shift;
+            __syncthreads();
+        }
+        for (uint32_t e = tid; e < listed; e += kThreads)
+            if (static_cast<int>(list[e] & 0xFFFFFFFFu) == first) done(first, unordered(static_cast<uint32_t>(list[e] >> 32)), total);
+        return;
+    }
+    if (held == kBucket && !(by_k && by_p)) {  // pass 3 left the parts' sums, but for the bucket's
+        for (uint32_t e = tid; e < listed; e += kThreads) {
+            const uint32_t key = static_cast<uint32_t>(list[e] >> 32);
+            const int i = static_cast<int>(list[e] & 0xFFFFFFFFu);
+            const u64 w = kept(unordered(key), i);
+            if (w) atomicAdd(&sm.part_w[(i + row.skip) / R::kVec / row.part()], w);
+        }
+    } else {
+        u64 sum = 0;
+        uint32_t none = 0;
+        row.each([&](float x, int i) { sum += kept(x, i); });
+        wave_scan(none, sum);
+        if (lane == 63) sm.part_w[wave] = sum;
+    }
+    __syncthreads();
+    u64 total = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) total += sm.part_w[i];
+    u64 goal = share_of(u, total);
+    int w = 0;
+    while (w < kWaves - 1 && goal >= sm.part_w[w]) goal -= sm.part_w[w++];
+    // that part's logits, a run of them a thread
+    const int begin = max(0, w * row.part() * R::kVec - row.skip), end = min(a.V, (w + 1) * row.part() * R::kVec - row.skip);
+    const int run = (end - begin + kThreads - 1) / kThreads, first = min(end, begin + tid * run), last = min(end, first + run);
+    u64 own = 0;
+    for (int i = first; i < last; ++i) own += kept(row.at(i), i);
+    find_bin(sm, 0u, own, 0u, 0ull, Target{Target::kPass, 0u, 0.0, goal});
+    if (tid == sm.bin) {
+        u64 left = goal - sm.before_w;
+        for (int i = first; i < last; ++i) {
+            const float x = row.at(i);
+            const u64 v = kept(x, i);
+            if (left < v) {
+                done(i, x, total);
+                break;
+            }
+            left -= v;
+        }
+    }
+}
+
+template <bool F16, bool STAGED>
+hipError_t run(const SampleArgs& a, int64_t B, int row_bytes, hipStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    constexpr int fixed = (sizeof(Shared) + 15) / 16 * 16;
+    static_assert(fixed + kStageBytes + 1024 * 8 <= kLdsBytes && fixed + kRingBytes + kMostList * 8 <= kLdsBytes, "fits a compute unit's LDS");
+    const auto k = sample_kernel<F16, STAGED>;
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(k), kLdsBytes, done);
+    if (e != hipSuccess) return e;
+    const int list_at = fixed + (STAGED ? row_bytes : kRingBytes), left = (kLdsBytes - list_at) / 8, room = left < kMostList ? left : kMostList;
+    k<<<dim3(static_cast<unsigned>(B)), dim3(kThreads), list_at + room * 8, st>>>(a, static_cast<uint32_t>(room), list_at);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_sample(const SampleArgs& a, int64_t B, bool f16, hipStream_t stream) {
+    const int bytes = (a.V * (f16 ? 2 : 4) + 15) / 16 * 16 + 16;  // a row that begins inside a piece has one more
+    if (bytes <= kStageBytes) return f16 ? run<true, true>(a, B, bytes, stream) : run<false, true>(a, B, bytes, stream);
+    return f16 ? run<true, false>(a, B, bytes, stream) : run<false, false>(a, B, bytes, stream);
+}
+
+}  // namespace apex4

@@ -1,0 +1,259 @@
+"""Sampling against the definition in 80 bits, and where the outcome is known without
+arithmetic."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_attn import dev
+
+pytestmark = pytest.mark.gpu
+F32 = np.float32
+
+
+@pytest.fixture(scope="module")
+def pk():
+    import paper_2606_08761_amd as pk
+    return pk
+
+
+def plain(x, u, t, k, p, least):
+    """(token, probability, how near the decision was: the distance of u's target from the
+    borders of the token's share, and of top-p's from the running sums beside it, as shares)."""
+    x = np.where(np.isnan(x), -np.inf, x.astype(np.longdouble))
+    order = np.argsort(-x, kind="stable")
+    if not x[order[0]] > -np.inf:
+        return -1, 0.0, 1.0
+    if not t > 0 or k == 1 or p <= 0 or least > 1:
+        return int(order[0]), 1.0, 1.0
+    d = np.where(x == x[order[0]], 0, x - x[order[0]])
+    with np.errstate(invalid="ignore"):
+        w = np.where(d == 0, 1, np.exp(np.where(d == -np.inf, -np.inf, d / np.longdouble(t))))
+    s = w[order]
+    n, near = len(x), 1.0
+    if 0 < k < n:
+        n = k
+    if p < 1:
+        run = np.cumsum(s[:n])
+        cut = np.longdouble(p) * run[-1]
+        near = float(np.abs(run - cut).min() / run[-1])
+        n = min(n, int((run < cut).sum()) + 1)
+    if least > 0:
+        inside = s[:n] >= np.longdouble(least)
+        n = max(1, int(inside.sum()))
+    chosen = np.sort(order[:n])
+    run = np.cumsum(w[chosen])
+    goal = np.longdouble(min(max(float(u), 0.0), 1.0) if u == u else 0.0) * run[-1]
+    i = int((run <= goal).sum())
+    if i >= len(chosen) or u >= 1:
+        i = int(np.nonzero(w[chosen] > 2.0 ** -45)[0][-1])
+    if u < 1:
+        near = min(near, float(np.abs(run[max(0, i - 1):i + 1] - goal).min() / run[-1]) if goal > 0 else 1.0)
+    return int(chosen[i]), float(w[chosen[i]] / run[-1]), near
+
+
+def check(pk, x, u, t=1.0, k=0, p=1.0, least=0.0, gap=0):
+    """x [B, V]; settings: numbers or [B].  Rounded weights (2^-46 of the largest each, V of
+    them) decide otherwise than exact ones only where a decision is as near as that."""
+    import torch
+    B, V = x.shape
+    wide = np.zeros((B, V + gap), x.dtype)
+    wide[:, :V] = x
+    u = np.asarray(u, F32)
+    kw = {n: dev(np.asarray(v, np.int32 if n == "top_k" else F32)) if np.ndim(v) else v
+          for n, v in (("temperature", t), ("top_k", k), ("top_p", p), ("min_p", least))}
+    tokens, probs = (y.cpu().numpy() for y in pk.apex4_sample(dev(wide)[:, :V], dev(u), **kw))
+    assert torch.cuda.current_stream() is not None
+    full = [np.broadcast_to(np.asarray(v, np.int64 if n == "k" else F32), (B,)) for n, v in (("t", t), ("k", k), ("p", p), ("least", least))]
+    for b in range(B):
+        token, prob, near = plain(x[b], u[b], *(f[b] for f in full))
+        assert tokens[b] == token or near <= V * 2.0 ** -45, (b, tokens[b], token, near)
+        if tokens[b] == token:  # probabilities: binary64 quotients, rounded to binary32; the sum is off by V units
+            assert abs(probs[b] - prob) <= 2.0 ** -24 * prob + V * 2.0 ** -45 + 1e-45, (b, probs[b], prob)
+
+
+def logits(g, B, V, dtype, sd=2.0):
+    return (g.standard_normal((B, V)) * sd + 10 * g.random((B, V)) ** 300).astype(dtype)
+
+
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 63, 1000, 1025, 16383, 32000, 32001, 32768, 65535, 100003, 131072, 262144])
+def test_every_setting(pk, dtype, V):
+    g = np.random.default_rng(V)
+    B = 12 if V < 40000 else 6
+    x = logits(g, B, V, dtype)
+    u = g.random(B)
+    t = (0.5 + g.random(B)).astype(F32)
+    check(pk, x, u)
+    check(pk, x, u, t=t, p=(0.5 + 0.5 * g.random(B)).astype(F32))
+    check(pk, x, u, t=t, k=g.integers(0, 200, B))
+    check(pk, x, u, t=0.7, k=max(2, V // 3), p=0.9, gap=13)
+    check(pk, x, u, t=t, least=(0.2 * g.random(B)).astype(F32))
+    check(pk, x, u, t=t, k=40, p=0.95, least=0.01, gap=3)
+    check(pk, x, u, t=np.where(np.arange(B) % 3 == 0, 0, t), k=np.where(np.arange(B) % 2 == 0, 0, 50), p=np.where(np.arange(B) % 4 == 1, 1, 0.8).astype(F32),
+          least=np.where(np.arange(B) % 5 == 0, 0.1, 0).astype(F32))
+
+
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+@pytest.mark.parametrize("V", [5, 1000, 32000, 90001, 262144])
+def test_equal_logits(pk, dtype, V):
+    """n equal ones are kept, the lowest indexes: the token is floor(u n).  (More members of a
+    bucket than its list holds.)"""
+    import torch
+    B = 16
+    g = np.random.default_rng(V)
+    x = torch.full((B, V), 3.25, dtype=torch.float16 if dtype == np.float16 else torch.float32, device="cuda")
+    u = g.random(B).astype(F32)
+    u[:3] = [0.0, 1 - 2.0 ** -24, 0.5]
+
+    def tokens(n, **kw):
+        got, probs = pk.apex4_sample(x, dev(u), **kw)
+        assert np.array_equal(got.cpu().numpy(), [int(float(v) * n) for v in u.astype(np.float64)])
+        assert np.array_equal(probs.cpu().numpy(), np.full(B, 1 / n, F32))
+    tokens(V)
+    tokens(V, temperature=0.3, min_p=1.0)
+    for k in {2, max(2, V // 2), max(2, V - 1), V, V + 5}:
+        tokens(min(k, V), top_k=k)
+    for p in (0.25, 0.5, 0.75):  # exact in binary: ceil(p V) of them
+        tokens(int(np.ceil(p * V)), top_p=p)
+        tokens(int(np.ceil(p * max(2, V // 2))), top_p=p, top_k=max(2, V // 2))
+
+
+def test_two_values(pk):
+    """Ties on both sides of the border, spread over the row."""
+    import torch
+    g = np.random.default_rng(3)
+    for V in (3000, 50000):
+        high = g.permutation(V)[:V // 5]
+        x = np.full((1, V), 1.0, np.float16)
+        x[0, high] = 2.0
+        low = np.setdiff1d(np.arange(V), high)
+        for extra in (1, 2, 257, len(low) - 1):
+            keep = np.sort(np.concatenate((high, np.sort(low)[:extra])))
+            e = np.exp(-1.0)
+            w = np.where(np.isin(keep, high), 1.0, e)
+            for u in (0.0, 0.3, 0.9999, 1 - 2.0 ** -24):
+                want = keep[(np.cumsum(w) <= F32(u) * w.sum()).sum()]
+                got, _ = pk.apex4_sample(dev(x), torch.tensor([u], device="cuda"), top_k=len(high) + extra)
+                assert int(got) == want
+                # a share in the midst of the extra-th one's weight keeps as many
+                share = (len(high) + (extra - 0.5) * e) / (len(high) + len(low) * e)
+                got, _ = pk.apex4_sample(dev(x), torch.tensor([u], device="cuda"), top_p=float(F32(share)))
+                assert int(got) == want
+
+
+def test_largest_logit(pk):
+    """Settings that leave one: the lowest index of equal ones, whatever u is."""
+    g = np.random.default_rng(4)
+    for V in (1, 9, 5000, 70000):
+        x = logits(g, 8, V, np.float16)
+        x[:, V // 2] = x[:, V - 1] = 60.0
+        x[5] = -0.0
+        x[5, V // 3] = 0.0
+        want = [V // 2] * 8
+        want[5] = 0
+        for kw in (dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(top_k=1), dict(top_p=0.0),
+                   dict(top_p=-0.5), dict(min_p=1.5)):
+            tokens, probs = pk.apex4_sample(dev(x), dev(g.random(8).astype(F32)), **kw)
+            assert tokens.tolist() == want and probs.tolist() == [1.0] * 8, kw
+
+
+def test_masked_rows(pk):
+    """-inf and NaN are never chosen; nothing else gives -1."""
+    import torch
+    g = np.random.default_rng(5)
+    for V in (40, 5001, 70000):
+        x = np.full((6, V), -np.inf, F32)
+        x[1] = np.nan
+        x[2, V - 3] = -5.0
+        x[3, ::7] = g.standard_normal(len(x[3, ::7]))
+        x[3, 1::7] = np.nan
+        x[4, 5], x[4, 6] = 1e30, -1e30
+        x[5, :] = -3e38
+        for dtype in (np.float32, np.float16):
+            y = x.astype(dtype) if dtype == np.float32 else np.clip(x, -65504, 65504, where=np.isfinite(x), out=x.copy()).astype(dtype)
+            for kw in (dict(), dict(k=3), dict(p=0.6), dict(t=0.0), dict(k=5, p=0.5, least=0.01)):
+                check(pk, y, g.random(6), **kw)
+            tokens, probs = pk.apex4_sample(dev(y), torch.rand(6, device="cuda"))
+            assert tokens[:3].tolist() == [-1, -1, V - 3] and probs[:3].tolist() == [0.0, 0.0, 1.0]
+
+
+def test_infinite_logits(pk):
+    """They share all of the weight."""
+    x = np.zeros((3, 300), F32)
+    x[:, [7, 100, 299]] = np.inf
+    for kw in (dict(), dict(top_k=5), dict(top_p=0.99), dict(min_p=0.5), dict(temperature=float("inf"))):
+        tokens, probs = pk.apex4_sample(dev(x), dev(np.array([0.1, 0.5, 0.9], F32)), **kw)
+        assert tokens.tolist() == [7, 100, 299] and np.allclose(probs.cpu().numpy(), 1 / 3, rtol=1e-6)
+
+
+def test_extreme_settings(pk):
+    g = np.random.default_rng(6)
+    x = logits(g, 4, 3001, F32)
+    for t in (1e-38, 1e-5, 0.01, 30.0, 1e5):
+        check(pk, x, g.random(4), t=t)
+        check(pk, x, g.random(4), t=t, p=0.9, k=1000)
+    check(pk, (x * 1e37).astype(F32), g.random(4), t=1e38)   # differences past binary32's range
+    check(pk, (x * 1e38).clip(-3e38, 3e38).astype(F32), g.random(4), t=1e38, p=0.8)
+    tokens, probs = pk.apex4_sample(dev(x), dev(np.array([0.0, 0.25, 0.5, 1 - 2.0 ** -24], F32)), temperature=float("inf"))
+    assert tokens.tolist() == [0, 750, 1500, 3000]
+    # off: NaN, numbers that keep everything
+    u = dev(g.random(4).astype(F32))
+    want = pk.apex4_sample(dev(x), u)[0]
+    for kw in (dict(top_p=float("nan")), dict(min_p=float("nan")), dict(top_p=2.0), dict(min_p=-1.0), dict(top_k=-5), dict(top_k=3001), dict(top_k=1 << 40)):
+        assert pk.apex4_sample(dev(x), u, **kw)[0].equal(want), kw
+
+
+def test_random_numbers_at_the_borders(pk):
+    import torch
+    g = np.random.default_rng(7)
+    x = logits(g, 8, 2000, np.float16)
+    x[:, 0] = -np.inf
+    x[:, -1] = -np.inf
+    u = [0.0, -1.0, float("nan"), 1.0, 7.0, float("inf"), 1 - 2.0 ** -24, 1e-38]
+    tokens, _ = pk.apex4_sample(dev(x), torch.tensor(u, device="cuda"))
+    assert tokens[:6].tolist() == [1, 1, 1, 1998, 1998, 1998] and int(tokens[7]) == 1
+    check(pk, x, u)
+
+
+def test_many_rows(pk):
+    g = np.random.default_rng(8)
+    x = logits(g, 700, 301, np.float16)
+    check(pk, x, g.random(700), t=(0.3 + g.random(700)).astype(F32), p=0.9)
+
+
+def test_settings_for_all_rows_or_each(pk):
+    import torch
+    g = np.random.default_rng(9)
+    x, u = dev(logits(g, 5, 900, np.float16)), dev(g.random(5).astype(F32))
+    a = pk.apex4_sample(x, u, temperature=0.8, top_k=30, top_p=0.9, min_p=0.02)
+    each = [torch.full((5,), v, device="cuda", dtype=torch.int32 if v == 30 else torch.float32) for v in (0.8, 30, 0.9, 0.02)]
+    b = pk.apex4_sample(x, u, *each)
+    assert a[0].equal(b[0]) and a[1].equal(b[1])
+    tokens, probs = torch.full((7,), 9, dtype=torch.int32, device="cuda"), torch.full((7,), 9.0, device="cuda")
+    pk.apex4_sample(x, u, *each, tokens=tokens[:5], probs=probs[:5])
+    assert tokens[:5].equal(a[0]) and probs[:5].equal(a[1]) and tokens[5:].tolist() == [9, 9] and probs[5:].tolist() == [9.0, 9.0]
+    none = pk.apex4_sample(x[:0], u[:0])
+    assert none[0].shape == (0,) and none[1].shape == (0,)
+
+
+def test_captured_and_on_another_stream(pk):
+    import torch
+    g = np.random.default_rng(10)
+    for V in (3000, 70000):
+        x, u = dev(logits(g, 6, V, np.float16)), dev(g.random(6).astype(F32))
+        p = torch.full((6,), 0.9, device="cuda")
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        eager = pk.apex4_sample(x, u, top_p=p, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = pk.apex4_sample(x, u, top_p=p)
+        for i in range(4):
+            out[0].fill_(-7)
+            graph.replay()
+            want = pk.apex4_sample(x, u, top_p=p)
+            assert out[0].equal(want[0]) and out[1].equal(want[1])
+            if i == 0:
+                assert out[0].equal(eager[0])
+            u.copy_(torch.rand(6, device="cuda"))
+            p.mul_(0.9)
