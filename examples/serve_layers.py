@@ -1,13 +1,15 @@
 """A small serving loop: decoder layers of W4A4 linears over a paged key-value cache.
 
-Prompts of several lengths are taken in (append, then attention of the packed
-tokens), tokens are decoded one a sequence (the step captured into a HIP graph and
-replayed), a sequence forks into two that go on by themselves, one ends, and the
-cache is compacted.  Weights are random and there are no position embeddings: it
-shows how the calls go together, and times them.
+Prompts of several lengths are taken in (append with rotary positions, then attention
+of the packed tokens), tokens are decoded one a sequence (the step captured into a HIP
+graph and replayed), a sequence forks into two that go on by themselves, one ends, and
+the cache is compacted.  The output head is a linear in 8 bits, and the next tokens are
+sampled from its logits (temperature 0: the largest).  Weights are random: it shows how
+the calls go together, and times them.
 
     python examples/serve_layers.py [--layers 4] [--batch 8] [--prompt 500] [--steps 32]
                                     [--cache fp16|int4] [--window 0] [--sinks 0]
+                                    [--temperature 0] [--top-k 0] [--top-p 1] [--min-p 0]
 """
 from __future__ import annotations
 
@@ -53,15 +55,25 @@ class Layer:
 
 class Model:
     def __init__(self, layers=4, hidden=1024, heads=8, kv_heads=2, head_dim=128, inner=2816, vocab=4096, slots=16,
-                 pages=1024, page=16, max_len=2048, cache="fp16", window=0, sinks=0, seed=0):
+                 pages=1024, page=16, max_len=2048, cache="fp16", window=0, sinks=0, seed=0, temperature=0.0, top_k=0, top_p=1.0,
+                 min_p=0.0):
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.layers = [Layer(hidden, heads, kv_heads, head_dim, inner, g) for _ in range(layers)]
         self.embed = torch.empty((vocab, hidden), dtype=torch.float16, device="cuda").normal_(0.0, 1.0, generator=g)
         self.cache = apex4.PagedKVCache(layers, pages, slots, kv_heads, head_dim, page, max_len, cache)
         self.mask = {"window": window, "sinks": sinks}
+        self.freq, _ = apex4.apex4_rope_freq(head_dim)
+        self.lm_head = apex4.W8A8Linear(torch.empty((vocab, hidden), dtype=torch.float16, device="cuda").normal_(0.0, hidden ** -0.5, generator=g))
+        self.settings = {"temperature": temperature, "top_k": top_k, "top_p": top_p, "min_p": min_p}
+        self.generator = torch.Generator(device="cuda").manual_seed(seed + 1)
+        self.u = torch.zeros(slots, device="cuda")  # a random number for each sequence of a step
+
+    def draw(self):
+        self.u.uniform_(generator=self.generator)
 
     def head(self, x):
-        return (norm(x) @ self.embed.t()).argmax(dim=-1)
+        tokens, _ = apex4.apex4_sample(self.lm_head(norm(x)), self.u[:x.shape[0]], **self.settings)
+        return tokens.long()
 
     def take_in(self, prompts, seqs):
         """Prompts (lists of token numbers) into the empty slots seqs; the next tokens."""
@@ -73,8 +85,9 @@ class Model:
         x = self.embed[torch.tensor([t for p in prompts for t in p], device="cuda")]
         for i, layer in enumerate(self.layers):
             q, k, v = layer.split(x)
-            self.cache.append(i, k, v, batch, start)
+            q = self.cache.append_rope(i, q, k, v, batch, self.freq, start)
             x = layer.finish(x, self.cache.prefill(i, q, batch, start, max(n), **self.mask))
+        self.draw()
         return self.head(x[start[1:].long() - 1])
 
     def step(self, tokens, batch):
@@ -82,7 +95,7 @@ class Model:
         x = self.embed[tokens]
         for i, layer in enumerate(self.layers):
             q, k, v = layer.split(x)
-            self.cache.append(i, k, v, batch)
+            q = self.cache.append_rope(i, q, k, v, batch, self.freq)
             x = layer.finish(x, self.cache.decode(i, q, batch, **self.mask))
         return self.head(x)
 
@@ -106,6 +119,7 @@ class Model:
         with torch.cuda.graph(graph):
             following = self.step(current, (table, kv_len))
         for i in range(steps):
+            self.draw()
             graph.replay()
             out[i] = following
             current.copy_(following)
@@ -144,14 +158,17 @@ def serve(layers=4, batch=8, prompt=500, steps=32, cache="fp16", window=0, sinks
     live = int(model.cache.compact().item())
     say(f"{live} pages in use")
     more = model.decode(torch.cat((tokens[-1][:len(seqs)], tokens[-1][:1])), [*seqs, spare], [*lens, lens[0]], steps)
-    assert torch.equal(more[:, 0], more[:, -1]), "a fork without a change goes on as its parent"
+    if not model.settings["temperature"] > 0:
+        assert torch.equal(more[:, 0], more[:, -1]), "a fork without a change goes on as its parent"
     return first, tokens, more
 
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    for name, value in (("layers", 4), ("batch", 8), ("prompt", 500), ("steps", 32), ("window", 0), ("sinks", 0)):
+    for name, value in (("layers", 4), ("batch", 8), ("prompt", 500), ("steps", 32), ("window", 0), ("sinks", 0), ("top-k", 0)):
         ap.add_argument(f"--{name}", type=int, default=value)
+    for name, value in (("temperature", 0.0), ("top-p", 1.0), ("min-p", 0.0)):
+        ap.add_argument(f"--{name}", type=float, default=value)
     ap.add_argument("--cache", choices=sorted(apex4.KV_CACHES), default="fp16")
     serve(**vars(ap.parse_args()))
 
