@@ -45,7 +45,7 @@ constexpr int kBuckets = 736;          // 1/16 octave each
 constexpr int kStageBytes = 128 << 10; // of a row in LDS
 constexpr int kLdsBytes = 160 << 10, kMostList = 9216;
 constexpr int kDepth = 4, kRingBytes = kWaves * kDepth * 1024;
-constexpr int kSteps = 64;             // table of 2^(i / 64)
+constexpr int kSteps = 128, kStepBits = 7;  // table of 2^(45 + i / 128)
 constexpr double kMagic = 0x1.8p52;    // added to a number below 2^51: its nearest whole one in the low bits
 constexpr float kNothing = -__builtin_inff();
 
@@ -85,7 +85,7 @@ __device__ __forceinline__ u32x4 read_lds(uint32_t at) {
 __device__ __forceinline__ void copy_to_lds(uint32_t to, uint32_t off, const uint8_t* base) {
     const uint64_t at = reinterpret_cast<uint64_t>(base);
     const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off),
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
                  "s"(static_cast<uint64_t>(hi) << 32 | lo)
                  : "memory", "m0");
 }
@@ -124,7 +124,13 @@ struct Row {
         if constexpr (F16) return __half2float(__ushort_as_half(static_cast<unsigned short>(j & 1 ? v[j >> 1] >> 16 : v[j >> 1] & 0xFFFFu)));
         else return __uint_as_float(v[j]);
     }
-    __device__ __forceinline__ float finite(float x) const { return infinite ? (x == -kNothing ? 0.f : kNothing) : x; }
+    __device__ __forceinline__ float finite(float x) const {
+        if (infinite) {
+            asm volatile("");  // a branch of the whole wave, not three instructions for every logit
+            x = x == -kNothing ? 0.f : kNothing;
+        }
+        return x;
+    }
     // Logit i of the row.
     __device__ __forceinline__ float at(int i) const {
         const void* p = STAGED ? static_cast<const void*>(staged) : base;
@@ -176,24 +182,22 @@ struct Row {
     // overflow).  NaN and -infinity are not below kBuckets: they are not live.
     __device__ __forceinline__ float below(float x) const { return fmaf(-0.5f, x, half) * c32; }
     __device__ __forceinline__ static bool live(float y) { return y < static_cast<float>(kBuckets); }
-    // 2^45 2^y for y = (x - max) c, not below -60, in binary64: y 64 = k + f, |f| <= 1/2, a power of two,
-    // the table's 2^(k % 64 / 64), and e^(f ln 2 / 64) by its series, whose terms from the
-    // third on (2^-25 and less) need binary32 alone.
+    // 2^45 2^y for y = (x - max) c, not below -60, in binary64: 128 y = k + f, |f| <= 1/2, a
+    // power of two, the table's 2^(k % 128 / 128), and e^r, r = f ln 2 / 128, by its series: the
+    // terms of r^3 and r^4 (2^-28 and less) in binary32, what follows is below 2^-49.
     __device__ __forceinline__ double weight(float x) const {
         const double y = (static_cast<double>(x) - max) * c64, t = y + kMagic, f = y - (t - kMagic);
         const int k = static_cast<int>(__double_as_longlong(t));
         constexpr double l = 0.69314718055994530942 / kSteps;
         const float g = static_cast<float>(f);
-        const float tail = g * g * g * static_cast<float>(l * l * l / 6) *
-                           fmaf(g, fmaf(g, static_cast<float>(l * l / 20), static_cast<float>(l / 4)), 1.f);
-        const double p = fma(f, fma(f, l * l / 2, l), static_cast<double>(tail));
-        const double a = table[k & (kSteps - 1)];
-        const double b = __longlong_as_double(__double_as_longlong(a) + (static_cast<long long>((k >> 6) + 45) << 52));
-        return fma(b, p, b);
+        const float tail = g * g * (g * fmaf(g, static_cast<float>(l * l * l * l / 24), static_cast<float>(l * l * l / 6)));
+        const double p = fma(f, fma(f, l * l / 2, l), static_cast<double>(tail)), a = table[k & (kSteps - 1)];
+        return ldexp(fma(a, p, a), k >> kStepBits);
     }
-    __device__ __forceinline__ static u64 whole(double w) {  // 0 .. 2^45
-        return static_cast<u64>(__double_as_longlong(w + 0x1p52)) & 0x000FFFFFFFFFFFFFull;
-    }
+    static constexpr u64 kZero = 0x4330000000000000ull;  // the bits of 2^52
+    // The bits of 2^52 + w: w rounded to a whole number, 0 .. 2^45, above kZero.
+    __device__ __forceinline__ static u64 above(double w) { return static_cast<u64>(__double_as_longlong(w + 0x1p52)); }
+    __device__ __forceinline__ static u64 whole(double w) { return above(w) - kZero; }
 };
 
 template <int CTRL, int ROWS>
@@ -291,7 +295,7 @@ enum Held : int { kNoList, kBucket, kAll };
 // not behind the first's.  parts: the waves' sums of the kept weights before the bucket are
 // left in sm.part_w (min-p's `least` included) where the list holds the bucket alone.
 template <class R>
-__device__ Border search(Shared& sm, const R& row, u64* list, uint32_t room, const Target& target, bool weigh, bool parts, double least,
+__device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, uint32_t room, const Target& target, bool weigh, bool parts, double least,
                          int& held, uint32_t& listed) {
     const int tid = threadIdx.x;
     find_bin(sm, tid < kBuckets ? sm.bucket_n[tid] : 0u, tid < kBuckets ? sm.bucket_w[tid] : 0ull, 0u, 0ull, target);
@@ -336,17 +340,21 @@ __device__ Border search(Shared& sm, const R& row, u64* list, uint32_t room, con
             });
         } else if (held == kBucket) {
             row.each_piece([&](const float(&x)[R::kVec], int i) {
-                uint32_t wanted = 0;
+                uint32_t wanted = 0, before = 0;
 #pragma unroll
                 for (int j = 0; j < R::kVec; ++j) {
                     const float y = row.below(x[j]);
                     wanted |= y >= top && y < end ? 1u << j : 0u;
-                    if (parts && y < top) {
-                        const double w = row.weight(x[j]);
-                        if (w >= least) sum += R::whole(w);
-                    }
+                    before |= y < top ? 1u << j : 0u;
                 }
                 if (__any(wanted)) append(wanted, x, i);
+                if (!parts || !__any(before)) return;
+#pragma unroll
+                for (int j = 0; j < R::kVec; ++j) {  // of what is not summed the weight is any number
+                    const double w = row.weight(x[j]);
+                    sum += (before >> j & 1 && w >= least ? R::above(w) : R::kZero) - R::kZero;
+                    if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
             });
         } else {
             row.each([&](float x, int) {
@@ -501,7 +509,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
         sm.bucket_n[tid] = 0u;
         sm.bucket_w[tid] = 0ull;
     }
-    if (tid < kSteps) sm.table[tid] = exp2(tid * (1.0 / kSteps));
+    if (tid < kSteps) sm.table[tid] = exp2(45.0 + tid * (1.0 / kSteps));
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) larger(sm.wave_max[i]);
@@ -512,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
         }
         return;
     }
-    row.infinite = m == -kNothing;
+    row.infinite = __builtin_amdgcn_readfirstlane(m == -kNothing);
     if (row.infinite) m = 0.f;
     // settings that leave the first alone: the largest logit, the lowest index of equal ones
     if (!(t > 0.f) || k == 1 || p <= 0.f || least > 1.f) {
@@ -553,11 +561,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
         group_sum(sm, n, w);
         __syncthreads();
         border.sum = w;
-        if (by_k && static_cast<uint32_t>(k) < n)
-            border = search(sm, row, list, room, Target{Target::kCount, static_cast<uint32_t>(k), 0.0, 0ull}, by_p, !by_p, floor_w, held, listed);
-        if (by_p)
-            border = search(sm, row, list, room, Target{Target::kShare, 0u, static_cast<double>(p) * static_cast<double>(border.sum), 0ull}, true, true,
-                            floor_w, held, listed);
+        for (int i = 0; i < 2; ++i) {  // top-k, then top-p of what it keeps
+            if (!(i ? by_p : by_k && static_cast<uint32_t>(k) < n)) continue;
+            const Target target = {i ? Target::kShare : Target::kCount, static_cast<uint32_t>(k), static_cast<double>(p) * static_cast<double>(border.sum), 0ull};
+            border = search(sm, row, list, room, target, by_p, i || !by_p, floor_w, held, listed);
+        }
     }
 
     // 4: the token.  The weight of a logit if it is kept, or 0: above `low`, and not one of
@@ -619,7 +627,24 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     } else {
         u64 sum = 0;
         uint32_t none = 0;
-        row.each([&](float x, int i) { sum += kept(x, i); });
+        const bool ties = border.last < a.V;
+        row.each_piece([&](const float(&x)[R::kVec], int i) {
+            uint32_t in = 0;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j) in |= x[j] > low ? 1u << j : 0u;
+            if (ties) {
+#pragma unroll
+                for (int j = 0; j < R::kVec; ++j)
+                    if (x[j] == tied && i + j > border.last) in &= ~(1u << j);
+            }
+            if (!__any(in)) return;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j) {
+                const double w = row.weight(x[j]);
+                sum += (in >> j & 1 && w >= floor_w ? R::above(w) : R::kZero) - R::kZero;
+                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // eight side by side do not fit the registers
+            }
+        });
         wave_scan(none, sum);
         if (lane == 63) sm.part_w[wave] = sum;
     }
