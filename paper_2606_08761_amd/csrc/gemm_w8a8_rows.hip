@@ -6,7 +6,7 @@
 // the columns; 16 R tokens), D pieces ahead.  The waves' integer sums meet in LDS at the
 // end: exact in any order.
 //
-// FUSED: a single token is quantized by every workgroup itself, into LDS, while its first
+// With SLOTS a single token is quantized by every workgroup itself, into LDS, while its first
 // weights are on their way; otherwise the codes come from the quantizer's buffer.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -22,15 +22,17 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kPiece = 128;
-constexpr int kSlots = 8, kMostFused = kThreads * kSlots * 8;  // of 8 values a thread: K of a token that is quantized on the way
+constexpr int kMostFused = kThreads * 8 * 8;  // K of a token that is quantized on the way
 constexpr uint32_t kNowhere = 0xFFFFFFFFu;  // past any buffer: such loads give zeros
 constexpr int kRsrcFlags = 0x00027000;      // raw buffer descriptor, 32-bit data format
 
-template <int R, int C, int D, bool FUSED>
+// SLOTS: of 8 values a thread, of a token that is quantized on the way; 0: none is.
+template <int R, int C, int D, int SLOTS>
 __global__ __launch_bounds__(kThreads) void w8a8_rows_kernel(const int8_t* __restrict__ A, const float* __restrict__ sa,
                                                              const uint16_t* __restrict__ x, const int8_t* __restrict__ W,
                                                              const float* __restrict__ sw, int M, int N, int K,
                                                              uint16_t* __restrict__ Y) {
+    constexpr bool FUSED = SLOTS > 0;
     extern __shared__ __align__(16) uint8_t smem[];  // FUSED: the token's codes; then the sums
     __shared__ uint32_t red[FUSED ? kWaves : 1];
     const int n0 = blockIdx.x * 16 * C, tid = threadIdx.x;
@@ -60,11 +62,11 @@ __global__ __launch_bounds__(kThreads) void w8a8_rows_kernel(const int8_t* __res
         }
     };
     // FUSED: the token first, since loads come back in order
-    u32x4 v[FUSED ? kSlots : 1];
+    u32x4 v[FUSED ? SLOTS : 1];
     if constexpr (FUSED) {
         const u32x4* xr = reinterpret_cast<const u32x4*>(x);
 #pragma unroll
-        for (int j = 0; j < kSlots; ++j) {
+        for (int j = 0; j < SLOTS; ++j) {
             v[j] = u32x4{0u, 0u, 0u, 0u};
             if (tid + j * kThreads < K / 8) v[j] = xr[tid + j * kThreads];
         }
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void w8a8_rows_kernel(const int8_t* __res
     if constexpr (FUSED) {
         uint32_t am = 0;
 #pragma unroll
-        for (int j = 0; j < kSlots; ++j) {
+        for (int j = 0; j < SLOTS; ++j) {
             const uint32_t b = quant::absmax8_bits(make_uint4(v[j][0], v[j][1], v[j][2], v[j][3]));
             am = am > b ? am : b;
         }
@@ -88,10 +90,19 @@ __global__ __launch_bounds__(kThreads) void w8a8_rows_kernel(const int8_t* __res
         for (int i = 0; i < kWaves; ++i) am = am > red[i] ? am : red[i];
         const Scale sc = scale_of(am);
         s_token = sc.s;
+        auto put = [&](int i, u32x4 t) {  // whole pieces: zeros behind K
+            if (i < pieces * (kPiece / 8)) *reinterpret_cast<u32x2*>(smem + 8 * i) = codes8(t, sc);
+        };
+        if constexpr (SLOTS <= 2) {
 #pragma unroll
-        for (int j = 0; j < kSlots; ++j) {  // whole pieces: zeros behind K
-            if (tid + j * kThreads < pieces * (kPiece / 8)) *reinterpret_cast<u32x2*>(smem + 8 * (tid + j * kThreads)) = codes8(v[j], sc);
-            __builtin_amdgcn_sched_barrier(0);  // slot after slot: side by side they take the registers of a second workgroup
+            for (int j = 0; j < SLOTS; ++j) put(tid + j * kThreads, v[j]);
+        } else {  // read once more: kept, they take the registers of a second workgroup
+#pragma unroll 1
+            for (int i = tid; i < pieces * (kPiece / 8); i += kThreads) {
+                u32x4 t = {0u, 0u, 0u, 0u};
+                if (i < K / 8) t = reinterpret_cast<const u32x4*>(x)[i];
+                put(i, t);
+            }
         }
         __syncthreads();
     }
@@ -147,11 +158,11 @@ __global__ __launch_bounds__(kThreads) void w8a8_rows_kernel(const int8_t* __res
     }
 }
 
-template <int R, int C, int D, bool FUSED>
+template <int R, int C, int D, int SLOTS>
 hipError_t run(const int8_t* A, const float* sa, const uint16_t* x, const int8_t* W, const float* sw, int M, int N, int K, uint16_t* Y, hipStream_t st) {
-    const int sums = kWaves * C * R * 64 * 16, codes = FUSED ? (K + kPiece - 1) / kPiece * kPiece : 0;
+    const int sums = kWaves * C * R * 64 * 16, codes = SLOTS ? (K + kPiece - 1) / kPiece * kPiece : 0;
     static_assert(kWaves * C * R * 64 * 16 <= 65536 && kMostFused <= 65536, "no more LDS than any launch may have");
-    w8a8_rows_kernel<R, C, D, FUSED><<<dim3(static_cast<unsigned>((N + 16 * C - 1) / (16 * C))), dim3(kThreads), sums > codes ? sums : codes, st>>>(
+    w8a8_rows_kernel<R, C, D, SLOTS><<<dim3(static_cast<unsigned>((N + 16 * C - 1) / (16 * C))), dim3(kThreads), sums > codes ? sums : codes, st>>>(
         A, sa, x, W, sw, M, N, K, Y);
     return hipGetLastError();
 }
@@ -166,11 +177,12 @@ bool w8a8_rows_fits(int64_t M, int64_t N) { return M <= 8 || (M <= 32 && N <= 16
 bool w8a8_fused_fits(int64_t M, int64_t K) { return M == 1 && K <= kMostFused; }
 
 hipError_t launch_w8a8_rows(const int8_t* A, const float* sa, const int8_t* W, const float* sw, int M, int N, int K, uint16_t* Y, hipStream_t st) {
-    if (M <= 16) return run<1, 1, 4, false>(A, sa, nullptr, W, sw, M, N, K, Y, st);
-    return run<2, 1, 4, false>(A, sa, nullptr, W, sw, M, N, K, Y, st);
+    if (M <= 16) return run<1, 1, 4, 0>(A, sa, nullptr, W, sw, M, N, K, Y, st);
+    return run<2, 1, 4, 0>(A, sa, nullptr, W, sw, M, N, K, Y, st);
 }
 hipError_t launch_w8a8_fused(const uint16_t* x, const int8_t* W, const float* sw, int N, int K, uint16_t* Y, hipStream_t st) {
-    return run<1, 1, 4, true>(nullptr, nullptr, x, W, sw, 1, N, K, Y, st);
+    if (K <= kThreads * 16) return run<1, 1, 4, 2>(nullptr, nullptr, x, W, sw, 1, N, K, Y, st);
+    return run<1, 1, 4, 8>(nullptr, nullptr, x, W, sw, 1, N, K, Y, st);
 }
 
 }  // namespace apex4

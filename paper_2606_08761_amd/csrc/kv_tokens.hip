@@ -14,7 +14,7 @@
 // bytes), back 12.8 us (3.8 TB/s); binary16 there and back 30.4 us (4.8 TB/s).
 //
 // With rotary positions on the way (kv_append_rope_kernel) a lane moves the 16 values
-// of one (token, head) that hold both of every pair, and blockIdx.y 2 turns the queries
+// of one (token, head) that hold both of every pair, and blockIdx.y 0 turns the queries
 // into a buffer of their own: one launch for what stands between a layer's projection
 // and its attention.
 #include <hip/hip_fp16.h>
@@ -181,7 +181,8 @@ __device__ __forceinline__ Spot spot_of(const KvView& c, const int32_t* q_start,
     return s;
 }
 
-// blockIdx.y: 0 keys, 1 values (not turned), 2 queries (into rows of their own).  A
+// blockIdx.y: 0 queries (into rows of their own; the longest first), 1 keys, 2 values (not
+// turned); without queries 1 and 2 are 0 and 1.  A
 // key is turned and rounded to binary16 before it is stored or quantized: what the
 // two calls, one after the other, would give, bit for bit.
 template <int D, bool I4, int FORM>
@@ -192,11 +193,12 @@ __global__ __launch_bounds__(kThreads) void kv_append_rope_kernel(KvView c, Rope
     __shared__ float2 turns[kMost * D / 2];
     const int64_t i0 = static_cast<int64_t>(blockIdx.x) * per;
     const int tokens = static_cast<int>(T - i0 < per ? T - i0 : per);
-    const bool turned = blockIdx.y != 1, cached = blockIdx.y != 2;
+    const int what = static_cast<int>(blockIdx.y) + (a.heads ? 0 : 1);
+    const bool turned = what != 2, cached = what != 0;
     const int heads = cached ? c.kv_heads : a.heads, pairs = r.rot / 2;
-    const uint16_t* src = blockIdx.y == 0 ? a.k : blockIdx.y == 1 ? a.v : a.q;
-    const int64_t stride = blockIdx.y == 0 ? a.k_stride : blockIdx.y == 1 ? a.v_stride : a.q_stride;
-    uint8_t* plane = const_cast<uint8_t*>(blockIdx.y ? c.v : c.k);
+    const uint16_t* src = what == 0 ? a.q : what == 1 ? a.k : a.v;
+    const int64_t stride = what == 0 ? a.q_stride : what == 1 ? a.k_stride : a.v_stride;
+    uint8_t* plane = const_cast<uint8_t*>(what == 2 ? c.v : c.k);
     if (static_cast<int>(threadIdx.x) < tokens) spots[threadIdx.x] = spot_of(c, q_start, T, i0 + threadIdx.x);
     __syncthreads();
     if (turned) {

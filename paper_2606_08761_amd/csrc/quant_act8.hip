@@ -65,19 +65,16 @@ hipError_t run(const uint16_t* x, int64_t M, int slots, int8_t* q, float* s, hip
 
 }  // namespace
 
-// K < 2^17: at most 16384 slots a row.  Few rows: a slot a thread while the workgroup
-// holds that many, so that a row's loads all go out at once; more rows than compute units
-// fill the chip with smaller workgroups.
+// K < 2^17: at most 16384 slots a row.  Two slots a thread keep more rows on a compute
+// unit than four do, one leaves its threads too little to load (4096 rows of 8192: 512
+// threads with two 21.4 us, 4.7 TB/s; 256 with four 24.2, 1024 with one 24.9; few rows: all alike).
 hipError_t launch_quantize8(const uint16_t* x, int64_t M, int64_t K, int8_t* q, float* s, hipStream_t st) {
     const int n = static_cast<int>(K / 8);
     if (n <= 64) return run<64, 1>(x, M, n, q, s, st);
+    if (n <= 128) return run<128, 1>(x, M, n, q, s, st);
     if (n <= 256) return run<256, 1>(x, M, n, q, s, st);
-    if (M > device_cu_count()) {
-        if (n <= 1024) return run<256, 4>(x, M, n, q, s, st);
-        if (n <= 4096) return run<512, 8>(x, M, n, q, s, st);
-    }
-    if (n <= 512) return run<512, 1>(x, M, n, q, s, st);
-    if (n <= 1024) return run<1024, 1>(x, M, n, q, s, st);
+    if (n <= 512) return run<256, 2>(x, M, n, q, s, st);
+    if (n <= 1024) return run<512, 2>(x, M, n, q, s, st);
     if (n <= 4096) return run<1024, 4>(x, M, n, q, s, st);
     return run<1024, 16>(x, M, n, q, s, st);
 }
