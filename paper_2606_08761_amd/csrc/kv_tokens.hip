@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_rope_kernel(KvView c, Rope
                                                                   int64_t T, Rotary r, int per) {
     constexpr int L = D / 16, U = 4;
     __shared__ Spot spots[kMost];
-    __shared__ float2 turns[kMost * D / 2];
+    __shared__ rope::Turn turns[kMost * D / 2];
     const int64_t i0 = static_cast<int64_t>(blockIdx.x) * per;
     const int tokens = static_cast<int>(T - i0 < per ? T - i0 : per);
     const int what = static_cast<int>(blockIdx.y) + (a.heads ? 0 : 1);

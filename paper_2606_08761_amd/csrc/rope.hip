@@ -25,7 +25,7 @@ template <int FORM, int LANES>
 __global__ __launch_bounds__(kThreads) void rope_kernel(const uint16_t* x, int64_t x_stride, const int32_t* __restrict__ positions,
                                                         int64_t T, int heads, int D, Rotary r, uint16_t* out, int64_t out_stride,
                                                         int per) {
-    __shared__ float2 turns[kMost * kMostPairs];
+    __shared__ Turn turns[kMost * kMostPairs];
     const int64_t i0 = static_cast<int64_t>(blockIdx.x) * per;
     const int tokens = static_cast<int>(T - i0 < per ? T - i0 : per);
     const int pairs = r.rot / 2;
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const uint16_t* x, int64
             }
             const int ea = r.interleaved ? 2 * u : u, eb = r.interleaved ? 2 * u + 1 : u + pairs;
             const float a = h2f(from[ea]), b = h2f(from[eb]);
-            const float2 c = turns[t * pairs + u];
+            const Turn c = turns[t * pairs + u];
             to[ea] = __half_as_ushort(__float2half_rn(first_of(a, b, c)));
             to[eb] = __half_as_ushort(__float2half_rn(second_of(a, b, c)));
         }

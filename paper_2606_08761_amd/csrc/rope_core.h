@@ -5,9 +5,11 @@
 // the pair is (j, j + rot / 2) in the half layout and (2 j, 2 j + 1) in the
 // interleaved one, and the values from rot on stay.  A position of any sign and size
 // has its angle: the turns are a binary64 product, and only what is left past whole
-// turns (exact) goes into the sine, in binary64 too; sine and cosine are rounded to
-// binary32 once, the turned values are binary32 and rounded once more, to binary16.
-// In binary32 the angle of position 10^6 would be off by 2^-5 of a turn's radian.
+// turns (exact) goes into the sine.  Sine, cosine and the turned values are binary64
+// (which the kernels, bound by memory, have the time for), rounded to binary32 and then
+// to binary16: a quarter as many results next to a border fall to its other side as with
+// binary32 sines and products, and a 4-bit code on the way into a cache is decided by
+// such results.  In binary32 the angle of position 10^6 would be off by 2^-5 of a radian.
 #pragma once
 
 #include <hip/hip_fp16.h>
@@ -38,23 +40,28 @@ __host__ __device__ inline int form_of(const Rotary& r, int D) {
 }
 
 // (cos, sin) of pair j at position p, times mag.
-__device__ __forceinline__ float2 turn_of(const Rotary& r, int p, int j) {
+typedef double Turn __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ Turn turn_of(const Rotary& r, int p, int j) {
     const double t = static_cast<double>(p) * r.freq[j];
     double s, c;
     sincospi(2.0 * (t - rint(t)), &s, &c);
-    return make_float2(static_cast<float>(c * r.mag), static_cast<float>(s * r.mag));
+    return Turn{c * r.mag, s * r.mag};
 }
 
 // One order of operations for every kernel, so that their results are the same bits.
-// The compiler may join an fma and its rounding to binary16 into one instruction, which
-// rounds once where two instructions round twice, here and not there; the empty
+// The compiler may join the two roundings into one, here and not there; the empty
 // statement keeps them apart.
-__device__ __forceinline__ float apart(float x) {
-    asm("" : "+v"(x));
-    return x;
+__device__ __forceinline__ float apart(double x) {
+    float y = static_cast<float>(x);
+    asm("" : "+v"(y));
+    return y;
 }
-__device__ __forceinline__ float first_of(float a, float b, float2 t) { return apart(fmaf(a, t.x, -(b * t.y))); }
-__device__ __forceinline__ float second_of(float a, float b, float2 t) { return apart(fmaf(b, t.x, a * t.y)); }
+__device__ __forceinline__ float first_of(float a, float b, Turn t) {
+    return apart(fma(static_cast<double>(a), t.x, -(static_cast<double>(b) * t.y)));
+}
+__device__ __forceinline__ float second_of(float a, float b, Turn t) {
+    return apart(fma(static_cast<double>(b), t.x, static_cast<double>(a) * t.y));
+}
 
 // The pieces (of 8 values) of lane l of a head.
 template <int FORM>
@@ -71,14 +78,14 @@ __device__ __forceinline__ uint32_t both(float a, float b) {
 
 // Turns lane l's two pieces; turns: the token's rot / 2 (cos, sin).
 template <int FORM>
-__device__ __forceinline__ void turn_pieces(const Rotary& r, int l, const float2* turns, u32x4& x, u32x4& y) {
+__device__ __forceinline__ void turn_pieces(const Rotary& r, int l, const Turn* turns, u32x4& x, u32x4& y) {
     if constexpr (FORM == kHalves) {
         if (l >= r.rot / 16) return;
-        const float2* t = turns + 8 * l;
+        const Turn* t = turns + 8 * l;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float a0 = low(x[i]), a1 = high(x[i]), b0 = low(y[i]), b1 = high(y[i]);
-            const float2 t0 = t[2 * i], t1 = t[2 * i + 1];
+            const Turn t0 = t[2 * i], t1 = t[2 * i + 1];
             x[i] = both(first_of(a0, b0, t0), first_of(a1, b1, t1));
             y[i] = both(second_of(a0, b0, t0), second_of(a1, b1, t1));
         }
@@ -87,7 +94,7 @@ __device__ __forceinline__ void turn_pieces(const Rotary& r, int l, const float2
         for (int n = 0; n < 2; ++n) {
             if (8 * (2 * l + n) >= r.rot) break;
             u32x4& z = n ? y : x;
-            const float2* t = turns + 4 * (2 * l + n);
+            const Turn* t = turns + 4 * (2 * l + n);
 #pragma unroll
             for (int i = 0; i < 4; ++i) z[i] = both(first_of(low(z[i]), high(z[i]), t[i]), second_of(low(z[i]), high(z[i]), t[i]));
         }
@@ -95,7 +102,7 @@ __device__ __forceinline__ void turn_pieces(const Rotary& r, int l, const float2
 }
 
 // Value e of a head's row (kSingles).
-__device__ __forceinline__ uint32_t turned_value(const Rotary& r, const uint16_t* row, int e, const float2* turns) {
+__device__ __forceinline__ uint32_t turned_value(const Rotary& r, const uint16_t* row, int e, const Turn* turns) {
     if (e >= r.rot) return row[e];
     const int half = r.rot / 2;
     const bool second = r.interleaved ? e & 1 : e >= half;
@@ -103,7 +110,7 @@ __device__ __forceinline__ uint32_t turned_value(const Rotary& r, const uint16_t
     const float a = h2f(row[r.interleaved ? e & ~1 : j]), b = h2f(row[r.interleaved ? e | 1 : j + half]);
     return __half_as_ushort(__float2half_rn(second ? second_of(a, b, turns[j]) : first_of(a, b, turns[j])));
 }
-__device__ __forceinline__ u32x4 turned_piece(const Rotary& r, const uint16_t* row, int piece, const float2* turns) {
+__device__ __forceinline__ u32x4 turned_piece(const Rotary& r, const uint16_t* row, int piece, const Turn* turns) {
     u32x4 z;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
