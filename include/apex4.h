@@ -630,15 +630,19 @@ int apex4_pages_copy(void* pool, int64_t planes, int64_t page_bytes, int64_t n_p
  * Weights are binary64 and summed exactly, in units of 2^-45 of the largest: the outcome
  * is a function of the row and its settings alone.  Logits below 2^-46 of the largest
  * weight count as never chosen.
- * logits 16-byte aligned, the others 4-byte; the aligned 16-byte pieces that hold a row's
- * logits are read whole.  B up to 2^21, V up to 2^18.
+ *   workspace: apex4_sample_workspace_size bytes, 16-byte aligned (NULL where that is 0); calls
+ *   that share one must be ordered on one stream.  Where rows are few and long,
+ *   several workgroups share each.
+ * logits aligned like their type (the
+ * aligned 16-byte pieces that hold a row's logits are read whole), the others 4-byte.  B up to 2^21, V up to 2^18.
  */
 #define APEX4_LOGITS_FP16 0
 #define APEX4_LOGITS_FP32 1
+int apex4_sample_workspace_size(int type, int64_t B, int64_t V, int64_t* bytes);
 int apex4_sample(const void* logits, int type, int64_t stride, int64_t B, int64_t V, const float* u,
                  const float* temperature, float temperature_all, const int32_t* top_k, int64_t top_k_all,
                  const float* top_p, float top_p_all, const float* min_p, float min_p_all, int32_t* tokens, float* probs,
-                 void* stream);
+                 void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Static description of a status code (never NULL). */
 const char* apex4_status_string(int status);

@@ -45,7 +45,7 @@ EXPORTED = ("apex4_quantize_act", "apex4_w4a4_gemm", "apex4_w4a4_gemm_groupsums"
             "apex4_attn_prefill_workspace_size", "apex4_attn_prefill", "apex4_pages_workspace_size",
             "apex4_pages_reserve", "apex4_pages_fork", "apex4_pages_free", "apex4_pages_compact", "apex4_pages_copy",
             "apex4_rope", "apex4_kv_append_rope", "apex4_quantize_act8", "apex4_w8a8_gemm", "apex4_w8a8_linear",
-            "apex4_sample")
+            "apex4_sample_workspace_size", "apex4_sample")
 
 _lib = None
 
@@ -106,7 +106,8 @@ def lib() -> ctypes.CDLL:
     L.apex4_quantize_act8.argtypes = [P, I, I, P, P, P]
     L.apex4_w8a8_gemm.argtypes = [P, P, P, P, I, I, I, P, P]
     L.apex4_w8a8_linear.argtypes = [P, P, P, I, I, I, P, P, P, P]
-    L.apex4_sample.argtypes = [P, C, I, I, I, P, P, F, P, I, P, F, P, F, P, P, P]
+    L.apex4_sample_workspace_size.argtypes = [C, I, I, P]
+    L.apex4_sample.argtypes = [P, C, I, I, I, P, P, F, P, I, P, F, P, F, P, P, P, I, P]
     for f in EXPORTED:
         getattr(L, f).restype = ctypes.c_int
     L.apex4_status_string.argtypes = [ctypes.c_int]
@@ -601,4 +602,4 @@ from .cache import (KV_CACHES, ROPE_LAYOUTS, PagedKVCache, apex4_attn_decode,  #
                     apex4_pages_copy, apex4_pages_fork, apex4_pages_free, apex4_pages_reserve, apex4_pages_workspace_size)
 from .linear8 import W8A8Linear, apex4_quantize_act8, apex4_w8a8_gemm, apex4_w8a8_linear  # noqa: E402,F401
 from .rotary import apex4_rope, apex4_rope_freq  # noqa: E402,F401
-from .sampling import apex4_sample  # noqa: E402,F401
+from .sampling import apex4_sample, apex4_sample_workspace_size  # noqa: E402,F401

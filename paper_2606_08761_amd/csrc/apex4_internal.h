@@ -193,11 +193,14 @@ struct SampleArgs {
     const float* min_p = nullptr;
     int32_t* tokens = nullptr;           // [B]
     float* probs = nullptr;              // [B] or nullptr
+    void* workspace = nullptr;           // sample_workspace bytes
     int64_t stride = 0;
     int V = 0;
     int top_k_all = 0;
     float temperature_all = 1.f, top_p_all = 1.f, min_p_all = 0.f;
 };
+// Bytes for workgroups that share long rows, where the rows are few (0: none do).
+int64_t sample_workspace(int64_t B, int64_t V, bool f16);
 hipError_t launch_sample(const SampleArgs& a, int64_t B, bool f16, hipStream_t stream);
 
 // A paged key-value cache as the kernels see it (layout: kv_cache.h).

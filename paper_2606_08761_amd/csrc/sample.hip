@@ -43,6 +43,7 @@ typedef unsigned long long u64;
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBuckets = 736;          // 1/16 octave each
 constexpr int kStageBytes = 128 << 10; // of a row in LDS
+constexpr int kSharedLogits = 48 << 10;  // rows from here on are shared where they are few
 constexpr int kLdsBytes = 160 << 10, kMostList = 9216;
 constexpr int kDepth = 4, kRingBytes = kWaves * kDepth * 1024;
 constexpr int kSteps = 128, kStepBits = 7;  // table of 2^(45 + i / 128)
@@ -66,11 +67,25 @@ struct Shared {
     uint32_t listed, low, high, first;
 };
 
+// What the workgroups that share a row leave for the next launch.
+struct Work {
+    u64 part_w[kWaves];
+    u64 bucket_w[kBuckets];
+    u64 list[kMostList];
+    uint32_t bucket_n[kBuckets];
+    float max[kWaves];
+    uint32_t listed, first;
+    uint32_t unused[2];
+};
+static_assert(sizeof(Work) % 16 == 0, "aligned");
+
 __device__ __forceinline__ uint32_t ordered(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);  // -0 as 0
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+// The next number below that of k; below 0 it is not -0, which is not less.
+__device__ __forceinline__ float under(uint32_t k) { return unordered(k == 0x80000000u ? k - 2u : k - 1u); }
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 __device__ __forceinline__ u32x4 read_lds(uint32_t at) {
@@ -102,6 +117,7 @@ struct Row {
     uint32_t ring;         // the ring's place in LDS
     const double* table;
     int skip, V, pieces;   // logits between base and the first; pieces that hold the row
+    int from, to;          // the pieces that the passes go over
     bool infinite;         // the largest logit is infinite: its like count as 0, the others as nothing
     float half, c32;
     double max, c64;
@@ -137,12 +153,12 @@ struct Row {
         if constexpr (F16) return finite(__half2float(__ushort_as_half(static_cast<const uint16_t*>(p)[i + skip])));
         else return finite(static_cast<const float*>(p)[i + skip]);
     }
-    // f(logits, index of the first) for the thread's pieces; wave w has the w-th part() of them,
-    // all its lanes together (a lane without a piece has -infinity).
+    // f(logits, index of the first) for the thread's pieces; wave w has the w-th sixteenth of
+    // them, all its lanes together (a lane without a piece has -infinity).
     template <class F>
     __device__ __forceinline__ void each_piece(F f) const {
         const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = threadIdx.x & 63;
-        const int begin = wave * part(), n = (min(pieces, begin + part()) - begin + 63) / 64;
+        const int part = (to - from + kWaves - 1) / kWaves, begin = from + wave * part, end = min(to, begin + part), n = (end - begin + 63) / 64;
         const uint32_t slots = ring + wave * (kDepth * 1024);
         auto fetch = [&](int it) {
             const int i = min(begin + 64 * it + lane, pieces - 1);
@@ -162,7 +178,7 @@ struct Row {
                 landed_but<kDepth - 1>();  // it is read before its place is loaded again
                 if (it + kDepth < n) fetch(it + kDepth);
             }
-            if (i >= min(pieces, begin + part())) v = u32x4{kNone, kNone, kNone, kNone};
+            if (i >= end) v = u32x4{kNone, kNone, kNone, kNone};
             float x[kVec];
 #pragma unroll
             for (int j = 0; j < kVec; ++j) x[j] = finite(raw(v, j));
@@ -176,7 +192,7 @@ struct Row {
             for (int j = 0; j < kVec; ++j) f(x[j], i + j);
         });
     }
-    __device__ __forceinline__ int part() const { return (pieces + kWaves - 1) / kWaves; }
+    __device__ __forceinline__ int part() const { return (pieces + kWaves - 1) / kWaves; }  // pieces of a part of the row
 
     // 1/16 octaves below the largest: rises as x falls (halves, whose difference cannot
     // overflow).  NaN and -infinity are not below kBuckets: they are not live.
@@ -291,12 +307,64 @@ struct Border {
 // What the list holds: nothing, the bucket of the border, or all down to it.
 enum Held : int { kNoList, kBucket, kAll };
 
-// A border's search.  The list is filled by the first (held < 0); the second one's border is
-// not behind the first's.  parts: the waves' sums of the kept weights before the bucket are
+// Where a search that found its bucket keeps the list, for n logits.
+__device__ __forceinline__ int held_by(uint32_t before, uint32_t members, uint32_t room) {
+    return before + members <= room ? kAll : members <= room ? kBucket : kNoList;
+}
+
+// The logits of the bucket from `top` to `end` (1/16 octaves), or all down to it, into `list`,
+// *listed of them so far; returns the thread's sum of the kept weights before it (parts).
+template <class R>
+__device__ __forceinline__ u64 collect(const R& row, u64* list, uint32_t* listed, uint32_t room, int held, float top, float end, bool parts,
+                                       double least) {
+    // a piece's logits that `wanted` has a bit of, into the list, one count for a wave
+    auto append = [&](uint32_t wanted, const float(&x)[R::kVec], int i) {
+        uint32_t n = __builtin_popcount(wanted), own = n;
+        u64 none = 0;
+        wave_scan(n, none);
+        uint32_t at = 0;
+        if ((threadIdx.x & 63) == 63) at = atomicAdd(listed, n);
+        at = __builtin_amdgcn_readlane(at, 63) + n - own;
+#pragma unroll
+        for (int j = 0; j < R::kVec; ++j)
+            if (wanted >> j & 1 && at < room) list[at++] = static_cast<u64>(ordered(x[j])) << 32 | static_cast<uint32_t>(i + j);
+    };
+    u64 sum = 0;
+    if (held == kAll) {
+        row.each_piece([&](const float(&x)[R::kVec], int i) {
+            uint32_t wanted = 0;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j) wanted |= row.below(x[j]) < end ? 1u << j : 0u;
+            if (__any(wanted)) append(wanted, x, i);
+        });
+    } else {
+        row.each_piece([&](const float(&x)[R::kVec], int i) {
+            uint32_t wanted = 0, before = 0;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j) {
+                const float y = row.below(x[j]);
+                wanted |= y >= top && y < end ? 1u << j : 0u;
+                before |= y < top ? 1u << j : 0u;
+            }
+            if (__any(wanted)) append(wanted, x, i);
+            if (!parts || !__any(before)) return;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j) {  // of what is not summed the weight is any number
+                const double w = row.weight(x[j]);
+                sum += (before >> j & 1 && w >= least ? R::above(w) : R::kZero) - R::kZero;
+                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+    }
+    return sum;
+}
+
+// A border's search.  The list is filled by the first (held < 0), or was by an earlier launch
+// (work: the list, and in sm.part_w the parts); the second one's border is not behind the first's.  parts: the waves' sums of the kept weights before the bucket are
 // left in sm.part_w (min-p's `least` included) where the list holds the bucket alone.
 template <class R>
 __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, uint32_t room, const Target& target, bool weigh, bool parts, double least,
-                         int& held, uint32_t& listed) {
+                         const Work* work, int& held, uint32_t& listed) {
     const int tid = threadIdx.x;
     find_bin(sm, tid < kBuckets ? sm.bucket_n[tid] : 0u, tid < kBuckets ? sm.bucket_w[tid] : 0ull, 0u, 0ull, target);
     const int bucket = sm.bin;
@@ -314,57 +382,24 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
         high = max(high, ordered(x));
     };
     if (held != kAll) {
-        held = before_n + members <= room ? kAll : members <= room ? kBucket : kNoList;
+        const bool ready = held < 0 && work != nullptr;
+        held = held_by(before_n, members, room);
         listed = held == kAll ? before_n + members : members;
         if (tid == 0) sm.listed = 0u;
         __syncthreads();
-        // a piece's logits that `wanted` has a bit of, into the list, one count for a wave
-        auto append = [&](uint32_t wanted, const float(&x)[R::kVec], int i) {
-            uint32_t n = __builtin_popcount(wanted), own = n;
-            u64 none = 0;
-            wave_scan(n, none);
-            uint32_t at = 0;
-            if ((tid & 63) == 63) at = atomicAdd(&sm.listed, n);
-            at = __builtin_amdgcn_readlane(at, 63) + n - own;
-#pragma unroll
-            for (int j = 0; j < R::kVec; ++j)
-                if (wanted >> j & 1 && at < room) list[at++] = static_cast<u64>(ordered(x[j])) << 32 | static_cast<uint32_t>(i + j);
-        };
-        u64 sum = 0;
-        if (held == kAll) {
-            row.each_piece([&](const float(&x)[R::kVec], int i) {
-                uint32_t wanted = 0;
-#pragma unroll
-                for (int j = 0; j < R::kVec; ++j) wanted |= row.below(x[j]) < end ? 1u << j : 0u;
-                if (__any(wanted)) append(wanted, x, i);
-            });
-        } else if (held == kBucket) {
-            row.each_piece([&](const float(&x)[R::kVec], int i) {
-                uint32_t wanted = 0, before = 0;
-#pragma unroll
-                for (int j = 0; j < R::kVec; ++j) {
-                    const float y = row.below(x[j]);
-                    wanted |= y >= top && y < end ? 1u << j : 0u;
-                    before |= y < top ? 1u << j : 0u;
-                }
-                if (__any(wanted)) append(wanted, x, i);
-                if (!parts || !__any(before)) return;
-#pragma unroll
-                for (int j = 0; j < R::kVec; ++j) {  // of what is not summed the weight is any number
-                    const double w = row.weight(x[j]);
-                    sum += (before >> j & 1 && w >= least ? R::above(w) : R::kZero) - R::kZero;
-                    if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                }
-            });
-        } else {
+        if (held == kNoList) {
             row.each([&](float x, int) {
                 const float y = row.below(x);
                 if (y >= top && y < end) member(x);
             });
+        } else if (ready) {
+            for (uint32_t i = tid; i < listed; i += kThreads) list[i] = work->list[i];
+        } else {
+            u64 sum = collect(row, list, &sm.listed, room, held, top, end, parts, least);
+            uint32_t none = 0;
+            wave_scan(none, sum);
+            if ((tid & 63) == 63) sm.part_w[tid >> 6] = sum;
         }
-        uint32_t none = 0;
-        wave_scan(none, sum);
-        if ((tid & 63) == 63) sm.part_w[tid >> 6] = sum;
     }
     __syncthreads();
     if (held != kNoList) {
@@ -462,16 +497,28 @@ __device__ __forceinline__ u64 share_of(float u, u64 total) {
     return shift < 128 ? static_cast<u64>(static_cast<unsigned __int128>(f) * total >> shift) : 0ull;
 }
 
-template <bool F16, bool STAGED>
+// A row is one workgroup's, in one launch, or sixteen workgroups share its passes, in four.
+enum Phase : int {
+    kWhole,
+    kMax,      // pass 1, and the counts are cleared
+    kCount,    // pass 2, or where no border is the parts' sums
+    kCollect,  // pass 3
+    kRest,     // the border inside its bucket, and the token: one workgroup
+};
+
+template <bool F16, bool STAGED, int PHASE>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t room, int list_at) {
     extern __shared__ __align__(16) uint8_t smem[];
     Shared& sm = *reinterpret_cast<Shared*>(smem);
     u64* list = reinterpret_cast<u64*>(smem + list_at);
     using R = Row<F16, STAGED>;
     constexpr int kSize = F16 ? 2 : 4;
+    constexpr bool kShares = PHASE == kMax || PHASE == kCount || PHASE == kCollect;
 
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int64_t b = blockIdx.x;
+    const int64_t b = kShares ? blockIdx.x / kWaves : blockIdx.x;
+    const int share = kShares ? blockIdx.x % kWaves : 0;
+    Work* work = PHASE == kWhole ? nullptr : static_cast<Work*>(a.workspace) + b;
     const uintptr_t at = reinterpret_cast<uintptr_t>(a.logits) + static_cast<uintptr_t>(b * a.stride) * kSize;
     R row;
     row.base = reinterpret_cast<const uint8_t*>(at & ~static_cast<uintptr_t>(15));
@@ -481,6 +528,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     row.skip = static_cast<int>(at & 15) / kSize;
     row.V = a.V;
     row.pieces = (row.skip + a.V + R::kVec - 1) / R::kVec;
+    row.from = kShares ? min(row.pieces, share * row.part()) : 0;
+    row.to = kShares ? min(row.pieces, row.from + row.part()) : row.pieces;
     row.infinite = false;
 
     const float t = a.temperature ? a.temperature[b] : a.temperature_all, p = a.top_p ? a.top_p[b] : a.top_p_all;
@@ -498,12 +547,14 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
 #pragma unroll
             for (int j = 0; j < R::kVec; ++j) larger(R::raw(v, j));
         }
-    } else {
+    } else if constexpr (PHASE == kWhole || PHASE == kMax) {
         row.each([&](float x, int) { larger(x); });
     }
+    if constexpr (PHASE == kWhole || PHASE == kMax) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) larger(__shfl_xor(m, d, 64));
-    if (lane == 0) sm.wave_max[wave] = m;
+        for (int d = 1; d < 64; d <<= 1) larger(__shfl_xor(m, d, 64));
+        if (lane == 0) sm.wave_max[wave] = m;
+    }
     if (tid == 0) sm.first = 0xFFFFFFFFu;
     if (tid < kBuckets) {
         sm.bucket_n[tid] = 0u;
@@ -512,9 +563,25 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     if (tid < kSteps) sm.table[tid] = exp2(45.0 + tid * (1.0 / kSteps));
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) larger(sm.wave_max[i]);
-    if (m == kNothing) {  // nothing can be chosen
+    for (int i = 0; i < kWaves; ++i) larger(PHASE == kWhole || PHASE == kMax ? sm.wave_max[i] : work->max[i]);
+    if constexpr (PHASE == kMax) {
+        constexpr int kEach = (kBuckets + kWaves - 1) / kWaves;
+        if (tid < kEach && share * kEach + tid < kBuckets) {
+            work->bucket_n[share * kEach + tid] = 0u;
+            work->bucket_w[share * kEach + tid] = 0ull;
+        }
         if (tid == 0) {
+            work->max[share] = m;
+            work->part_w[share] = 0ull;
+            if (share == 0) {
+                work->listed = 0u;
+                work->first = 0xFFFFFFFFu;
+            }
+        }
+        return;
+    }
+    if (m == kNothing) {  // nothing can be chosen
+        if (!kShares && tid == 0) {
             a.tokens[b] = -1;
             if (a.probs) a.probs[b] = 0.f;
         }
@@ -524,14 +591,16 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     if (row.infinite) m = 0.f;
     // settings that leave the first alone: the largest logit, the lowest index of equal ones
     if (!(t > 0.f) || k == 1 || p <= 0.f || least > 1.f) {
-        uint32_t first = 0xFFFFFFFFu;
-        row.each([&](float x, int i) {
-            if (x == m) first = min(first, static_cast<uint32_t>(i));
-        });
-        if (first != 0xFFFFFFFFu) atomicMin(&sm.first, first);
-        __syncthreads();
-        if (tid == 0) {
-            a.tokens[b] = static_cast<int>(sm.first);
+        if constexpr (PHASE == kWhole || PHASE == kCount) {
+            uint32_t first = 0xFFFFFFFFu;
+            row.each([&](float x, int i) {
+                if (x == m) first = min(first, static_cast<uint32_t>(i));
+            });
+            if (first != 0xFFFFFFFFu) atomicMin(PHASE == kCount ? &work->first : &sm.first, first);
+            __syncthreads();
+        }
+        if (!kShares && tid == 0) {
+            a.tokens[b] = static_cast<int>(PHASE == kRest ? work->first : sm.first);
             if (a.probs) a.probs[b] = 1.f;
         }
         return;
@@ -548,23 +617,50 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     Border border = {0u, a.V, 0ull};
     int held = -1;
     uint32_t listed = 0;
+    bool found = false;  // a border
     if (by_k || by_p) {
-        row.each([&](float x, int) {
-            const float y = row.below(x);
-            if (!R::live(y)) return;
-            atomicAdd(&sm.bucket_n[static_cast<int>(y)], 1u);
-            if (by_p) atomicAdd(&sm.bucket_w[static_cast<int>(y)], R::whole(row.weight(x)));
-        });
+        if constexpr (PHASE == kWhole || PHASE == kCount) {
+            row.each([&](float x, int) {
+                const float y = row.below(x);
+                if (!R::live(y)) return;
+                atomicAdd(&sm.bucket_n[static_cast<int>(y)], 1u);
+                if (by_p) atomicAdd(&sm.bucket_w[static_cast<int>(y)], R::whole(row.weight(x)));
+            });
+        } else if (tid < kBuckets) {
+            sm.bucket_n[tid] = work->bucket_n[tid];
+            sm.bucket_w[tid] = work->bucket_w[tid];
+        }
         __syncthreads();
         uint32_t n = tid < kBuckets ? sm.bucket_n[tid] : 0u;
         u64 w = tid < kBuckets ? sm.bucket_w[tid] : 0ull;
+        if constexpr (PHASE == kCount) {
+            if (n) {
+                atomicAdd(&work->bucket_n[tid], n);
+                if (w) atomicAdd(&work->bucket_w[tid], w);
+            }
+            return;
+        }
         group_sum(sm, n, w);
         __syncthreads();
         border.sum = w;
         for (int i = 0; i < 2; ++i) {  // top-k, then top-p of what it keeps
             if (!(i ? by_p : by_k && static_cast<uint32_t>(k) < n)) continue;
             const Target target = {i ? Target::kShare : Target::kCount, static_cast<uint32_t>(k), static_cast<double>(p) * static_cast<double>(border.sum), 0ull};
-            border = search(sm, row, list, room, target, by_p, i || !by_p, floor_w, held, listed);
+            if constexpr (PHASE == kCollect) {
+                find_bin(sm, tid < kBuckets ? sm.bucket_n[tid] : 0u, tid < kBuckets ? sm.bucket_w[tid] : 0ull, 0u, 0ull, target);
+                held = held_by(sm.before_n, sm.in_n, room);
+                u64 sum = 0;
+                if (held != kNoList)
+                    sum = collect(row, work->list, &work->listed, room, held, static_cast<float>(sm.bin), static_cast<float>(sm.bin + 1), i || !by_p, floor_w);
+                uint32_t none = 0;
+                group_sum(sm, none, sum);
+                if (tid == 0) work->part_w[share] = sum;
+                return;
+            } else {
+                if (PHASE == kRest && !found && tid < kWaves) sm.part_w[tid] = work->part_w[tid];
+                border = search(sm, row, list, room, target, by_p, i || !by_p, floor_w, work, held, listed);
+                found = true;
+            }
         }
     }
 
@@ -572,14 +668,46 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     // those equal to the border's that come after its last.
     // Where no border is, what is 50 octaves below the largest (rounded anyhow: 46 to 60
     // would do) stays out, and what is no number.
-    const float dead = fminf(m - static_cast<float>(50.0 / c), unordered(ordered(m) - 1u));
-    const float low = border.key ? unordered(border.key - 1u) : dead;
+    const float dead = fminf(m - static_cast<float>(50.0 / c), under(ordered(m)));
+    const float low = border.key ? under(border.key) : dead;
     const float tied = border.last < a.V ? unordered(border.key) : __builtin_nanf("");
     auto kept = [&](float x, int i) -> u64 {
         if (!(x > low) || (x == tied && i > border.last)) return 0ull;
         const double w = row.weight(x);
         return w >= floor_w ? R::whole(w) : 0ull;
     };
+    // the thread's share of the kept weights
+    auto kept_sum = [&]() -> u64 {
+        u64 sum = 0;
+        const bool ties = border.last < a.V;
+        row.each_piece([&](const float(&x)[R::kVec], int i) {
+            uint32_t in = 0;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j) in |= x[j] > low ? 1u << j : 0u;
+            if (ties) {
+#pragma unroll
+                for (int j = 0; j < R::kVec; ++j)
+                    if (x[j] == tied && i + j > border.last) in &= ~(1u << j);
+            }
+            if (!__any(in)) return;
+#pragma unroll
+            for (int j = 0; j < R::kVec; ++j) {
+                const double w = row.weight(x[j]);
+                sum += (in >> j & 1 && w >= floor_w ? R::above(w) : R::kZero) - R::kZero;
+                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // eight side by side do not fit the registers
+            }
+        });
+        return sum;
+    };
+    if constexpr (kShares) {  // no border: the parts' sums, in the launch that finds that out
+        if (PHASE == kCount || by_k) {
+            u64 sum = kept_sum();
+            uint32_t none = 0;
+            group_sum(sm, none, sum);
+            if (tid == 0) work->part_w[share] = sum;
+        }
+        return;
+    }
     auto done = [&](int i, float x, u64 total) {
         a.tokens[b] = i;
         if (a.probs) a.probs[b] = static_cast<float>(row.weight(x) / static_cast<double>(total));
@@ -624,27 +752,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
             const u64 w = kept(unordered(key), i);
             if (w) atomicAdd(&sm.part_w[(i + row.skip) / R::kVec / row.part()], w);
         }
+    } else if (PHASE == kRest && !found) {
+        if (tid < kWaves) sm.part_w[tid] = work->part_w[tid];
     } else {
-        u64 sum = 0;
+        u64 sum = kept_sum();
         uint32_t none = 0;
-        const bool ties = border.last < a.V;
-        row.each_piece([&](const float(&x)[R::kVec], int i) {
-            uint32_t in = 0;
-#pragma unroll
-            for (int j = 0; j < R::kVec; ++j) in |= x[j] > low ? 1u << j : 0u;
-            if (ties) {
-#pragma unroll
-                for (int j = 0; j < R::kVec; ++j)
-                    if (x[j] == tied && i + j > border.last) in &= ~(1u << j);
-            }
-            if (!__any(in)) return;
-#pragma unroll
-            for (int j = 0; j < R::kVec; ++j) {
-                const double w = row.weight(x[j]);
-                sum += (in >> j & 1 && w >= floor_w ? R::above(w) : R::kZero) - R::kZero;
-                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // eight side by side do not fit the registers
-            }
-        });
         wave_scan(none, sum);
         if (lane == 63) sm.part_w[wave] = sum;
     }
@@ -675,25 +787,44 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     }
 }
 
-template <bool F16, bool STAGED>
-hipError_t run(const SampleArgs& a, int64_t B, int row_bytes, hipStream_t st) {
+template <bool F16, bool STAGED, int PHASE>
+hipError_t run(const SampleArgs& a, int64_t groups, int row_bytes, hipStream_t st) {
     static std::atomic<uint64_t> done{0};
     constexpr int fixed = (sizeof(Shared) + 15) / 16 * 16;
     static_assert(fixed + kStageBytes + 1024 * 8 <= kLdsBytes && fixed + kRingBytes + kMostList * 8 <= kLdsBytes, "fits a compute unit's LDS");
-    const auto k = sample_kernel<F16, STAGED>;
+    const auto k = sample_kernel<F16, STAGED, PHASE>;
     const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(k), kLdsBytes, done);
     if (e != hipSuccess) return e;
     const int list_at = fixed + (STAGED ? row_bytes : kRingBytes), left = (kLdsBytes - list_at) / 8, room = left < kMostList ? left : kMostList;
-    k<<<dim3(static_cast<unsigned>(B)), dim3(kThreads), list_at + room * 8, st>>>(a, static_cast<uint32_t>(room), list_at);
+    const bool lists = PHASE == kWhole || PHASE == kRest;
+    k<<<dim3(static_cast<unsigned>(groups)), dim3(kThreads), list_at + (lists ? room * 8 : 0), st>>>(a, static_cast<uint32_t>(room), list_at);
     return hipGetLastError();
+}
+
+template <bool F16>
+hipError_t run_shared(const SampleArgs& a, int64_t B, hipStream_t st) {
+    hipError_t e = run<F16, false, kMax>(a, B * kWaves, 0, st);
+    if (e == hipSuccess) e = run<F16, false, kCount>(a, B * kWaves, 0, st);
+    if (e == hipSuccess) e = run<F16, false, kCollect>(a, B * kWaves, 0, st);
+    return e == hipSuccess ? run<F16, false, kRest>(a, B, 0, st) : e;
 }
 
 }  // namespace
 
+// Sharing takes three more launches (some 8 us where the host keeps up, 15 where it does
+// not) and a row's passes a sixteenth of their time.  top-p over 131072 binary32 logits, us shared
+// and not: 1 row 43 and 75, 8 rows 50 and 75, 32 rows 72 and 100, 64 rows 107 and 102; over 65000 of binary16 1
+// row 39 and 57, 64 rows 96 and 57; 32000: 35 and 30.
+int64_t sample_workspace(int64_t B, int64_t V, bool) {
+    const bool shared = B > 0 && V >= kSharedLogits && B * kWaves * kSharedLogits <= device_cu_count() * V;
+    return shared ? B * static_cast<int64_t>(sizeof(Work)) : 0;
+}
+
 hipError_t launch_sample(const SampleArgs& a, int64_t B, bool f16, hipStream_t stream) {
+    if (sample_workspace(B, a.V, f16)) return f16 ? run_shared<true>(a, B, stream) : run_shared<false>(a, B, stream);
     const int bytes = (a.V * (f16 ? 2 : 4) + 15) / 16 * 16 + 16;  // a row that begins inside a piece has one more
-    if (bytes <= kStageBytes) return f16 ? run<true, true>(a, B, bytes, stream) : run<false, true>(a, B, bytes, stream);
-    return f16 ? run<true, false>(a, B, bytes, stream) : run<false, false>(a, B, bytes, stream);
+    if (bytes <= kStageBytes) return f16 ? run<true, true, kWhole>(a, B, bytes, stream) : run<false, true, kWhole>(a, B, bytes, stream);
+    return f16 ? run<true, false, kWhole>(a, B, bytes, stream) : run<false, false, kWhole>(a, B, bytes, stream);
 }
 
 }  // namespace apex4

@@ -140,6 +140,23 @@ def test_two_values(pk):
                 assert int(got) == want
 
 
+@pytest.mark.parametrize("V", [600, 50001, 131072])
+def test_borders_at_zero(pk, V):
+    """Zeros of both signs are one value, at the border, above it and as the largest."""
+    import torch
+    g = np.random.default_rng(V)
+    sign = np.where(g.random(V) < 0.5, 0.0, -0.0)
+    for other in (1.0, -1.0):
+        x = np.where(np.arange(V) % 3 == 0, other, sign).astype(np.float32)[None]
+        for u in (0.0, 0.7, 1 - 2.0 ** -24):
+            for kw in (dict(), dict(top_k=V // 3 + 100), dict(top_k=V // 2), dict(top_p=0.5), dict(top_p=0.9), dict(min_p=0.5),
+                       dict(temperature=1e-40), dict(temperature=0.0)):
+                got, prob = pk.apex4_sample(dev(x), torch.tensor([u], device="cuda"), **kw)
+                want, share, near = plain(x[0], F32(u), F32(kw.get("temperature", 1.0)), kw.get("top_k", 0), F32(kw.get("top_p", 1)), F32(kw.get("min_p", 0)))
+                assert int(got) == want or near < V * 2.0 ** -45, (other, u, kw)
+                assert float(prob) == pytest.approx(share, rel=1e-6)
+
+
 def test_largest_logit(pk):
     """Settings that leave one: the lowest index of equal ones, whatever u is."""
     g = np.random.default_rng(4)
@@ -218,6 +235,47 @@ def test_many_rows(pk):
     g = np.random.default_rng(8)
     x = logits(g, 700, 301, np.float16)
     check(pk, x, g.random(700), t=(0.3 + g.random(700)).astype(F32), p=0.9)
+
+
+@pytest.mark.parametrize("dtype,V", [(np.float32, 50001), (np.float16, 100003), (np.float16, 131072)])
+def test_few_long_rows_and_many(pk, dtype, V):
+    """Long rows that several workgroups share where they are few, and one has where they are
+    many: the same bits.  Lists that hold all down to the border, its bucket, or nothing."""
+    import torch
+    g = np.random.default_rng(V)
+    B = 70
+    x = logits(g, B, V, dtype)
+    x[0] = 1.0
+    x[1, ::2] = -np.inf
+    x[2] = np.round(x[2])
+    x[3, 5] = np.inf
+    x[4] = np.nan
+    x[5] = -np.inf
+    assert pk.apex4_sample_workspace_size(6, V, torch.float16 if dtype == np.float16 else torch.float32) > 0
+    assert pk.apex4_sample_workspace_size(B, V, torch.float16 if dtype == np.float16 else torch.float32) == 0
+    x, u = dev(x), dev(g.random(B).astype(F32))
+    for kw in (dict(), dict(temperature=0.0), dict(top_k=30), dict(top_k=20000), dict(top_p=0.9), dict(temperature=1.5, top_p=0.99), dict(min_p=0.01),
+               dict(top_k=50, top_p=0.8), dict(top_k=30000, top_p=0.95), dict(top_k=V - 1), dict(temperature=0.05, top_k=V - 1, top_p=0.5),
+               dict(temperature=2.0, top_p=0.97, min_p=0.001), dict(temperature=30.0, top_p=0.5)):
+        whole = pk.apex4_sample(x, u, **kw)
+        for i in range(0, B, 7):
+            part = pk.apex4_sample(x[i:i + 7], u[i:i + 7], **kw)
+            assert part[0].equal(whole[0][i:i + 7]) and part[1].equal(whole[1][i:i + 7]), (kw, i)
+
+
+def test_workspace(pk):
+    """The caller's, of the size asked for; a shorter one is refused."""
+    import torch
+    x, u = torch.randn((3, 100000), device="cuda"), torch.rand(3, device="cuda")
+    need = pk.apex4_sample_workspace_size(3, 100000, torch.float32)
+    work = torch.full((need + 64,), 0xEE, dtype=torch.uint8, device="cuda")
+    for kw in (dict(top_p=0.9), dict(top_k=9, top_p=0.9), dict(), dict(temperature=0.0)):
+        got = pk.apex4_sample(x, u, workspace=work[:need], **kw)
+        assert got[0].equal(pk.apex4_sample(x, u, **kw)[0])
+    assert (work[need:] == 0xEE).all()
+    with pytest.raises(pk.Apex4Error) as e:
+        pk.apex4_sample(x, u, workspace=work[:need - 16])
+    assert e.value.status == -7
 
 
 def test_settings_for_all_rows_or_each(pk):
