@@ -179,7 +179,7 @@ hipError_t launch_w8a8_tiles(const int8_t* A, const float* sa, const int8_t* W, 
 bool w8a8_rows_fits(int64_t M, int64_t N);
 hipError_t launch_w8a8_rows(const int8_t* A, const float* sa, const int8_t* W, const float* sw, int M, int N, int K, uint16_t* Y,
                             hipStream_t stream);
-bool w8a8_fused_fits(int64_t M, int64_t K);
+bool w8a8_fused_fits(int64_t M, int64_t N, int64_t K);
 hipError_t launch_w8a8_fused(const uint16_t* x, const int8_t* W, const float* sw, int N, int K, uint16_t* Y, hipStream_t stream);
 
 // Sampling: B rows of V logits (binary16 or binary32), `stride` elements apart.  Settings

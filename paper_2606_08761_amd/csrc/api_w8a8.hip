@@ -64,7 +64,7 @@ int apex4_w8a8_linear(const void* x, const int8_t* W_8, const float* s_w, int64_
     if ((rc = check_device())) return rc;
     if (M == 0) return APEX4_OK;
     const auto st = static_cast<hipStream_t>(stream);
-    if (apex4::w8a8_fused_fits(M, K))
+    if (apex4::w8a8_fused_fits(M, N, K))
         return status_of(apex4::launch_w8a8_fused(static_cast<const uint16_t*>(x), W_8, s_w, static_cast<int>(N), static_cast<int>(K),
                                                   static_cast<uint16_t*>(Y), st));
     const hipError_t e = apex4::launch_quantize8(static_cast<const uint16_t*>(x), M, K, A_8_work, s_a_work, st);

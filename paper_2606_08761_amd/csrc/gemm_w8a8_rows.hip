@@ -173,8 +173,11 @@ hipError_t run(const int8_t* A, const float* sa, const uint16_t* x, const int8_t
 // units idle (1024 channels, K 8192, 16 and 32 rows: 9.7 and 13.0 us, tiles 16.8 and 16.9).
 // One group of 16 channels a workgroup: two fill the chip with half as many waves (8 rows of
 // 8192 and 57344 channels: 15.9 and 87.8 us, two groups 19.8 and 102).
-bool w8a8_rows_fits(int64_t M, int64_t N) { return M <= 8 || (M <= 32 && N <= 16 * static_cast<int64_t>(device_cu_count())); }
-bool w8a8_fused_fits(int64_t M, int64_t K) { return M == 1 && K <= kMostFused; }
+bool w8a8_rows_fits(int64_t M, int64_t N) {
+    if (N > 1 << 26) return false;  // a grid holds less than 2^32 threads
+    return M <= 8 || (M <= 32 && N <= 16 * static_cast<int64_t>(device_cu_count()));
+}
+bool w8a8_fused_fits(int64_t M, int64_t N, int64_t K) { return M == 1 && N <= 1 << 26 && K <= kMostFused; }
 
 hipError_t launch_w8a8_rows(const int8_t* A, const float* sa, const int8_t* W, const float* sw, int M, int N, int K, uint16_t* Y, hipStream_t st) {
     if (M <= 16) return run<1, 1, 4, 0>(A, sa, nullptr, W, sw, M, N, K, Y, st);

@@ -25,9 +25,11 @@ namespace {
 using namespace quant8;
 
 template <int T, int U>
-__global__ __launch_bounds__(T) void quant8_kernel(const uint16_t* __restrict__ x, int slots, int8_t* __restrict__ q, float* __restrict__ s) {
+__global__ __launch_bounds__(T) void quant8_kernel(const uint16_t* __restrict__ x, int64_t M, int slots, int8_t* __restrict__ q,
+                                                   float* __restrict__ s) {
     __shared__ uint32_t red[T / 64];
-    const int64_t row = blockIdx.x;
+    const int64_t row = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+    if (row >= M) return;
     const u32x4* xr = reinterpret_cast<const u32x4*>(x) + row * slots;
     u32x2* qr = reinterpret_cast<u32x2*>(q) + row * slots;
     u32x4 v[U];
@@ -59,7 +61,9 @@ __global__ __launch_bounds__(T) void quant8_kernel(const uint16_t* __restrict__ 
 
 template <int T, int U>
 hipError_t run(const uint16_t* x, int64_t M, int slots, int8_t* q, float* s, hipStream_t st) {
-    quant8_kernel<T, U><<<dim3(static_cast<unsigned>(M)), dim3(T), 0, st>>>(x, slots, q, s);
+    constexpr int64_t kMost = 1 << 21;  // of the first dimension, which holds less than 2^32 threads
+    const int64_t n = M < kMost ? M : kMost;
+    quant8_kernel<T, U><<<dim3(static_cast<unsigned>(n), static_cast<unsigned>((M + n - 1) / n)), dim3(T), 0, st>>>(x, M, slots, q, s);
     return hipGetLastError();
 }
 

@@ -8,7 +8,7 @@
 """
 from __future__ import annotations
 
-from . import _check, _dev, _stream, _torch, lib
+from . import _check, _stream, _torch, lib
 from .cache import _empty, _one_device, _output, _ptr
 
 
@@ -99,5 +99,8 @@ class W8A8Linear:
     def __call__(self, x, stream=None):
         if x.shape[-1] != self.K:
             raise ValueError(f"expected last dimension {self.K}, got {x.shape[-1]}")
-        _dev(x.contiguous(), _torch().float16, "x")
-        return apex4_w8a8_linear(x.reshape(-1, self.K), self.W_8, self.s_w, stream=stream).view(*x.shape[:-1], self.N)
+        shape = x.shape[:-1]
+        if not x.is_contiguous():
+            with _torch().cuda.stream(stream):  # None: the current one
+                x = x.contiguous()
+        return apex4_w8a8_linear(x.view(-1, self.K), self.W_8, self.s_w, stream=stream).view(*shape, self.N)

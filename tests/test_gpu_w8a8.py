@@ -185,6 +185,41 @@ def test_operands_past_2_gib(pk):
         assert same(y[:, rows], product(A, sa, W[rows].cpu().numpy(), sw.cpu().numpy()[rows]))
 
 
+def test_more_rows_and_channels_than_a_grid_has(pk):
+    """2^22 and more rows to quantize, 2^26 and more channels."""
+    import torch
+    M, K = (1 << 22) + 5, 32
+    x = torch.randn((M, K), device="cuda", dtype=torch.float16)
+    q, s = pk.apex4_quantize_act8(x)
+    rows = torch.tensor([0, 1, (1 << 21) - 1, 1 << 21, (1 << 22) - 1, 1 << 22, M - 1], device="cuda")
+    want_q, want_s = quantized(x[rows].cpu().numpy())
+    assert np.array_equal(q[rows].cpu().numpy(), want_q) and np.array_equal(s[rows].cpu().numpy(), want_s)
+    N = (1 << 26) + 100
+    W, sw = torch.randint(-127, 128, (N, K), dtype=torch.int8, device="cuda"), torch.rand(N, device="cuda")
+    cols = torch.tensor([0, 31, 1 << 20, (1 << 26) - 1, 1 << 26, N - 1], device="cuda")
+    for m in (1, 3):
+        y = pk.apex4_w8a8_linear(x[:m], W, sw)
+        qa, sa = quantized(x[:m].cpu().numpy())
+        assert same(y[:, cols], product(qa, sa, W[cols].cpu().numpy(), sw[cols].cpu().numpy()))
+
+
+def test_rows_with_gaps_on_another_stream(pk):
+    """The layer's own copy of such rows is made on the stream of the call."""
+    import torch
+    g = np.random.default_rng(12)
+    layer = pk.W8A8Linear(dev(g.standard_normal((64, 128)).astype(np.float16)))
+    wide = dev(g.standard_normal((4096, 256)).astype(np.float16))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(50):
+            wide.mul_(-1.0)
+        wide.add_(1.0)
+    y = layer(wide[:, 64:192], stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert y.equal(layer(wide[:, 64:192].contiguous()))
+
+
 def test_captured_and_on_another_stream(pk):
     import torch
     g = np.random.default_rng(8)
