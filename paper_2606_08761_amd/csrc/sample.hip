@@ -13,7 +13,7 @@
 // hundred of a flat distribution over 10^5 tokens would get another token.)  A logit 46
 // octaves below the largest weighs nothing.
 //
-// A workgroup takes a row; rows of up to 128 KB stay in LDS, longer ones are read again,
+// A workgroup takes a row; rows of up to 126 KB stay in LDS, longer ones are read again,
 // through a ring in LDS that keeps four loads a wave in flight and no registers.  Passes
 // over the row:
 //   1  the largest logit;
@@ -42,11 +42,11 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBuckets = 736;          // 1/16 octave each
-constexpr int kStageBytes = 128 << 10; // of a row in LDS
+constexpr int kStageBytes = 126 << 10; // of a row in LDS
 constexpr int kSharedLogits = 48 << 10;  // rows from here on are shared where they are few
-constexpr int kLdsBytes = 160 << 10, kMostList = 9216;
+constexpr int kLdsBytes = 160 << 10, kMostList = 8704;
 constexpr int kDepth = 4, kRingBytes = kWaves * kDepth * 1024;
-constexpr int kSteps = 128, kStepBits = 7;  // table of 2^(45 + i / 128)
+constexpr int kSteps = 512, kStepBits = 9;  // table of 2^(i / 512)
 constexpr double kMagic = 0x1.8p52;    // added to a number below 2^51: its nearest whole one in the low bits
 constexpr float kNothing = -__builtin_inff();
 
@@ -120,7 +120,7 @@ struct Row {
     int from, to;          // the pieces that the passes go over
     bool infinite;         // the largest logit is infinite: its like count as 0, the others as nothing
     float half, c32;
-    double max, c64;
+    double max, c64;       // 512 c
 
     static constexpr uint32_t kNone = F16 ? 0xFC00FC00u : 0xFF800000u;  // -infinity
     // A piece as it was read, with -infinity for what is not of the row.
@@ -198,16 +198,14 @@ struct Row {
     // overflow).  NaN and -infinity are not below kBuckets: they are not live.
     __device__ __forceinline__ float below(float x) const { return fmaf(-0.5f, x, half) * c32; }
     __device__ __forceinline__ static bool live(float y) { return y < static_cast<float>(kBuckets); }
-    // 2^45 2^y for y = (x - max) c, not below -60, in binary64: 128 y = k + f, |f| <= 1/2, a
-    // power of two, the table's 2^(k % 128 / 128), and e^r, r = f ln 2 / 128, by its series: the
-    // terms of r^3 and r^4 (2^-28 and less) in binary32, what follows is below 2^-49.
+    // 2^45 2^((x - max) c), the power not below -60, in binary64: 512 (x - max) c = k + f, |f| <=
+    // 1/2, a power of two, the table's 2^(k % 512 / 512), and e^r - 1, r = f ln 2 / 512, by its
+    // series to r^3 (what follows is below 2^-46).
     __device__ __forceinline__ double weight(float x) const {
         const double y = (static_cast<double>(x) - max) * c64, t = y + kMagic, f = y - (t - kMagic);
         const int k = static_cast<int>(__double_as_longlong(t));
         constexpr double l = 0.69314718055994530942 / kSteps;
-        const float g = static_cast<float>(f);
-        const float tail = g * g * (g * fmaf(g, static_cast<float>(l * l * l * l / 24), static_cast<float>(l * l * l / 6)));
-        const double p = fma(f, fma(f, l * l / 2, l), static_cast<double>(tail)), a = table[k & (kSteps - 1)];
+        const double p = f * fma(f, fma(f, l * l * l / 6, l * l / 2), l), a = table[k & (kSteps - 1)];
         return ldexp(fma(a, p, a), k >> kStepBits);
     }
     static constexpr u64 kZero = 0x4330000000000000ull;  // the bits of 2^52
@@ -624,8 +622,10 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
                 const float y = row.below(x);
                 if (!R::live(y)) return;
                 atomicAdd(&sm.bucket_n[static_cast<int>(y)], 1u);
-                if (by_p) atomicAdd(&sm.bucket_w[static_cast<int>(y)], R::whole(row.weight(x)));
+                if (by_p) atomicAdd(&sm.bucket_w[static_cast<int>(y)], R::above(row.weight(x)));  // kZero too much for each
             });
+            __syncthreads();
+            if (by_p && tid < kBuckets) sm.bucket_w[tid] -= sm.bucket_n[tid] * R::kZero;
         } else if (tid < kBuckets) {
             sm.bucket_n[tid] = work->bucket_n[tid];
             sm.bucket_w[tid] = work->bucket_w[tid];
