@@ -227,19 +227,26 @@ hipError_t run_tile(const int8_t* A, const float* sa, const int8_t* W, const flo
 
 namespace {
 
-// The forms and their times in us for K = 8192 where the chip is full: `tiles` at once,
-// one or two a compute unit.
+// The forms and their times in us for K = 8192 where the chip is full: one tile a compute
+// unit, of the smallest two.  Tiles of 256 x 256 read the fewest bytes for their products;
+// the others are for counts of them that leave units idle (4096 x 10240: 2.5 rounds of
+// 256 x 256 357 us, 2 of 256 x 320 324; 300 x 57344: 128 x 256 200, 320 x 256 168;
+// 1024 x 10240: 256 x 256 109, 256 x 192 100; 3000 x 8192: 256 x 256 227,
+// 128 x 256 222, 192 x 256 210; 768 x 8192 of K 28672: 128 x 256 205, 192 x 128 192;
+// 300 x 8192: 128 x 256 56, 128 x 128 38).
 struct Form {
     int bm, bn, tiles_a_unit;
     double us;
 };
-constexpr Form kForms[] = {{256, 256, 1, 128.0}, {128, 256, 1, 70.0}, {128, 128, 1, 40.0}, {128, 64, 2, 46.0}, {64, 64, 2, 29.0}};
+constexpr Form kForms[] = {{256, 256, 1, 128.0}, {256, 320, 1, 151.0}, {320, 256, 1, 151.0}, {256, 192, 1, 97.0}, {192, 256, 1, 99.0},
+                           {128, 256, 1, 70.0}, {192, 128, 1, 52.0},  {128, 128, 1, 40.0},   {64, 64, 2, 29.0}};
+constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
 
 // Time of a form: whole rounds of tiles, and for those that are left 0.3 of a round and
 // as much of the rest as they fill (fewer tiles at once run at a higher clock and share
-// less); a tile starts in 5 us and goes over K evenly.  Within 8 % of what was measured
-// for 65 to 1536 rows of 8192, 10240 and 57344 channels, K 8192 and 28672, save where the
-// weights' bytes bound every form alike.
+// less); a tile starts in 5 us and goes over K evenly.  For 200 to 4096 rows of 8192,
+// 10240, 28672 and 57344 channels, K 8192 and 28672 (30 calls), the form that it picks
+// is the fastest of those listed or within 2 % of it.
 double cost_of(const Form& f, int64_t M, int64_t N, int64_t K, int cus) {
     const double tiles = static_cast<double>((M + f.bm - 1) / f.bm) * static_cast<double>((N + f.bn - 1) / f.bn);
     const double at_once = static_cast<double>(cus) * f.tiles_a_unit;
@@ -262,13 +269,17 @@ hipError_t launch_w8a8_tiles(const int8_t* A, const float* sa, const int8_t* W, 
         return run_tile<64, 64, 2, 2, 5>(A, sa, W, sw, M, N, K, Y, st);
     }
     int best = 0;
-    for (int i = 1; i < 5; ++i)
+    for (int i = 1; i < kFormCount; ++i)
         if (cost_of(kForms[i], M, N, K, cus) < cost_of(kForms[best], M, N, K, cus)) best = i;
     switch (best) {
         case 0: return run_tile<256, 256, 2, 4, 2>(A, sa, W, sw, M, N, K, Y, st);
-        case 1: return run_tile<128, 256, 2, 4, 3>(A, sa, W, sw, M, N, K, Y, st);
-        case 2: return run_tile<128, 128, 2, 4, 4>(A, sa, W, sw, M, N, K, Y, st);
-        case 3: return run_tile<128, 64, 2, 2, 3>(A, sa, W, sw, M, N, K, Y, st);
+        case 1: return run_tile<256, 320, 4, 2, 2>(A, sa, W, sw, M, N, K, Y, st);
+        case 2: return run_tile<320, 256, 2, 4, 2>(A, sa, W, sw, M, N, K, Y, st);
+        case 3: return run_tile<256, 192, 4, 2, 2>(A, sa, W, sw, M, N, K, Y, st);
+        case 4: return run_tile<192, 256, 2, 4, 2>(A, sa, W, sw, M, N, K, Y, st);
+        case 5: return run_tile<128, 256, 2, 4, 3>(A, sa, W, sw, M, N, K, Y, st);
+        case 6: return run_tile<192, 128, 2, 4, 3>(A, sa, W, sw, M, N, K, Y, st);
+        case 7: return run_tile<128, 128, 2, 4, 4>(A, sa, W, sw, M, N, K, Y, st);
         default: return run_tile<64, 64, 2, 2, 5>(A, sa, W, sw, M, N, K, Y, st);
     }
 }

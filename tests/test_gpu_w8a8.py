@@ -96,7 +96,10 @@ def test_infinities_and_nan_stay_in_their_row(pk):
 SIZES = [(1, 1, 32), (1, 100, 96), (2, 33, 160), (8, 16, 128), (7, 1001, 1056), (9, 17, 4128), (16, 520, 8192), (17, 40, 32), (32, 4096, 256),
          (20, 5003, 544), (32, 9000, 160), (33, 70, 96), (64, 8192, 512), (50, 8225, 192), (64, 8200, 128), (65, 64, 32), (65, 8193, 416),
          (130, 260, 2048), (128, 16384, 128), (300, 520, 1056), (257, 4100, 96), (513, 1001, 160), (700, 10240, 288), (1030, 8191, 64),
-         (2048, 8192, 128), (3000, 2100, 32), (4100, 4097, 160)]
+         (2048, 8192, 128), (3000, 2100, 32), (4100, 4097, 160),
+         # each tile, and K that ends inside a stage
+         (2501, 3276, 672), (1156, 7302, 672), (1539, 3859, 672), (389, 7183, 672), (3204, 1158, 672), (385, 3514, 672), (525, 1415, 1056),
+         (1481, 193, 1056), (263, 100, 1056), (257, 4867, 160), (261, 3075, 160), (2577, 579, 160), (2725, 133, 160)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
