@@ -28,6 +28,7 @@
 //      logits of the part that holds it.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 #include <atomic>
@@ -51,21 +52,29 @@ constexpr double kMagic = 0x1.8p52;    // added to a number below 2^51: its near
 constexpr float kNothing = -__builtin_inff();
 
 struct Shared {
-    u64 bucket_w[kBuckets];
-    u64 bin_w[1024];
-    double table[kSteps];
-    uint32_t bucket_n[kBuckets];
+    alignas(16) u64 bucket_w[kBuckets];
+    alignas(16) u64 bin_w[1024];
     uint32_t bin_n[1024];
+    double table[kSteps];
+    alignas(16) uint32_t bucket_n[kBuckets];
     u64 wave_w[kWaves];
-    u64 part_w[kWaves];   // of the waves' parts of the row
+    u64 part_w[kWaves];   // of the waves' parts of the row, or at 4 q of its quarter q
     uint32_t wave_n[kWaves];
     float wave_max[kWaves];
     // the border's bin: what lies before it and in it
-    u64 before_w, in_w;
+    u64 before_w, in_w, goal, total;
     uint32_t before_n, in_n;
     int bin;
     uint32_t listed, low, high, first;
 };
+
+// In pass 2 of a row that is one workgroup's the buckets' sums are held by quarters of the
+// row: the first in bucket_w, two where the bins are later, the last in the list's place.
+constexpr int kQuarters = 4, kQuarterWaves = kWaves / kQuarters;
+static_assert(offsetof(Shared, bin_n) == offsetof(Shared, bin_w) + 1024 * 8 && 2 * kBuckets * 8 <= 1024 * 12, "two of them where the bins are");
+__device__ __forceinline__ u64* quarter(Shared& sm, u64* list, int q) {
+    return q == 0 ? sm.bucket_w : q == kQuarters - 1 ? list : sm.bin_w + (q - 1) * kBuckets;
+}
 
 // What the workgroups that share a row leave for the next launch.
 struct Work {
@@ -199,19 +208,43 @@ struct Row {
     __device__ __forceinline__ float below(float x) const { return fmaf(-0.5f, x, half) * c32; }
     __device__ __forceinline__ static bool live(float y) { return y < static_cast<float>(kBuckets); }
     // 2^45 2^((x - max) c), the power not below -60, in binary64: 512 (x - max) c = k + f, |f| <=
-    // 1/2, a power of two, the table's 2^(k % 512 / 512), and e^r - 1, r = f ln 2 / 512, by its
-    // series to r^3 (what follows is below 2^-46).
+    // 1/2, the table's 2^(k % 512 / 512), a power of two (which only adds to its exponent), and
+    // e^r - 1, r = f ln 2 / 512, by its series to r^3 (what follows is below 2^-46).  Each fma
+    // is written out: a row's sums of different passes are compared, so all have the same bits.
     __device__ __forceinline__ double weight(float x) const {
-        const double y = (static_cast<double>(x) - max) * c64, t = y + kMagic, f = y - (t - kMagic);
+        const double d = static_cast<double>(x) - max, t = fma(d, c64, kMagic), f = fma(d, c64, -(t - kMagic));
         const int k = static_cast<int>(__double_as_longlong(t));
         constexpr double l = 0.69314718055994530942 / kSteps;
-        const double p = f * fma(f, fma(f, l * l * l / 6, l * l / 2), l), a = table[k & (kSteps - 1)];
-        return ldexp(fma(a, p, a), k >> kStepBits);
+        const double p = f * fma(f, fma(f, l * l * l / 6, l * l / 2), l);
+        const u64 two = static_cast<u64>(__double_as_longlong(table[k & (kSteps - 1)])) + (static_cast<u64>(static_cast<uint32_t>(k & -kSteps) << (20 - kStepBits)) << 32);
+        const double a = __longlong_as_double(static_cast<long long>(two));
+        return fma(a, p, a);
+    }
+    // f(j, weight) for a piece's logits; four of them are worked out side by side (one after the
+    // other they would wait for the table, and eight do not fit the registers), those that
+    // are not asked for as any number.
+    template <class F>
+    __device__ __forceinline__ void weights(const float (&x)[kVec], F f) const {
+#pragma unroll
+        for (int g = 0; g < kVec; g += 4) {
+            double w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = weight(x[g + q]);
+            asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));  // not put off into f's branches
+#pragma unroll
+            for (int q = 0; q < 4; ++q) f(g + q, w[q]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     static constexpr u64 kZero = 0x4330000000000000ull;  // the bits of 2^52
     // The bits of 2^52 + w: w rounded to a whole number, 0 .. 2^45, above kZero.
     __device__ __forceinline__ static u64 above(double w) { return static_cast<u64>(__double_as_longlong(w + 0x1p52)); }
     __device__ __forceinline__ static u64 whole(double w) { return above(w) - kZero; }
+    // The same, or kZero if not `in`: what is left of w without its high half is nothing beside 2^52.
+    __device__ __forceinline__ static u64 above_if(bool in, double w) {
+        const u64 bits = static_cast<u64>(__double_as_longlong(w));
+        return above(__longlong_as_double(static_cast<long long>(in ? bits : bits & 0xFFFFFFFFull)));
+    }
 };
 
 template <int CTRL, int ROWS>
@@ -235,62 +268,131 @@ __device__ __forceinline__ void wave_scan(uint32_t& n, u64& w) {
     add_before<0x143, 0xC>(n, w);
 }
 
-// The workgroup's sums, to every thread.  Begins with a barrier.
-__device__ __forceinline__ void group_sum(Shared& sm, uint32_t& n, u64& w) {
-    wave_scan(n, w);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) {
+// Running sums over the waves, in lanes 0 .. 15, of what the last lane of each has in (n, w).
+// Has one barrier, and wants one before the next.
+static_assert(kWaves == 16, "a row of lanes");
+__device__ __forceinline__ void across_waves(Shared& sm, uint32_t& n, u64& w) {
+    const int lane = threadIdx.x & 63;
+    if (lane == 63) {
         sm.wave_n[threadIdx.x >> 6] = n;
         sm.wave_w[threadIdx.x >> 6] = w;
     }
     __syncthreads();
-    n = 0;
-    w = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        n += sm.wave_n[i];
-        w += sm.wave_w[i];
-    }
+    n = sm.wave_n[lane & 15];
+    w = sm.wave_w[lane & 15];
+    add_before<0x111, 0xF>(n, w);
+    add_before<0x112, 0xF>(n, w);
+    add_before<0x114, 0xF>(n, w);
+    add_before<0x118, 0xF>(n, w);
+}
+__device__ __forceinline__ u64 of_lane(u64 w, int lane) {
+    return static_cast<u64>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(w >> 32), lane))) << 32 |
+           static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(w), lane));
 }
 
-// What a border is looked for by: the k-th, the first whose running sum reaches `share`, or
-// the first whose running sum passes `goal`.
+// The workgroup's sums, to every thread.  Begins with a barrier.
+__device__ __forceinline__ void group_sum(Shared& sm, uint32_t& n, u64& w) {
+    wave_scan(n, w);
+    __syncthreads();
+    across_waves(sm, n, w);
+    n = __builtin_amdgcn_readlane(static_cast<int>(n), kWaves - 1);
+    w = of_lane(w, kWaves - 1);
+}
+
+// The largest whole number that is not above u total (total >= 1), and below total.
+__device__ __forceinline__ u64 share_of(float u, u64 total) {
+    if (!(u > 0.f)) return 0ull;
+    if (u >= 1.f) return total - 1;
+    int e;
+    const u64 f = static_cast<u64>(ldexpf(frexpf(u, &e), 24));  // u = f 2^(e - 24)
+    const int shift = 24 - e;
+    return shift < 128 ? static_cast<u64>(static_cast<unsigned __int128>(f) * total >> shift) : 0ull;
+}
+
+// The least whole number that is a share p of total, above 0.
+__device__ __forceinline__ u64 least_share(float p, u64 total) {
+    const double s = ceil(static_cast<double>(p) * static_cast<double>(total));
+    return s > 1.0 ? static_cast<u64>(s) : 1ull;
+}
+
+// What a border is looked for by: the k-th; the first whose running sum reaches the goal; or
+// that with the goal for a share `part` of all, or for passing it.
 struct Target {
-    enum Kind { kCount, kShare, kPass } kind;
+    enum Kind { kCount, kSum, kShare, kPass } kind;
     uint32_t k;
-    double share;
     u64 goal;
-    __device__ __forceinline__ bool reached(uint32_t n, u64 w) const {
-        return kind == kCount ? n >= k : kind == kShare ? static_cast<double>(w) >= share : w > goal;
-    }
+    float part;
 };
 
-// Of 1024 bins, a thread with (n, w) of each, the one in which what comes after (base_n,
-// base_w) reaches the target: to sm.bin, before_*, in_*.  Ends in a barrier.
-__device__ __forceinline__ void find_bin(Shared& sm, uint32_t n, u64 w, uint32_t base_n, u64 base_w, const Target& target) {
-    const int wave = threadIdx.x >> 6;
-    uint32_t sn = n;
-    u64 sw = w;
-    wave_scan(sn, sw);
-    if ((threadIdx.x & 63) == 63) {
-        sm.wave_n[wave] = sn;
-        sm.wave_w[wave] = sw;
+// Of the bins with counts ns and sums ws the one in which what comes after (base_n, base_w)
+// reaches the target: to sm.bin, or -1, before_*, in_*, and the goal and the sum of all.
+// Four waves do it, one a SIMD and a lane with four bins: sixteen take twice the time for the
+// scans that all of them repeat.  The bins are complete at a barrier before, what the last
+// call left has been read at one; ends in a barrier.
+template <int BINS, bool N, bool W>
+__device__ __forceinline__ void find_bin(Shared& sm, const uint32_t* ns, const u64* ws, uint32_t base_n, u64 base_w, const Target& target) {
+    constexpr int kFinders = 4;
+    static_assert(BINS % 4 == 0 && BINS <= kFinders * 256, "four bins a lane");
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint32_t n[4] = {0, 0, 0, 0}, sum_n = 0, end_n = 0;
+    u64 w[4] = {0, 0, 0, 0}, sum_w = 0, end_w = 0;
+    if (wave < kFinders) {
+        if (4 * tid < BINS) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (N) n[q] = ns[4 * tid + q];
+                if (W) w[q] = ws[4 * tid + q];
+            }
+        }
+        end_n = sum_n = n[0] + n[1] + n[2] + n[3];
+        end_w = sum_w = w[0] + w[1] + w[2] + w[3];
+        wave_scan(end_n, end_w);
+        if ((tid & 63) == 63) {
+            sm.wave_n[wave] = end_n;
+            sm.wave_w[wave] = end_w;
+        }
+        if (tid == 0) sm.bin = -1;
     }
     __syncthreads();
+    if (wave < kFinders) {
+        u64 total = 0;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i)
-        if (i < wave) {
-            base_n += sm.wave_n[i];
-            base_w += sm.wave_w[i];
+        for (int i = 0; i < kFinders; ++i) {
+            const uint32_t one_n = sm.wave_n[i];
+            const u64 one_w = sm.wave_w[i];
+            base_n += i < wave ? one_n : 0u;
+            base_w += i < wave ? one_w : 0ull;
+            total += one_w;
         }
-    const uint32_t after_n = base_n + sn, first_n = after_n - n;
-    const u64 after_w = base_w + sw, first_w = after_w - w;
-    if (!target.reached(first_n, first_w) && target.reached(after_n, after_w)) {
-        sm.bin = threadIdx.x;
-        sm.before_n = first_n;
-        sm.before_w = first_w;
-        sm.in_n = n;
-        sm.in_w = w;
+        u64 goal = target.goal;
+        if (W && target.kind == Target::kShare) goal = least_share(target.part, total);
+        if (W && target.kind == Target::kPass) goal = share_of(target.part, total) + 1;
+        const bool by_n = N && (!W || target.kind == Target::kCount);
+        auto reached = [&](uint32_t at_n, u64 at_w) { return by_n ? at_n >= target.k : at_w >= goal; };
+        end_n += base_n;
+        end_w += base_w;
+        uint32_t at_n = end_n - sum_n;
+        u64 at_w = end_w - sum_w;
+        if (reached(end_n, end_w) && !reached(at_n, at_w)) {
+            int q = 0;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                if (q == i && !reached(at_n + n[i], at_w + w[i])) {
+                    at_n += n[i];
+                    at_w += w[i];
+                    q = i + 1;
+                }
+            }
+            sm.bin = 4 * tid + q;
+            sm.before_n = at_n;
+            sm.before_w = at_w;
+            sm.in_n = q == 0 ? n[0] : q == 1 ? n[1] : q == 2 ? n[2] : n[3];
+            sm.in_w = q == 0 ? w[0] : q == 1 ? w[1] : q == 2 ? w[2] : w[3];
+        }
+        if (tid == 0) {
+            sm.goal = goal;
+            sm.total = total;
+        }
     }
     __syncthreads();
 }
@@ -315,56 +417,63 @@ __device__ __forceinline__ int held_by(uint32_t before, uint32_t members, uint32
 template <class R>
 __device__ __forceinline__ u64 collect(const R& row, u64* list, uint32_t* listed, uint32_t room, int held, float top, float end, bool parts,
                                        double least) {
-    // a piece's logits that `wanted` has a bit of, into the list, one count for a wave
-    auto append = [&](uint32_t wanted, const float(&x)[R::kVec], int i) {
-        uint32_t n = __builtin_popcount(wanted), own = n;
-        u64 none = 0;
-        wave_scan(n, none);
-        uint32_t at = 0;
-        if ((threadIdx.x & 63) == 63) at = atomicAdd(listed, n);
-        at = __builtin_amdgcn_readlane(at, 63) + n - own;
+    // a piece's wanted logits into the list, one count for a wave
+    auto append = [&](const bool (&wanted)[R::kVec], const float(&x)[R::kVec], int i) {
+        u64 lanes[R::kVec];
+        uint32_t n = 0;
 #pragma unroll
-        for (int j = 0; j < R::kVec; ++j)
-            if (wanted >> j & 1 && at < room) list[at++] = static_cast<u64>(ordered(x[j])) << 32 | static_cast<uint32_t>(i + j);
+        for (int j = 0; j < R::kVec; ++j) {
+            lanes[j] = __ballot(wanted[j]);
+            n += __builtin_popcountll(lanes[j]);
+        }
+        if (n == 0) return;
+        uint32_t at = 0;
+        if ((threadIdx.x & 63) == 0) at = atomicAdd(listed, n);
+        at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+        for (int j = 0; j < R::kVec; ++j) {
+            if (lanes[j] == 0) continue;
+            const uint32_t place = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes[j] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes[j]), at));
+            if (wanted[j] && place < room) list[place] = static_cast<u64>(ordered(x[j])) << 32 | static_cast<uint32_t>(i + j);
+            at += __builtin_popcountll(lanes[j]);
+        }
     };
     u64 sum = 0;
     if (held == kAll) {
         row.each_piece([&](const float(&x)[R::kVec], int i) {
-            uint32_t wanted = 0;
+            bool wanted[R::kVec];
 #pragma unroll
-            for (int j = 0; j < R::kVec; ++j) wanted |= row.below(x[j]) < end ? 1u << j : 0u;
-            if (__any(wanted)) append(wanted, x, i);
+            for (int j = 0; j < R::kVec; ++j) wanted[j] = row.below(x[j]) < end;
+            append(wanted, x, i);
         });
     } else {
         row.each_piece([&](const float(&x)[R::kVec], int i) {
-            uint32_t wanted = 0, before = 0;
+            bool wanted[R::kVec], before = false;
 #pragma unroll
             for (int j = 0; j < R::kVec; ++j) {
                 const float y = row.below(x[j]);
-                wanted |= y >= top && y < end ? 1u << j : 0u;
-                before |= y < top ? 1u << j : 0u;
+                wanted[j] = (y >= top) & (y < end);
+                before |= y < top;
             }
-            if (__any(wanted)) append(wanted, x, i);
+            append(wanted, x, i);
             if (!parts || !__any(before)) return;
-#pragma unroll
-            for (int j = 0; j < R::kVec; ++j) {  // of what is not summed the weight is any number
-                const double w = row.weight(x[j]);
-                sum += (before >> j & 1 && w >= least ? R::above(w) : R::kZero) - R::kZero;
-                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-            }
+            row.weights(x, [&](int j, double w) { sum += R::above_if((row.below(x[j]) < top) & (w >= least), w); });
+            sum -= R::kVec * R::kZero;
         });
     }
     return sum;
 }
 
-// A border's search.  The list is filled by the first (held < 0), or was by an earlier launch
-// (work: the list, and in sm.part_w the parts); the second one's border is not behind the first's.  parts: the waves' sums of the kept weights before the bucket are
-// left in sm.part_w (min-p's `least` included) where the list holds the bucket alone.
+// A border's search in the bucket that find_bin left in sm.  The list is filled by the first (held < 0), or was by an earlier launch
+// (work: the list, and in sm.part_w the parts); the second one's border is not behind the
+// first's.  parts: the sums of the kept weights before the bucket are left in sm.part_w (min-p's
+// `least` included) where the list holds the bucket alone: of the quarters, if pass 2 left
+// their buckets (quartered, which says afterwards if it is so) and min-p keeps all before the
+// bucket's end, or of the waves' parts.
 template <class R>
 __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, uint32_t room, const Target& target, bool weigh, bool parts, double least,
-                         const Work* work, int& held, uint32_t& listed) {
+                         const Work* work, bool& quartered, int& held, uint32_t& listed) {
     const int tid = threadIdx.x;
-    find_bin(sm, tid < kBuckets ? sm.bucket_n[tid] : 0u, tid < kBuckets ? sm.bucket_w[tid] : 0ull, 0u, 0ull, target);
     const int bucket = sm.bin;
     uint32_t before_n = sm.before_n;
     const uint32_t members = sm.in_n;
@@ -383,6 +492,28 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
         const bool ready = held < 0 && work != nullptr;
         held = held_by(before_n, members, room);
         listed = held == kAll ? before_n + members : members;
+        // (the bucket's end is at 2^-((bucket + 1) / 16) but for the roundings of below())
+        quartered = quartered && parts && held == kBucket && least <= exp2(45.0 - 1e-3 - (bucket + 1) * (1.0 / 16.0));
+        if (quartered) {
+            const int wave = tid >> 6, lane = tid & 63;
+            if (wave > 0 && wave < kQuarters) {
+                const u64* q = quarter(sm, list, wave);
+                u64 sum = 0;
+                for (int i = lane; i < bucket; i += 64) sum += q[i];
+                uint32_t none = 0;
+                wave_scan(none, sum);
+                if (lane == 63) sm.part_w[wave] = sum;
+            }
+            __syncthreads();
+            if (tid == 0) {
+                const u64 w1 = sm.part_w[1], w2 = sm.part_w[2], w3 = sm.part_w[3];
+                for (int i = 0; i < kWaves; ++i) sm.part_w[i] = 0ull;
+                sm.part_w[0] = before_w - w1 - w2 - w3;
+                sm.part_w[kQuarterWaves] = w1;
+                sm.part_w[2 * kQuarterWaves] = w2;
+                sm.part_w[3 * kQuarterWaves] = w3;
+            }
+        }
         if (tid == 0) sm.listed = 0u;
         __syncthreads();
         if (held == kNoList) {
@@ -393,10 +524,10 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
         } else if (ready) {
             for (uint32_t i = tid; i < listed; i += kThreads) list[i] = work->list[i];
         } else {
-            u64 sum = collect(row, list, &sm.listed, room, held, top, end, parts, least);
+            u64 sum = collect(row, list, &sm.listed, room, held, top, end, parts && !quartered, least);
             uint32_t none = 0;
             wave_scan(none, sum);
-            if ((tid & 63) == 63) sm.part_w[tid >> 6] = sum;
+            if ((tid & 63) == 63 && !quartered) sm.part_w[tid >> 6] = sum;
         }
     }
     __syncthreads();
@@ -435,7 +566,7 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
             if (weigh) atomicAdd(&sm.bin_w[bin], R::whole(row.weight(unordered(key))));
         });
         __syncthreads();
-        find_bin(sm, sm.bin_n[tid], sm.bin_w[tid], before_n, before_w, target);
+        find_bin<1024, true, true>(sm, sm.bin_n, sm.bin_w, before_n, before_w, target);
         before_n = sm.before_n;
         before_w = sm.before_w;
         const uint32_t first = high - (static_cast<uint32_t>(sm.bin) << shift);
@@ -455,17 +586,17 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
     if (target.kind == Target::kCount) {
         take = target.k - before_n;
     } else {
-        const double t = ceil((target.share - static_cast<double>(before_w)) / static_cast<double>(w));
+        const double t = ceil(static_cast<double>(target.goal - before_w) / static_cast<double>(w));
         take = t < 1.0 ? 1u : t > equal ? equal : static_cast<uint32_t>(t);
-        while (take > 1 && target.reached(0, before_w + (take - 1) * w)) --take;
-        while (take < equal && !target.reached(0, before_w + take * w)) ++take;
+        while (take > 1 && before_w + (take - 1) * w >= target.goal) --take;
+        while (take < equal && before_w + take * w < target.goal) ++take;
     }
     b.sum = before_w + take * w;
     b.last = row.V;
     if (take < equal) {
         int first = 0;
         uint32_t done = 0;
-        const Target nth = {Target::kCount, take, 0.0, 0ull};
+        const Target nth = {Target::kCount, take, 0ull, 0.f};
         for (int shift = 8; shift >= 0; shift -= 8) {  // V <= 2^18
             __syncthreads();
             sm.bin_n[tid] = 0u;
@@ -475,7 +606,7 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
                 if (key == b.key && bin >= 0 && bin < 1024) atomicAdd(&sm.bin_n[bin], 1u);
             });
             __syncthreads();
-            find_bin(sm, sm.bin_n[tid], 0ull, done, 0ull, nth);
+            find_bin<1024, true, false>(sm, sm.bin_n, nullptr, done, 0ull, nth);
             done = sm.before_n;
             first += sm.bin << shift;
         }
@@ -483,16 +614,6 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
     }
     __syncthreads();
     return b;
-}
-
-// The largest whole number that is not above u total (total >= 1), and below total.
-__device__ __forceinline__ u64 share_of(float u, u64 total) {
-    if (!(u > 0.f)) return 0ull;
-    if (u >= 1.f) return total - 1;
-    int e;
-    const u64 f = static_cast<u64>(ldexpf(frexpf(u, &e), 24));  // u = f 2^(e - 24)
-    const int shift = 24 - e;
-    return shift < 128 ? static_cast<u64>(static_cast<unsigned __int128>(f) * total >> shift) : 0ull;
 }
 
 // A row is one workgroup's, in one launch, or sixteen workgroups share its passes, in four.
@@ -557,6 +678,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     if (tid < kBuckets) {
         sm.bucket_n[tid] = 0u;
         sm.bucket_w[tid] = 0ull;
+        if constexpr (PHASE == kWhole)
+            for (int q = 1; q < kQuarters; ++q) quarter(sm, list, q)[tid] = 0ull;
     }
     if (tid < kSteps) sm.table[tid] = exp2(45.0 + tid * (1.0 / kSteps));
     __syncthreads();
@@ -615,39 +738,53 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     Border border = {0u, a.V, 0ull};
     int held = -1;
     uint32_t listed = 0;
-    bool found = false;  // a border
+    bool found = false, quartered = PHASE == kWhole && by_p;  // a border; the quarters' buckets, then their sums, are there
     if (by_k || by_p) {
         if constexpr (PHASE == kWhole || PHASE == kCount) {
-            row.each([&](float x, int) {
-                const float y = row.below(x);
-                if (!R::live(y)) return;
-                atomicAdd(&sm.bucket_n[static_cast<int>(y)], 1u);
-                if (by_p) atomicAdd(&sm.bucket_w[static_cast<int>(y)], R::above(row.weight(x)));  // kZero too much for each
+            u64* sums = PHASE == kWhole ? quarter(sm, list, __builtin_amdgcn_readfirstlane(wave) / kQuarterWaves) : sm.bucket_w;
+            row.each_piece([&](const float(&x)[R::kVec], int) {
+                float y[R::kVec];
+                bool live = false;
+#pragma unroll
+                for (int j = 0; j < R::kVec; ++j) {
+                    y[j] = row.below(x[j]);
+                    live |= R::live(y[j]);
+                }
+                if (!__any(live)) return;
+#pragma unroll
+                for (int j = 0; j < R::kVec; ++j)
+                    if (R::live(y[j])) atomicAdd(&sm.bucket_n[static_cast<int>(y[j])], 1u);
+                if (by_p)
+                    row.weights(x, [&](int j, double w) {
+                        if (R::live(y[j])) atomicAdd(&sums[static_cast<int>(y[j])], R::whole(w));
+                    });
             });
             __syncthreads();
-            if (by_p && tid < kBuckets) sm.bucket_w[tid] -= sm.bucket_n[tid] * R::kZero;
+            if (PHASE == kWhole && by_p && tid < kBuckets)
+                for (int q = 1; q < kQuarters; ++q) sm.bucket_w[tid] += quarter(sm, list, q)[tid];
         } else if (tid < kBuckets) {
             sm.bucket_n[tid] = work->bucket_n[tid];
             sm.bucket_w[tid] = work->bucket_w[tid];
         }
         __syncthreads();
-        uint32_t n = tid < kBuckets ? sm.bucket_n[tid] : 0u;
-        u64 w = tid < kBuckets ? sm.bucket_w[tid] : 0ull;
         if constexpr (PHASE == kCount) {
-            if (n) {
-                atomicAdd(&work->bucket_n[tid], n);
-                if (w) atomicAdd(&work->bucket_w[tid], w);
+            if (tid < kBuckets && sm.bucket_n[tid]) {
+                atomicAdd(&work->bucket_n[tid], sm.bucket_n[tid]);
+                if (sm.bucket_w[tid]) atomicAdd(&work->bucket_w[tid], sm.bucket_w[tid]);
             }
             return;
         }
-        group_sum(sm, n, w);
-        __syncthreads();
-        border.sum = w;
         for (int i = 0; i < 2; ++i) {  // top-k, then top-p of what it keeps
-            if (!(i ? by_p : by_k && static_cast<uint32_t>(k) < n)) continue;
-            const Target target = {i ? Target::kShare : Target::kCount, static_cast<uint32_t>(k), static_cast<double>(p) * static_cast<double>(border.sum), 0ull};
+            if (!(i ? by_p : by_k)) continue;
+            Target target = {i ? found ? Target::kSum : Target::kShare : Target::kCount, static_cast<uint32_t>(k), found ? least_share(p, border.sum) : 0ull, p};
+            find_bin<kBuckets, true, true>(sm, sm.bucket_n, sm.bucket_w, 0u, 0ull, target);
+            if (sm.bin < 0) {  // fewer than k
+                __syncthreads();
+                continue;
+            }
+            target.goal = sm.goal;
+            if (i) target.kind = Target::kSum;
             if constexpr (PHASE == kCollect) {
-                find_bin(sm, tid < kBuckets ? sm.bucket_n[tid] : 0u, tid < kBuckets ? sm.bucket_w[tid] : 0ull, 0u, 0ull, target);
                 held = held_by(sm.before_n, sm.in_n, room);
                 u64 sum = 0;
                 if (held != kNoList)
@@ -658,7 +795,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
                 return;
             } else {
                 if (PHASE == kRest && !found && tid < kWaves) sm.part_w[tid] = work->part_w[tid];
-                border = search(sm, row, list, room, target, by_p, i || !by_p, floor_w, work, held, listed);
+                border = search(sm, row, list, room, target, by_p, i || !by_p, floor_w, work, quartered, held, listed);
                 found = true;
             }
         }
@@ -680,22 +817,20 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     auto kept_sum = [&]() -> u64 {
         u64 sum = 0;
         const bool ties = border.last < a.V;
-        row.each_piece([&](const float(&x)[R::kVec], int i) {
-            uint32_t in = 0;
+        row.each_piece([&](const float(&v)[R::kVec], int i) {
+            float x[R::kVec], most = kNothing;
 #pragma unroll
-            for (int j = 0; j < R::kVec; ++j) in |= x[j] > low ? 1u << j : 0u;
+            for (int j = 0; j < R::kVec; ++j) x[j] = v[j];
             if (ties) {
 #pragma unroll
                 for (int j = 0; j < R::kVec; ++j)
-                    if (x[j] == tied && i + j > border.last) in &= ~(1u << j);
+                    if (x[j] == tied && i + j > border.last) x[j] = kNothing;
             }
-            if (!__any(in)) return;
 #pragma unroll
-            for (int j = 0; j < R::kVec; ++j) {
-                const double w = row.weight(x[j]);
-                sum += (in >> j & 1 && w >= floor_w ? R::above(w) : R::kZero) - R::kZero;
-                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // eight side by side do not fit the registers
-            }
+            for (int j = 0; j < R::kVec; ++j) most = fmaxf(most, x[j]);
+            if (!__any(most > low)) return;
+            row.weights(x, [&](int j, double w) { sum += R::above_if((x[j] > low) & (w >= floor_w), w); });
+            sum -= R::kVec * R::kZero;
         });
         return sum;
     };
@@ -716,27 +851,23 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
         // by indexes, 256 at a time, then 1
         int first = 0;
         u64 total = 0, passed = 0;
-        Target target = {Target::kPass, 0u, 0.0, 0ull};
+        Target target = {Target::kPass, 0u, 0ull, u};
         for (int shift = 8; shift >= 0; shift -= 8) {
             sm.bin_w[tid] = 0ull;
             __syncthreads();
-            u64 sum = 0;
             for (uint32_t e = tid; e < listed; e += kThreads) {
-                const uint32_t key = static_cast<uint32_t>(list[e] >> 32);
                 const int i = static_cast<int>(list[e] & 0xFFFFFFFFu), bin = (i - first) >> shift;
                 if (bin < 0 || bin >= 1024) continue;
-                const u64 w = kept(unordered(key), i);
+                const u64 w = kept(unordered(static_cast<uint32_t>(list[e] >> 32)), i);
                 if (w) atomicAdd(&sm.bin_w[bin], w);
-                sum += w;
-            }
-            if (shift) {
-                uint32_t none = 0;
-                total = sum;
-                group_sum(sm, none, total);
-                target.goal = share_of(u, total);
             }
             __syncthreads();
-            find_bin(sm, 0u, sm.bin_w[tid], 0u, passed, target);
+            find_bin<1024, false, true>(sm, nullptr, sm.bin_w, 0u, passed, target);
+            if (shift) {
+                total = sm.total;
+                target.kind = Target::kSum;
+                target.goal = sm.goal;
+            }
             passed = sm.before_w;
             first += sm.bin << shift;
             __syncthreads();
@@ -745,34 +876,53 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
             if (static_cast<int>(list[e] & 0xFFFFFFFFu) == first) done(first, unordered(static_cast<uint32_t>(list[e] >> 32)), total);
         return;
     }
-    if (held == kBucket && !(by_k && by_p)) {  // pass 3 left the parts' sums, but for the bucket's
+    const int part = row.part();
+    bool summed = true;
+    if (held == kBucket && (quartered || !(by_k && by_p))) {  // the parts' sums, but for the bucket's, are there
         for (uint32_t e = tid; e < listed; e += kThreads) {
             const uint32_t key = static_cast<uint32_t>(list[e] >> 32);
-            const int i = static_cast<int>(list[e] & 0xFFFFFFFFu);
+            const int i = static_cast<int>(list[e] & 0xFFFFFFFFu), p = (i + row.skip) / R::kVec / part;
             const u64 w = kept(unordered(key), i);
-            if (w) atomicAdd(&sm.part_w[(i + row.skip) / R::kVec / row.part()], w);
+            if (w) atomicAdd(&sm.part_w[quartered ? p / kQuarterWaves * kQuarterWaves : p], w);
         }
     } else if (PHASE == kRest && !found) {
         if (tid < kWaves) sm.part_w[tid] = work->part_w[tid];
     } else {
-        u64 sum = kept_sum();
-        uint32_t none = 0;
-        wave_scan(none, sum);
-        if (lane == 63) sm.part_w[wave] = sum;
+        summed = quartered = false;
     }
-    __syncthreads();
-    u64 total = 0;
+    // the part that holds the token; of a quarter its sixteenths are summed first
+    u64 total = 0, goal = 0;
+    int w;
+    for (bool first = true;; first = false) {
+        if (!summed) {
+            u64 sum = kept_sum();
+            uint32_t none = 0;
+            wave_scan(none, sum);
+            if (lane == 63) sm.part_w[wave] = sum;
+        }
+        __syncthreads();
+        if (first) {
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) total += sm.part_w[i];
-    u64 goal = share_of(u, total);
-    int w = 0;
-    while (w < kWaves - 1 && goal >= sm.part_w[w]) goal -= sm.part_w[w++];
+            for (int i = 0; i < kWaves; ++i) total += sm.part_w[i];
+            goal = share_of(u, total);
+        }
+        w = 0;
+        while (w < kWaves - 1 && goal >= sm.part_w[w]) goal -= sm.part_w[w++];
+        if (!quartered) break;
+        quartered = summed = false;
+        row.from = min(row.pieces, w * part);
+        row.to = min(row.pieces, (w + kQuarterWaves) * part);
+        __syncthreads();
+    }
     // that part's logits, a run of them a thread
-    const int begin = max(0, w * row.part() * R::kVec - row.skip), end = min(a.V, (w + 1) * row.part() * R::kVec - row.skip);
+    const int each = (row.to - row.from + kWaves - 1) / kWaves;
+    const int begin = max(0, (row.from + w * each) * R::kVec - row.skip), end = min(a.V, min(row.to, row.from + (w + 1) * each) * R::kVec - row.skip);
     const int run = (end - begin + kThreads - 1) / kThreads, first = min(end, begin + tid * run), last = min(end, first + run);
     u64 own = 0;
     for (int i = first; i < last; ++i) own += kept(row.at(i), i);
-    find_bin(sm, 0u, own, 0u, 0ull, Target{Target::kPass, 0u, 0.0, goal});
+    sm.bin_w[tid] = own;
+    __syncthreads();
+    find_bin<1024, false, true>(sm, nullptr, sm.bin_w, 0u, 0ull, Target{Target::kSum, 0u, goal + 1, 0.f});
     if (tid == sm.bin) {
         u64 left = goal - sm.before_w;
         for (int i = first; i < last; ++i) {
@@ -791,7 +941,7 @@ template <bool F16, bool STAGED, int PHASE>
 hipError_t run(const SampleArgs& a, int64_t groups, int row_bytes, hipStream_t st) {
     static std::atomic<uint64_t> done{0};
     constexpr int fixed = (sizeof(Shared) + 15) / 16 * 16;
-    static_assert(fixed + kStageBytes + 1024 * 8 <= kLdsBytes && fixed + kRingBytes + kMostList * 8 <= kLdsBytes, "fits a compute unit's LDS");
+    static_assert(fixed + kStageBytes + 1024 * 8 <= kLdsBytes && fixed + kRingBytes + kMostList * 8 <= kLdsBytes && 1024 >= kBuckets, "fits a compute unit's LDS");
     const auto k = sample_kernel<F16, STAGED, PHASE>;
     const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(k), kLdsBytes, done);
     if (e != hipSuccess) return e;
