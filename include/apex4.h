@@ -414,8 +414,8 @@ int apex4_w4a4_gemm_mx_ws(const uint8_t* A_6, const uint8_t* e_a,
  * apex4_w8a8_linear: both, Y bit for bit as after the two calls.  A_8_work [M, K] and
  *   s_a_work [M] are scratch (a single token is quantized on the way and leaves them alone).
  *
- * All buffers device memory, 16-byte aligned.  M >= 0, N >= 1, K % 32 == 0, 32 <= K <
- * 131072; each operand's codes under 4 GiB (M K and N K below 2^32).
+ * All buffers device memory, 16-byte aligned; outputs and scratch overlap no input.
+ * M >= 0, N >= 1, K % 32 == 0, 32 <= K < 131072; each operand's codes under 4 GiB (M K and N K below 2^32).
  */
 int apex4_quantize_act8(const void* x, int64_t M, int64_t K, int8_t* A_8, float* s_a, void* stream);
 int apex4_w8a8_gemm(const int8_t* A_8, const float* s_a, const int8_t* W_8, const float* s_w, int64_t M, int64_t N, int64_t K,
@@ -633,8 +633,8 @@ int apex4_pages_copy(void* pool, int64_t planes, int64_t page_bytes, int64_t n_p
  *   workspace: apex4_sample_workspace_size bytes, 16-byte aligned (NULL where that is 0); calls
  *   that share one must be ordered on one stream.  Where rows are few and long,
  *   several workgroups share each.
- * logits aligned like their type (the
- * aligned 16-byte pieces that hold a row's logits are read whole), the others 4-byte.  B up to 2^21, V up to 2^18.
+ * Alignment: logits that of their type (the aligned 16-byte pieces that hold a row's
+ * logits are read whole), the others 4 bytes.  B up to 2^21, V up to 2^18, stride at least V.
  */
 #define APEX4_LOGITS_FP16 0
 #define APEX4_LOGITS_FP32 1

@@ -13,8 +13,10 @@ not gfx950 the call raises.
     lin = W4A4Linear(w, G); y = lin(x)                  # drop-in layer (weights quantized once)
 
 The paged key-value cache and the attention over it (``PagedKVCache`` and the
-``apex4_kv_*``, ``apex4_attn_*`` and ``apex4_pages_*`` calls) are in ``cache.py``
-and are names of this package too.
+``apex4_kv_*``, ``apex4_attn_*`` and ``apex4_pages_*`` calls) are in ``cache.py``,
+rotary positions (``apex4_rope``, ``apex4_rope_freq``) in ``rotary.py``, linears in 8 bits
+(``W8A8Linear``, ``apex4_quantize_act8``, ``apex4_w8a8_*``) in ``linear8.py`` and sampling
+(``apex4_sample``) in ``sampling.py``; all are names of this package too.
 """
 from __future__ import annotations
 

@@ -17,15 +17,26 @@
 // through a ring in LDS that keeps four loads a wave in flight and no registers.  Passes
 // over the row:
 //   1  the largest logit;
-//   2  only for top-k or top-p: counts and sums by buckets of 1/16 octave below it; a scan
-//      gives the bucket of the border;
+//   2  only for top-k or top-p: counts and sums by buckets of 1/16 octave below it, the sums
+//      by quarters of the row; a scan gives the bucket of the border;
 //   3  the logits down to that bucket into a list, if it holds them; then all that follows
 //      goes over the list.  If not, the bucket's own go there, and the weights before it
-//      are summed by the waves' parts of the row.  The range of the bucket's logits is
-//      split into 1024 until one value is left, and for equal ones their indexes, 256 and
-//      then 1 at a time (where the list does not even hold the bucket, over the row);
-//   4  the token: by indexes in the list, or by the waves' parts of the row, then the
-//      logits of the part that holds it.
+//      are known by quarters, or are summed by the waves' parts of the row.  The range of
+//      the bucket's logits is split into 1024 until one value is left, and for equal ones
+//      their indexes, 256 and then 1 at a time (where the list does not even hold the bucket,
+//      over the row);
+//   4  the token: by indexes in the list, or by the quarter that holds it and that one's
+//      sixteenths, or by the waves' parts, then the logits of the part.
+//
+// Bound by the arithmetic of a row's one compute unit and by the steps that follow each
+// other.  48 rows of 32000 binary16 logits with top-p take 34 to 38 us, of which the load
+// and pass 1 are 2.7, pass 2 8.5 (3.3 without weights), pass 3 6.3, each search through
+// the bins 1.2, the token 2.4 from the list or 5 from the row; with top-k 50 19 us, with
+// neither 14.  256 rows of 131072 binary32 logits with top-p: 112 us; pass 1 comes from
+// memory in 20 us, the others as fast from the cache behind it, and weights add 20 to pass 2.
+// Tried: weights one after the other, each in its own branch (+10 %), pass 3 that weighs all
+// that is before the bucket (+12 us there), sixteen waves for the bins (+0.3 us a search),
+// counts for the list by scans of the wave instead of ballots (+2 %).
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 #include <stddef.h>
@@ -962,9 +973,10 @@ hipError_t run_shared(const SampleArgs& a, int64_t B, hipStream_t st) {
 }  // namespace
 
 // Sharing takes three more launches (some 8 us where the host keeps up, 15 where it does
-// not) and a row's passes a sixteenth of their time.  top-p over 131072 binary32 logits, us shared
-// and not: 1 row 43 and 75, 8 rows 50 and 75, 32 rows 72 and 100, 64 rows 107 and 102; over 65000 of binary16 1
-// row 39 and 57, 64 rows 96 and 57; 32000: 35 and 30.
+// not) and a row's passes a sixteenth of their time.  top-p, us one workgroup a row and
+// shared: 131072 binary32 logits 1 row 86 and 43, 32 rows 89 and 64, 64 rows 88 and 96;
+// 65000 of binary16 1 row 48 and 37, 16 rows 54 and 46, 32 rows 52 and 57; 32000 1 row 23 and
+// 26, 32 rows 34 and 54.
 int64_t sample_workspace(int64_t B, int64_t V, bool) {
     const bool shared = B > 0 && V >= kSharedLogits && B * kWaves * kSharedLogits <= device_cu_count() * V;
     return shared ? B * static_cast<int64_t>(sizeof(Work)) : 0;

@@ -140,6 +140,20 @@ def test_two_values(pk):
                 assert int(got) == want
 
 
+@pytest.mark.parametrize("B,V,dtype", [(14, 32000, np.float16), (14, 31999, np.float32), (24, 70001, np.float32), (3, 70001, np.float16)])
+def test_top_p_and_min_p_together(pk, B, V, dtype):
+    """min-p's border behind top-p's, beside it in the same bucket, and before it; tokens in
+    every part of the row."""
+    g = np.random.default_rng(V)
+    x = (g.standard_normal((B, V)) * 1.5).astype(dtype)
+    u = ((np.arange(B) + g.random(B)) / B).astype(F32)
+    for p in (0.3, 0.8, 0.97):
+        w = np.sort(np.exp((x[0] - x[0].max()).astype(np.float64)))[::-1]
+        border = w[(np.cumsum(w) < p * w.sum()).sum()]
+        for near in (1e-3, 0.5, 0.97, 0.999, 1.001, 1.03, 2.0, 30.0):
+            check(pk, x, u, p=p, least=border * near)
+
+
 @pytest.mark.parametrize("V", [600, 50001, 131072])
 def test_borders_at_zero(pk, V):
     """Zeros of both signs are one value, at the border, above it and as the largest."""
