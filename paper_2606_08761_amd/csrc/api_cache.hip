@@ -70,6 +70,17 @@ int check_rows(int64_t T, int64_t heads, int64_t D, int64_t stride) {
     return APEX4_OK;
 }
 
+// Whether T rows of n elements of x and of out_n of out share memory.  Of unequal strides the
+// whole ranges count.
+bool overlap(const void* x, int64_t x_stride, int64_t n, const void* out, int64_t out_stride, int64_t out_n, int64_t T) {
+    if (T < 1) return false;
+    const int64_t a = static_cast<int64_t>(reinterpret_cast<uintptr_t>(x) / 2), b = static_cast<int64_t>(reinterpret_cast<uintptr_t>(out) / 2);
+    if (a + (T - 1) * x_stride + n <= b || b + (T - 1) * out_stride + out_n <= a) return false;
+    if (T == 1 || x_stride != out_stride) return true;
+    const int64_t d = ((b - a) % x_stride + x_stride) % x_stride;  // from a row of x on to the next one of out
+    return d < n || d + out_n > x_stride;
+}
+
 int make_rotary(Rotary& r, const double* freq, int64_t D, int64_t rot, int layout, float mag) {
     if (rot < 2 || rot > D || rot % 2 != 0) return APEX4_ERR_SHAPE;
     if (layout != APEX4_ROPE_HALF && layout != APEX4_ROPE_INTERLEAVED) return APEX4_ERR_SHAPE;
@@ -178,6 +189,7 @@ int apex4_rope(const void* x, int64_t x_stride, const int32_t* positions, int64_
     if ((rc = check_rows(T, heads, head_dim, x_stride)) || (rc = check_rows(T, heads, head_dim, out_stride))) return rc;
     if (T > 1 && x == out && x_stride != out_stride) return APEX4_ERR_SHAPE;
     if (!aligned(x, 16) || !aligned(positions, 4) || !aligned(freq, 8) || !aligned(out, 16)) return APEX4_ERR_ALIGN;
+    if (x != out && overlap(x, x_stride, heads * head_dim, out, out_stride, heads * head_dim, T)) return APEX4_ERR_SHAPE;
     if ((rc = check_device())) return rc;
     if (T == 0) return APEX4_OK;
     return status_of(apex4::launch_rope(static_cast<const uint16_t*>(x), x_stride, positions, T, static_cast<int>(heads),
@@ -205,7 +217,12 @@ int apex4_kv_append_rope(const void* q, int64_t q_stride, int64_t heads, void* q
     if (heads && q == q_out && T > 0) return APEX4_ERR_SHAPE;
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(q_start, 4) || !aligned(positions, 4) || !aligned(freq, 8)) return APEX4_ERR_ALIGN;
     if (heads && (!aligned(q, 16) || !aligned(q_out, 16))) return APEX4_ERR_ALIGN;
-    if ((rc = check_view_pointers(c)) || (rc = check_device())) return rc;
+    if ((rc = check_view_pointers(c))) return rc;
+    const int64_t row = heads * head_dim, kv_row = kv_heads * head_dim;
+    if (heads && (overlap(q, q_stride, row, q_out, row, row, T) || overlap(k, k_stride, kv_row, q_out, row, row, T) ||
+                  overlap(v, v_stride, kv_row, q_out, row, row, T)))
+        return APEX4_ERR_SHAPE;
+    if ((rc = check_device())) return rc;
     if (T == 0) return APEX4_OK;
     apex4::RopeRows a;
     a.q = static_cast<const uint16_t*>(q);

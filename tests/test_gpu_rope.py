@@ -86,6 +86,29 @@ def test_infinities_and_nan_stay_in_their_pair(pk):
     assert torch.isinf(y[1, 0, 40])
 
 
+def test_outputs_beside_the_inputs(pk):
+    """Rows whose outputs are other heads of the same buffer; what overlaps is refused."""
+    import torch
+    g = np.random.default_rng(4)
+    whole = rows(g, 33, 12, 64)
+    positions = dev(g.integers(0, 5000, 33).astype(np.int32))
+    freq, _ = pk.apex4_rope_freq(64)
+    want = pk.apex4_rope(whole[:, 3:6], positions, freq)
+    kept = whole.clone()
+    for first in (0, 6, 9):
+        buffer = kept.clone()
+        pk.apex4_rope(buffer[:, 3:6], positions, freq, out=buffer[:, first:first + 3])
+        assert buffer[:, first:first + 3].equal(want)
+        rest = [h for h in range(12) if not first <= h < first + 3]
+        assert buffer[:, rest].equal(kept[:, rest])
+    for first in (1, 2, 4, 5):
+        with pytest.raises(pk.Apex4Error):
+            pk.apex4_rope(kept[:, 3:6], positions, freq, out=kept[:, first:first + 3])
+    with pytest.raises(pk.Apex4Error):  # the next token's rows
+        pk.apex4_rope(kept[:32, 3:6], positions[:32], freq, out=kept[1:, 3:6])
+    assert kept.equal(whole)
+
+
 def test_no_tokens(pk):
     import torch
     freq, _ = pk.apex4_rope_freq(64)

@@ -42,6 +42,21 @@ def test_without_queries_their_pointers_are_not_asked_for(L):  # noqa: F811
     assert L.apex4_kv_append_rope(*args(FUSED_ORDER, FUSED, heads=0, q=NULL, q_out=NULL, q_stride=0, table=P + 2)) == -4
 
 
+@pytest.mark.parametrize("out,out_stride,T", [
+    (P + 2032, 2048, 5), (P + 2064, 2048, 5), (P + 16, 2048, 5), (P - 16, 2048, 1), (P + 2032, 2048, 1), (P + 3 * 4096 + 16, 2048, 5),
+    (P - 3 * 4096 - 16, 2048, 5), (P + 2048, 1024, 5), (P - 5 * 2048 + 16, 1024, 5)])
+def test_outputs_that_overlap(L, out, out_stride, T):  # noqa: F811
+    """Rows of 1024 values, those of x 2048 apart: between them is room for out's.  (Without
+    an overlap the call would run; that is tested on the device.)"""
+    assert L.apex4_rope(*args(ROPE_ORDER, ROPE, x_stride=2048, out=out, out_stride=out_stride, T=T)) == -2
+    if out_stride == 1024:  # as q_out, which has no gaps
+        far = dict(q=P + (1 << 29), k=P + (1 << 30), v=P + (1 << 31), q_stride=2048, q_out=out, T=T)
+        assert L.apex4_kv_append_rope(*args(FUSED_ORDER, FUSED, **{**far, "q": P})) == -2
+    for name in ("k", "v"):
+        far = dict(q=P + (1 << 29), k=P + (1 << 30), v=P + (1 << 31), q_out=P + 16)
+        assert L.apex4_kv_append_rope(*args(FUSED_ORDER, FUSED, **{**far, name: P})) == -2
+
+
 def test_binding_refuses(L):  # noqa: F811
     import torch
 
