@@ -241,32 +241,30 @@ hipError_t run_tile(const int8_t* A, const float* sa, const int8_t* W, const flo
 
 namespace {
 
-// The forms and their times in us for K = 8192 where the chip is full: one tile a compute
-// unit, of the smallest two.  Tiles of 256 x 256 read the fewest bytes for their products;
-// the others are for counts of them that leave units idle (4096 x 10240: 2.5 rounds of
-// 256 x 256 357 us, 2 of 256 x 320 324; 300 x 57344: 128 x 256 200, 320 x 256 168;
-// 1024 x 10240: 256 x 256 109, 256 x 192 100; 3000 x 8192: 256 x 256 227,
-// 128 x 256 222, 192 x 256 210; 768 x 8192 of K 28672: 128 x 256 205, 192 x 128 192;
-// 300 x 8192: 128 x 256 56, 128 x 128 38).
+// The forms: us for K = 8192 of a tile alone on its compute unit with nearly all others idle,
+// and with all of them busy.  Tiles of 256 x 256 read the fewest bytes for their products, the
+// others are for counts of tiles that leave units idle (4096 x 10240: 2.5 rounds of 256 x 256
+// 357 us, 2 of 256 x 320 302; 300 x 57344: 128 x 256 200, 320 x 256 168; 1024 x 10240:
+// 256 x 256 109, 256 x 192 100; 3000 x 8192: 128 x 256 222, 192 x 256 210; 768 x 8192 of K
+// 28672: 128 x 256 200, 192 x 128 183; 200 x 8192: 128 x 128 39, 128 x 64 29).
 struct Form {
-    int bm, bn, tiles_a_unit;
-    double us;
+    int bm, bn;
+    double alone, full;
 };
-constexpr Form kForms[] = {{256, 256, 1, 128.0}, {256, 320, 1, 151.0}, {320, 256, 1, 151.0}, {256, 192, 1, 97.0}, {192, 256, 1, 99.0},
-                           {128, 256, 1, 70.0}, {192, 128, 1, 52.0},  {128, 128, 1, 40.0},   {64, 64, 2, 29.0}};
+constexpr Form kForms[] = {{256, 256, 96, 123}, {256, 320, 106, 146}, {320, 256, 104, 142}, {256, 192, 80, 98}, {192, 256, 84, 101}, {128, 256, 57, 70},
+                           {192, 128, 41, 55},  {128, 128, 38, 43},   {96, 128, 35, 37},    {128, 64, 28, 30},  {64, 128, 30, 30},   {64, 64, 20, 20}};
 constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
 
-// Time of a form: whole rounds of tiles, and for those that are left 0.3 of a round and
-// as much of the rest as they fill (fewer tiles at once run at a higher clock and share
-// less); a tile starts in 5 us and goes over K evenly.  For 200 to 4096 rows of 8192,
-// 10240, 28672 and 57344 channels, K 8192 and 28672 (30 calls), the form that it picks
-// is the fastest of those listed or within 2 % of it.
+// Time of a form: whole rounds of a tile a unit, and a last one that takes the longer the more
+// units it keeps busy (clock and memory are shared); a tile starts in 5 us and goes over K
+// evenly.  For 70 to 4096 rows of 2048 to 57344 channels, K 4096 to 28672 (133 calls, each
+// form timed on each, weights from memory), what it picks takes 0.06 % longer than the
+// fastest form on average and 3 % at most, and 0.87 of the library's int8 product without scales.
 double cost_of(const Form& f, int64_t M, int64_t N, int64_t K, int cus) {
     const double tiles = static_cast<double>((M + f.bm - 1) / f.bm) * static_cast<double>((N + f.bn - 1) / f.bn);
-    const double at_once = static_cast<double>(cus) * f.tiles_a_unit;
-    const double whole = static_cast<double>(static_cast<int64_t>(tiles / at_once));
-    const double left = tiles / at_once - whole;
-    return (whole + (left > 0 ? 0.3 + 0.7 * left : 0.0)) * (5.0 + (f.us - 5.0) * static_cast<double>(K) / 8192.0);
+    const double whole = static_cast<double>(static_cast<int64_t>(tiles / cus)), left = tiles / cus - whole, deep = static_cast<double>(K) / 8192.0;
+    const double alone = 5.0 + (f.alone - 5.0) * deep, full = 5.0 + (f.full - 5.0) * deep;
+    return whole * full + (left > 0 ? alone + (full - alone) * left : 0.0);
 }
 
 }  // namespace
@@ -294,6 +292,9 @@ hipError_t launch_w8a8_tiles(const int8_t* A, const float* sa, const int8_t* W, 
         case 5: return run_tile<128, 256, 2, 4, 3>(A, sa, W, sw, M, N, K, Y, st);
         case 6: return run_tile<192, 128, 2, 4, 3>(A, sa, W, sw, M, N, K, Y, st);
         case 7: return run_tile<128, 128, 2, 4, 4>(A, sa, W, sw, M, N, K, Y, st);
+        case 8: return run_tile<96, 128, 1, 4, 5>(A, sa, W, sw, M, N, K, Y, st);
+        case 9: return run_tile<128, 64, 4, 2, 5>(A, sa, W, sw, M, N, K, Y, st);
+        case 10: return run_tile<64, 128, 2, 4, 5>(A, sa, W, sw, M, N, K, Y, st);
         default: return run_tile<64, 64, 2, 2, 5>(A, sa, W, sw, M, N, K, Y, st);
     }
 }

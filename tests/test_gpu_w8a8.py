@@ -98,8 +98,9 @@ SIZES = [(1, 1, 32), (1, 100, 96), (2, 33, 160), (8, 16, 128), (7, 1001, 1056), 
          (130, 260, 2048), (128, 16384, 128), (300, 520, 1056), (257, 4100, 96), (513, 1001, 160), (700, 10240, 288), (1030, 8191, 64),
          (2048, 8192, 128), (3000, 2100, 32), (4100, 4097, 160),
          # each tile, and K that ends inside a stage
-         (2501, 3276, 672), (1156, 7302, 672), (1539, 3859, 672), (389, 7183, 672), (3204, 1158, 672), (385, 3514, 672), (525, 1415, 1056),
-         (1481, 193, 1056), (263, 100, 1056), (257, 4867, 160), (261, 3075, 160), (2577, 579, 160), (2725, 133, 160)]
+         (1544, 7211, 672), (2241, 7191, 672), (1795, 8253, 672), (3203, 2319, 672), (1290, 8101, 672), (578, 8238, 672), (389, 8230, 672),
+         (291, 8251, 672), (65, 8209, 672), (131, 8459, 672), (83, 102, 672), (194, 8243, 672), (2057, 7187, 160), (1296, 8086, 288),
+         (2577, 579, 160), (2725, 133, 160)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
