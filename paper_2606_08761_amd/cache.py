@@ -119,7 +119,7 @@ def _empty(like, shape, dtype, stream):
     """Memory of the stream that the call runs on: what an earlier owner on another
     stream still has under way does not reach it, nor this call its next owner."""
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
+        return like.new_empty(shape) if like.dtype is dtype else like.new_empty(shape, dtype=dtype)
     with _torch().cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
 
@@ -185,18 +185,22 @@ def apex4_kv_append_rope(q, k, v, k_pages, v_pages, table, kv_len, page: int, fr
     vp, vs = _rows(v, "v")
     fp, rot = _freq(freq)
     qp, qs, heads, op = None, 0, 0, None
+    given = out
     if q is not None:
         qp, qs = _rows(q, "q")
-        if q.shape[0] != T or q.shape[2] != D:
+        rows, heads, size = q.shape
+        if rows != T or size != D:
             raise ValueError("q must be [T, heads, head_dim], as k")
-        heads = q.shape[1]
-        out = _output(out, q.shape, q, stream)
-        op = _ptr(out, torch.float16, "out")
+        if out is None:
+            out = _empty(q, (T, heads, D), torch.float16, stream)
+            op = out.data_ptr()
+        else:
+            op = _ptr(_output(out, (T, heads, D), q, stream), torch.float16, "out")
     if positions is not None and tuple(positions.shape) != (T,):
         raise ValueError("positions must be [T]")
     kpp, vpp, n = _planes(k_pages, v_pages, H, D, page, cache)
     tp, width, lp, B = _tables(table, kv_len)
-    _one_device(k, v, q, out, k_pages, v_pages, table, kv_len, freq, q_start, positions)
+    _one_device(k, v, q, given, k_pages, v_pages, table, kv_len, freq, q_start, positions)
     rc = lib().apex4_kv_append_rope(qp, qs, heads, op, kp, ks, vp, vs, _starts(q_start, B), T,
                                     None if positions is None else _index(positions, "positions"), fp, rot, _layout(layout),
                                     scale, kpp, vpp, n, tp, width, lp, B, H, D, page, _kind(cache), _stream(k, stream))

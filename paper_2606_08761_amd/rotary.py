@@ -10,7 +10,7 @@ from __future__ import annotations
 import math
 
 from . import _check, _stream, _torch, lib
-from .cache import _freq, _layout, _one_device, _output, _ptr, _rows
+from .cache import _empty, _freq, _layout, _one_device, _output, _ptr, _rows
 
 
 def apex4_rope_freq(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: int = 8192,
@@ -64,9 +64,13 @@ def apex4_rope(x, positions, freq, layout: str = "half", scale: float = 1.0, out
     if positions.dim() != 1 or positions.shape[0] != T:
         raise ValueError("positions must be [T]")
     fp, rot = _freq(freq)
-    out = _output(out, (T, H, D), x, stream)
-    op, os = _rows(out, "out")
-    _one_device(x, positions, freq, out)
+    if out is None:
+        out = _empty(x, (T, H, D), torch.float16, stream)
+        op, os = out.data_ptr(), H * D
+        _one_device(x, positions, freq)
+    else:
+        op, os = _rows(_output(out, (T, H, D), x, stream), "out")
+        _one_device(x, positions, freq, out)
     rc = lib().apex4_rope(xp, xs, _ptr(positions, torch.int32, "positions"), T, H, D, fp, rot, _layout(layout), scale, op, os,
                           _stream(x, stream))
     _check("apex4_rope", rc)
