@@ -29,14 +29,14 @@
 //      sixteenths, or by the waves' parts, then the logits of the part.
 //
 // Bound by the arithmetic of a row's one compute unit and by the steps that follow each
-// other.  48 rows of 32000 binary16 logits with top-p take 34 to 38 us, of which the load
+// other.  48 rows of 32000 binary16 logits with top-p take 31 to 34 us, of which the load
 // and pass 1 are 2.7, pass 2 8.5 (3.3 without weights), pass 3 6.3, each search through
 // the bins 1.2, the token 2.4 from the list or 5 from the row; with top-k 50 19 us, with
 // neither 14.  256 rows of 131072 binary32 logits with top-p: 112 us; pass 1 comes from
 // memory in 20 us, the others as fast from the cache behind it, and weights add 20 to pass 2.
-// Tried: weights one after the other, each in its own branch (+10 %), pass 3 that weighs all
-// that is before the bucket (+12 us there), sixteen waves for the bins (+0.3 us a search),
-// counts for the list by scans of the wave instead of ballots (+2 %).
+// Tried: weights one after the other, each in its own branch (+4 to 8 %), pass 3 that weighs
+// all that is before the bucket (+18 us there), sixteen waves for a scan of the bins (+0.6
+// us), places in the list by a scan of the wave instead of ballots (+2 %).
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 #include <stddef.h>
@@ -57,6 +57,7 @@ constexpr int kBuckets = 736;          // 1/16 octave each
 constexpr int kStageBytes = 126 << 10; // of a row in LDS
 constexpr int kSharedLogits = 48 << 10;  // rows from here on are shared where they are few
 constexpr int kLdsBytes = 160 << 10, kMostList = 8704;
+constexpr uint32_t kShortList = 4096;  // logits
 constexpr int kDepth = 4, kRingBytes = kWaves * kDepth * 1024;
 constexpr int kSteps = 512, kStepBits = 9;  // table of 2^(i / 512)
 constexpr double kMagic = 0x1.8p52;    // added to a number below 2^51: its nearest whole one in the low bits
@@ -418,9 +419,11 @@ struct Border {
 // What the list holds: nothing, the bucket of the border, or all down to it.
 enum Held : int { kNoList, kBucket, kAll };
 
-// Where a search that found its bucket keeps the list, for n logits.
-__device__ __forceinline__ int held_by(uint32_t before, uint32_t members, uint32_t room) {
-    return before + members <= room ? kAll : members <= room ? kBucket : kNoList;
+// What goes into a list with room for `room` logits: up to `most` all of them.  Where pass 2
+// left the quarters' sums a long list costs more than a quarter (48 rows of 32000 that keep
+// 7900: 37.4 us with all in the list, 33.6 with the bucket; that keep 2400: 30.2 and 32.9).
+__device__ __forceinline__ int held_by(uint32_t before, uint32_t members, uint32_t room, uint32_t most) {
+    return before + members <= min(room, most) ? kAll : members <= room ? kBucket : kNoList;
 }
 
 // The logits of the bucket from `top` to `end` (1/16 octaves), or all down to it, into `list`,
@@ -501,7 +504,7 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
     };
     if (held != kAll) {
         const bool ready = held < 0 && work != nullptr;
-        held = held_by(before_n, members, room);
+        held = held_by(before_n, members, room, quartered && parts ? kShortList : room);
         listed = held == kAll ? before_n + members : members;
         // (the bucket's end is at 2^-((bucket + 1) / 16) but for the roundings of below())
         quartered = quartered && parts && held == kBucket && least <= exp2(45.0 - 1e-3 - (bucket + 1) * (1.0 / 16.0));
@@ -796,7 +799,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
             target.goal = sm.goal;
             if (i) target.kind = Target::kSum;
             if constexpr (PHASE == kCollect) {
-                held = held_by(sm.before_n, sm.in_n, room);
+                held = held_by(sm.before_n, sm.in_n, room, room);
                 u64 sum = 0;
                 if (held != kNoList)
                     sum = collect(row, work->list, &work->listed, room, held, static_cast<float>(sm.bin), static_cast<float>(sm.bin + 1), i || !by_p, floor_w);

@@ -223,7 +223,7 @@ def test_extreme_settings(pk):
         check(pk, x, g.random(4), t=t)
         check(pk, x, g.random(4), t=t, p=0.9, k=1000)
     check(pk, (x * 1e37).astype(F32), g.random(4), t=1e38)   # differences past binary32's range
-    check(pk, (x * 1e38).clip(-3e38, 3e38).astype(F32), g.random(4), t=1e38, p=0.8)
+    check(pk, (x.astype(np.float64) * 1e38).clip(-3e38, 3e38).astype(F32), g.random(4), t=1e38, p=0.8)
     tokens, probs = pk.apex4_sample(dev(x), dev(np.array([0.0, 0.25, 0.5, 1 - 2.0 ** -24], F32)), temperature=float("inf"))
     assert tokens.tolist() == [0, 750, 1500, 3000]
     # off: NaN, numbers that keep everything
