@@ -18,7 +18,8 @@
 // over the row:
 //   1  the largest logit;
 //   2  only for top-k or top-p: counts and sums by buckets of 1/16 octave below it, the sums
-//      by quarters of the row; a scan gives the bucket of the border;
+//      by quarters of the row (of a small top-k's top-p later, over the list); a scan
+//      gives the bucket of the border;
 //   3  the logits down to that bucket into a list, if it holds them; then all that follows
 //      goes over the list.  If not, the bucket's own go there, and the weights before it
 //      are known by quarters, or are summed by the waves' parts of the row.  The range of
@@ -32,7 +33,7 @@
 // other.  48 rows of 32000 binary16 logits with top-p take 31 to 34 us, of which the load
 // and pass 1 are 2.7, pass 2 8.5 (3.3 without weights), pass 3 6.3, each search through
 // the bins 1.2, the token 2.4 from the list or 5 from the row; with top-k 50 19 us, with
-// neither 14.  256 rows of 131072 binary32 logits with top-p: 112 us; pass 1 comes from
+// both 25, with neither 14.  256 rows of 131072 binary32 logits with top-p: 112 us; pass 1 comes from
 // memory in 20 us, the others as fast from the cache behind it, and weights add 20 to pass 2.
 // Tried: weights one after the other, each in its own branch (+4 to 8 %), pass 3 that weighs
 // all that is before the bucket (+18 us there), sixteen waves for a scan of the bins (+0.6
@@ -58,6 +59,9 @@ constexpr int kStageBytes = 126 << 10; // of a row in LDS
 constexpr int kSharedLogits = 48 << 10;  // rows from here on are shared where they are few
 constexpr int kLdsBytes = 160 << 10, kMostList = 8704;
 constexpr uint32_t kShortList = 4096;  // logits
+// top-p of up to so many that top-k keeps weighs them alone (256 rows of 131072 binary32 logits,
+// top-k 50, top-p 0.9: 78 us, all of them weighed 97; 48 of 32000: 25 and 29).
+constexpr int kFewKept = 1024;
 constexpr int kDepth = 4, kRingBytes = kWaves * kDepth * 1024;
 constexpr int kSteps = 512, kStepBits = 9;  // table of 2^(i / 512)
 constexpr double kMagic = 0x1.8p52;    // added to a number below 2^51: its nearest whole one in the low bits
@@ -483,10 +487,11 @@ __device__ __forceinline__ u64 collect(const R& row, u64* list, uint32_t* listed
 // first's.  parts: the sums of the kept weights before the bucket are left in sm.part_w (min-p's
 // `least` included) where the list holds the bucket alone: of the quarters, if pass 2 left
 // their buckets (quartered, which says afterwards if it is so) and min-p keeps all before the
-// bucket's end, or of the waves' parts.
+// bucket's end, or of the waves' parts.  fresh: the buckets' sums are not there yet and come from
+// the list, which holds all that top-k can keep.
 template <class R>
-__device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, uint32_t room, const Target& target, bool weigh, bool parts, double least,
-                         const Work* work, bool& quartered, int& held, uint32_t& listed) {
+__device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, uint32_t room, const Target& target, bool weigh, bool parts, bool fresh,
+                                         double least, const Work* work, bool& quartered, int& held, uint32_t& listed) {
     const int tid = threadIdx.x;
     const int bucket = sm.bin;
     uint32_t before_n = sm.before_n;
@@ -549,6 +554,7 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
         for (uint32_t i = tid; i < listed; i += kThreads) {
             const float x = unordered(static_cast<uint32_t>(list[i] >> 32)), y = row.below(x);
             if (y >= top && y < end) member(x);
+            if (fresh) atomicAdd(&sm.bucket_w[static_cast<int>(y)], R::whole(row.weight(x)));
         }
     }
     if (high) {
@@ -558,6 +564,10 @@ __device__ __forceinline__ Border search(Shared& sm, const R& row, u64* list, ui
     __syncthreads();
     low = sm.low;
     high = sm.high;
+    if (fresh) {
+        find_bin<kBuckets, true, true>(sm, sm.bucket_n, sm.bucket_w, 0u, 0ull, target);
+        before_w = sm.before_w;
+    }
     // f(key, index): the bucket's are all the logits from low to high
     auto each = [&](auto f) {
         if (held != kNoList) {
@@ -753,28 +763,39 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     int held = -1;
     uint32_t listed = 0;
     bool found = false, quartered = PHASE == kWhole && by_p;  // a border; the quarters' buckets, then their sums, are there
+    // top-p of what a small top-k keeps: only that is weighed, in the list (if it holds all of it)
+    bool few = PHASE == kWhole && by_k && by_p && k <= kFewKept;
     if (by_k || by_p) {
         if constexpr (PHASE == kWhole || PHASE == kCount) {
             u64* sums = PHASE == kWhole ? quarter(sm, list, __builtin_amdgcn_readfirstlane(wave) / kQuarterWaves) : sm.bucket_w;
-            row.each_piece([&](const float(&x)[R::kVec], int) {
-                float y[R::kVec];
-                bool live = false;
+            for (bool first = true;; first = false) {
+                row.each_piece([&](const float(&x)[R::kVec], int) {
+                    float y[R::kVec];
+                    bool live = false;
 #pragma unroll
-                for (int j = 0; j < R::kVec; ++j) {
-                    y[j] = row.below(x[j]);
-                    live |= R::live(y[j]);
-                }
-                if (!__any(live)) return;
+                    for (int j = 0; j < R::kVec; ++j) {
+                        y[j] = row.below(x[j]);
+                        live |= R::live(y[j]);
+                    }
+                    if (!__any(live)) return;
+                    if (first) {
 #pragma unroll
-                for (int j = 0; j < R::kVec; ++j)
-                    if (R::live(y[j])) atomicAdd(&sm.bucket_n[static_cast<int>(y[j])], 1u);
-                if (by_p)
-                    row.weights(x, [&](int j, double w) {
-                        if (R::live(y[j])) atomicAdd(&sums[static_cast<int>(y[j])], R::whole(w));
-                    });
-            });
-            __syncthreads();
-            if (PHASE == kWhole && by_p && tid < kBuckets)
+                        for (int j = 0; j < R::kVec; ++j)
+                            if (R::live(y[j])) atomicAdd(&sm.bucket_n[static_cast<int>(y[j])], 1u);
+                    }
+                    if (by_p && !few)
+                        row.weights(x, [&](int j, double w) {
+                            if (R::live(y[j])) atomicAdd(&sums[static_cast<int>(y[j])], R::whole(w));
+                        });
+                });
+                __syncthreads();
+                if (!few) break;
+                find_bin<kBuckets, true, false>(sm, sm.bucket_n, nullptr, 0u, 0ull, Target{Target::kCount, static_cast<uint32_t>(k), 0ull, 0.f});
+                if (sm.bin >= 0 && sm.before_n + sm.in_n <= room) break;
+                few = false;
+                __syncthreads();
+            }
+            if (PHASE == kWhole && by_p && !few && tid < kBuckets)
                 for (int q = 1; q < kQuarters; ++q) sm.bucket_w[tid] += quarter(sm, list, q)[tid];
         } else if (tid < kBuckets) {
             sm.bucket_n[tid] = work->bucket_n[tid];
@@ -791,7 +812,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
         for (int i = 0; i < 2; ++i) {  // top-k, then top-p of what it keeps
             if (!(i ? by_p : by_k)) continue;
             Target target = {i ? found ? Target::kSum : Target::kShare : Target::kCount, static_cast<uint32_t>(k), found ? least_share(p, border.sum) : 0ull, p};
-            find_bin<kBuckets, true, true>(sm, sm.bucket_n, sm.bucket_w, 0u, 0ull, target);
+            if (i || !few) find_bin<kBuckets, true, true>(sm, sm.bucket_n, sm.bucket_w, 0u, 0ull, target);
             if (sm.bin < 0) {  // fewer than k
                 __syncthreads();
                 continue;
@@ -809,7 +830,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
                 return;
             } else {
                 if (PHASE == kRest && !found && tid < kWaves) sm.part_w[tid] = work->part_w[tid];
-                border = search(sm, row, list, room, target, by_p, i || !by_p, floor_w, work, quartered, held, listed);
+                border = search(sm, row, list, room, target, by_p, i || !by_p, !i && few, floor_w, work, quartered, held, listed);
                 found = true;
             }
         }

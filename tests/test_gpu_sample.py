@@ -140,6 +140,31 @@ def test_two_values(pk):
                 assert int(got) == want
 
 
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+@pytest.mark.parametrize("B,V", [(9, 700), (9, 32000), (30, 70001), (2, 70001)])
+def test_top_p_of_a_small_top_k(pk, B, V, dtype):
+    """As many logits as top-k keeps, fewer, and more equal ones at its border than a list holds."""
+    import torch
+    g = np.random.default_rng(V + B)
+    x = logits(g, B, V, dtype)
+    u = g.random(B)
+    for k in (2, 50, 600, 1024, 1025):
+        for p in (0.2, 0.9):
+            check(pk, x, u, k=k, p=p)
+            check(pk, x, u, k=k, p=p, t=1.7, least=0.02)
+    some = x.copy()
+    some[:, 40:] = -np.inf
+    check(pk, some, u, k=50, p=0.8)
+    check(pk, some, u, k=40, p=0.8)
+    check(pk, some, u, k=39, p=0.8)
+    flat = torch.full((B, V), 0.5, dtype=torch.float16 if dtype == np.float16 else torch.float32, device="cuda")
+    flat[:, 5] = 0.5 + np.log(8.0)  # not exact: its share is near 8
+    got, _ = pk.apex4_sample(flat, dev(u.astype(F32)), top_k=401, top_p=0.5)
+    assert ((got >= 0) & (got <= 198)).all()  # 8 and 400 ones: 196 ones, up to a rounding of the logit
+    got, _ = pk.apex4_sample(flat, torch.full((B,), 1 - 2.0 ** -24, device="cuda"), top_k=401, top_p=0.5)
+    assert ((got >= 194) & (got <= 198)).all()
+
+
 @pytest.mark.parametrize("B,V,dtype", [(14, 32000, np.float16), (14, 31999, np.float32), (24, 70001, np.float32), (3, 70001, np.float16)])
 def test_top_p_and_min_p_together(pk, B, V, dtype):
     """min-p's border behind top-p's, beside it in the same bucket, and before it; tokens in
