@@ -27,9 +27,10 @@ def _matrix(t, name):
 
 
 def _weights(W_8, s_w, K):
-    if _matrix(W_8, "W_8")[1] != K or tuple(s_w.shape) != (W_8.shape[0],):
+    shape = _matrix(W_8, "W_8")
+    if shape[1] != K or s_w.shape != shape[:1]:
         raise ValueError(f"W_8 must be [N, {K}] and s_w [N]")
-    return W_8.shape[0]
+    return shape[0]
 
 
 def apex4_quantize_act8(x, A_8=None, s_a=None, stream=None):
@@ -68,13 +69,18 @@ def apex4_w8a8_linear(x, W_8, s_w, Y=None, A_8_work=None, s_a_work=None, stream=
     M, K = _matrix(x, "x")
     N = _weights(W_8, s_w, K)
     xp = _ptr(x, torch.float16, "x")
-    Y = _output(Y, (M, N), x, stream)
-    A_8_work = _made(A_8_work, (M, K), torch.int8, x, stream, "A_8_work")
-    s_a_work = _made(s_a_work, (M,), torch.float32, x, stream, "s_a_work")
     _one_device(x, W_8, s_w, Y, A_8_work, s_a_work)
+    Y = _output(Y, (M, N), x, stream)
+    if A_8_work is None and s_a_work is None:  # one buffer for both: an allocation is 1.5 us of a small call's 12
+        work = _empty(x, (M * (K + 4),), torch.uint8, stream)
+        Ap = work.data_ptr()
+        sp = Ap + M * K
+    else:
+        A_8_work = _made(A_8_work, (M, K), torch.int8, x, stream, "A_8_work")
+        s_a_work = _made(s_a_work, (M,), torch.float32, x, stream, "s_a_work")
+        Ap, sp = _ptr(A_8_work, torch.int8, "A_8_work"), _ptr(s_a_work, torch.float32, "s_a_work")
     rc = lib().apex4_w8a8_linear(xp, _ptr(W_8, torch.int8, "W_8"), _ptr(s_w, torch.float32, "s_w"), M, N, K,
-                                 _ptr(Y, torch.float16, "Y"), _ptr(A_8_work, torch.int8, "A_8_work"),
-                                 _ptr(s_a_work, torch.float32, "s_a_work"), _stream(x, stream))
+                                 _ptr(Y, torch.float16, "Y"), Ap, sp, _stream(x, stream))
     _check("apex4_w8a8_linear", rc)
     return Y
 
@@ -103,4 +109,6 @@ class W8A8Linear:
         if not x.is_contiguous():
             with _torch().cuda.stream(stream):  # None: the current one
                 x = x.contiguous()
+        if len(shape) == 1:
+            return apex4_w8a8_linear(x, self.W_8, self.s_w, stream=stream)
         return apex4_w8a8_linear(x.view(-1, self.K), self.W_8, self.s_w, stream=stream).view(*shape, self.N)

@@ -207,6 +207,34 @@ def test_more_rows_and_channels_than_a_grid_has(pk):
         assert same(y[:, cols], product(qa, sa, W[cols].cpu().numpy(), sw[cols].cpu().numpy()))
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 24, 64), (1, 20, 32800), (3, 40, 96), (70, 36, 160)])
+def test_scratch_made_here_or_given(pk, M, N, K):
+    """Both buffers, one of them or neither: the same bits.  Both given, they hold the codes
+    and scales afterwards (but for a token that is quantized on the way)."""
+    import torch
+    g = np.random.default_rng(M + K)
+    x, W, sw = dev(g.standard_normal((M, K)).astype(np.float16)), dev(codes(g, N, K)), dev(scales(g, N))
+    want = pk.apex4_w8a8_linear(x, W, sw)
+    A, s = torch.full((M, K), 5, dtype=torch.int8, device="cuda"), torch.full((M,), 5.0, device="cuda")
+    assert pk.apex4_w8a8_linear(x, W, sw, A_8_work=A, s_a_work=s).equal(want)
+    q, t = quantized(x.cpu().numpy())
+    if M > 1:
+        assert same(pk.apex4_w8a8_gemm(A, s, W, sw), want.cpu().numpy()) and np.array_equal(A.cpu().numpy(), q) and np.array_equal(s.cpu().numpy(), t)
+    assert pk.apex4_w8a8_linear(x, W, sw, A_8_work=A).equal(want) and pk.apex4_w8a8_linear(x, W, sw, s_a_work=s).equal(want)
+    layer = pk.W8A8Linear(dev(g.standard_normal((N, K)).astype(np.float16)))
+    y = layer(x)
+    assert layer(x[0]).equal(y[0]) and layer(x.expand(2, M, K)).equal(y.expand(2, M, N))
+    with pytest.raises(ValueError):
+        pk.apex4_w8a8_linear(x, W, sw, A_8_work=A[:, :32])
+    with pytest.raises(TypeError):
+        pk.apex4_w8a8_linear(x, W, sw, A_8_work=A, s_a_work=s.half())
+    with pytest.raises(ValueError):
+        pk.apex4_w8a8_linear(x, W, sw, A_8_work=A.cpu(), s_a_work=s)
+    for odd in (K - 8, K - 1):
+        with pytest.raises(pk.Apex4Error):
+            pk.apex4_w8a8_linear(x[:, :odd].contiguous(), W[:, :odd].contiguous(), sw)
+
+
 def test_rows_with_gaps_on_another_stream(pk):
     """The layer's own copy of such rows is made on the stream of the call."""
     import torch
