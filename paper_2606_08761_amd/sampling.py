@@ -32,7 +32,9 @@ def _need(device, type, B, V):
 def apex4_sample_workspace_size(B: int, V: int, dtype) -> int:
     """Bytes of workspace apex4_sample needs for logits [B, V] of dtype on the current device (0: none)."""
     torch = _torch()
-    return _need(torch.cuda.current_device(), {torch.float16: 0, torch.float32: 1}[dtype], B, V)
+    if dtype is not torch.float16 and dtype is not torch.float32:
+        raise TypeError("logits must be torch.float16 or torch.float32")
+    return _need(torch.cuda.current_device(), 0 if dtype is torch.float16 else 1, B, V)
 
 
 def apex4_sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, probs=None, workspace=None,

@@ -39,3 +39,6 @@ def test_binding_refuses(L):  # noqa: F811
         pk.apex4_sample(x, u)
     with pytest.raises(ValueError):
         pk.apex4_sample(x[0], u)
+    for dtype in (torch.bfloat16, torch.int32, "float16"):
+        with pytest.raises(TypeError):
+            pk.apex4_sample_workspace_size(2, 8, dtype)
