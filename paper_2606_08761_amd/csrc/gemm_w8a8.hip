@@ -73,8 +73,13 @@ __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 template <int N>
 __device__ __forceinline__ void landed_but() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 
-// WM x WN waves; NB: stages in LDS.
-template <int BM, int BN, int WM, int WN, int NB>
+// WM x WN waves; NB: stages in LDS.  AHEAD, for waves of one block and few of them on a compute
+// unit: a step's one product is over before the next step's fragments arrive, so those of a
+// whole stage are read at once while the stage before is multiplied.  With 64 x 32 tiles: 16
+// rows of 8192 channels, K 8192, 17.5 -> 16.1 us, 4112 channels of K 28672 50 -> 42; 64 rows of
+// 8192, bound by what a unit draws, 19.0 and 18.9.  Where several workgroups share a unit it
+// gives nothing (27 rows of 57344, 32 x 64 tiles: 92 and 96).
+template <int BM, int BN, int WM, int WN, int NB, bool AHEAD>
 __global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(const int8_t* __restrict__ A, const float* __restrict__ sa,
                                                                  const int8_t* __restrict__ W, const float* __restrict__ sw, int M,
                                                                  int N, int K, uint16_t* __restrict__ Y) {
@@ -136,62 +141,115 @@ __global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(const int8_t* _
     uint32_t at[KK];
 #pragma unroll
     for (int k = 0; k < KK; ++k) at[k] = ((2 * k + lh) ^ swizzle(l32)) * 16;
-    i32x4 fa[2][MI], fb[2][NI];
-    auto read = [&](int i, int set, int buffer, int k) {
-        if (i < NI) fb[set][i] = read_lds(rowB + buffer * kBuf + i * 32 * kStage + at[k]);
-        else fa[set][i - NI] = read_lds(rowA + buffer * kBuf + (i - NI) * 32 * kStage + at[k]);
-    };
-    // Products first .. last of a step with the fragments of `set`, and among them, evenly,
-    // the reads of the next step's into the other set and loads from .. to of stage t.
-    auto step = [&](auto tail, int first, int last, int set, int buffer, int k, int from, int to, int t) {
-        constexpr int R = MI + NI;
-        const int P = last - first, loads = to - from;
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (k >= 0) {
-#pragma unroll
-                for (int i = p * R / P; i < (p + 1) * R / P; ++i) read(i, set ^ 1, buffer, k);
-            }
-#pragma unroll
-            for (int i = from + p * loads / P; i < from + (p + 1) * loads / P; ++i) fetch(tail, i, t);
-            const int n = (first + p) % NI, m = (first + p) / NI;
-            acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[set][n], fa[set][m], acc[n][m], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-
-    constexpr int L = LA + LB, kFirst = (L + 1) / 2, P = MI * NI, kHalf = P / 2;
+    constexpr int L = LA + LB;
     const std::true_type yes;
     const std::false_type no;
-    for (int t = 0; t < NB; ++t) {
+    if constexpr (AHEAD) {
+        static_assert(MI * NI == 1 && KK % 2 == 0 && (NB - 1) * L < 64, "one block, a count that the wait can hold");
+        i32x4 f[2][2][KK];
+        i32x16 odd;  // every other step's sums: a product does not wait for the one before
 #pragma unroll
-        for (int i = 0; i < L; ++i)
-            if (t < NB - 1 || i < kFirst) fetch(yes, i, t);
-    }
-    landed_but<(NB - 2) * L + kFirst>();
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+        for (int i = 0; i < 16; ++i) odd[i] = 0;
+        auto read = [&](int set, int buffer) {
 #pragma unroll
-    for (int i = 0; i < MI + NI; ++i) read(i, 0, 0, 0);
-    int b = 0;
-    // A stage: its steps but the last, half of that one's products, and then, when all of
-    // the stage is read and the next one has landed, for every wave past the barrier, the
-    // other half beside the next stage's first reads and the loads into the buffer that
-    // became free.  (Products wait for neither: their fragments are there.)
-    auto stage = [&](auto tail, int s) {
-        const int b1 = b + 1 == NB ? 0 : b + 1;
+            for (int k = 0; k < KK; ++k) {
+                f[set][0][k] = read_lds(rowB + buffer * kBuf + at[k]);
+                f[set][1][k] = read_lds(rowA + buffer * kBuf + at[k]);
+            }
+        };
+        auto fetch_all = [&](auto tail, int t) {
 #pragma unroll
-        for (int k = 0; k < KK - 1; ++k) step(tail, 0, P, k & 1, b, k + 1, kFirst, k == 0 ? L : kFirst, s + NB - 1);
-        step(tail, 0, kHalf, (KK - 1) & 1, b, -1, 0, 0, 0);
-        landed_but<(NB - 2) * L>();
+            for (int i = 0; i < L; ++i) fetch(tail, i, t);
+        };
+        for (int t = 0; t < NB; ++t) fetch_all(yes, t);
+        landed_but<(NB - 1) * L>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        step(tail, kHalf, P, (KK - 1) & 1, b1, 0, 0, kFirst, s + NB);  // behind the last stage the reads are of what the buffer holds, not used
-        b = b1;
-    };
-    int s = 0;
-    for (; s < stages - NB - 1; ++s) stage(no, s);
-    for (; s < stages; ++s) stage(yes, s);
+        read(0, 0);
+        int b = 0;
+        // all of stage s is in registers, the next one has landed; stage s + NB takes its buffer
+        auto stage = [&](auto tail, int set, int s) {
+            b = b + 1 == NB ? 0 : b + 1;
+            landed_but<(NB - 2) * L>();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            read(set ^ 1, b);  // behind the last stage what the buffer holds, not used
+            fetch_all(tail, s + NB);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < KK; k += 2) {
+                acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[set][0][k], f[set][1][k], acc[0][0], 0, 0, 0);
+                odd = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[set][0][k + 1], f[set][1][k + 1], odd, 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int s = 0;
+        for (; s + 2 + NB < stages; s += 2) {  // stages up to s + 1 + NB are whole
+            stage(no, 0, s);
+            stage(no, 1, s + 1);
+        }
+        for (; s < stages; s += 2) {
+            stage(yes, 0, s);
+            if (s + 1 < stages) stage(yes, 1, s + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[0][0][i] += odd[i];
+    } else {
+        i32x4 fa[2][MI], fb[2][NI];
+        auto read = [&](int i, int set, int buffer, int k) {
+            if (i < NI) fb[set][i] = read_lds(rowB + buffer * kBuf + i * 32 * kStage + at[k]);
+            else fa[set][i - NI] = read_lds(rowA + buffer * kBuf + (i - NI) * 32 * kStage + at[k]);
+        };
+        // Products first .. last of a step with the fragments of `set`, and among them, evenly,
+        // the reads of the next step's into the other set and loads from .. to of stage t.
+        auto step = [&](auto tail, int first, int last, int set, int buffer, int k, int from, int to, int t) {
+            constexpr int R = MI + NI;
+            const int P = last - first, loads = to - from;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (k >= 0) {
+#pragma unroll
+                    for (int i = p * R / P; i < (p + 1) * R / P; ++i) read(i, set ^ 1, buffer, k);
+                }
+#pragma unroll
+                for (int i = from + p * loads / P; i < from + (p + 1) * loads / P; ++i) fetch(tail, i, t);
+                const int n = (first + p) % NI, m = (first + p) / NI;
+                acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[set][n], fa[set][m], acc[n][m], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+
+        constexpr int kFirst = (L + 1) / 2, P = MI * NI, kHalf = P / 2;
+        for (int t = 0; t < NB; ++t) {
+#pragma unroll
+            for (int i = 0; i < L; ++i)
+                if (t < NB - 1 || i < kFirst) fetch(yes, i, t);
+        }
+        landed_but<(NB - 2) * L + kFirst>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < MI + NI; ++i) read(i, 0, 0, 0);
+        int b = 0;
+        // A stage: its steps but the last, half of that one's products, and then, when all of
+        // the stage is read and the next one has landed, for every wave past the barrier, the
+        // other half beside the next stage's first reads and the loads into the buffer that
+        // became free.  (Products wait for neither: their fragments are there.)
+        auto stage = [&](auto tail, int s) {
+            const int b1 = b + 1 == NB ? 0 : b + 1;
+#pragma unroll
+            for (int k = 0; k < KK - 1; ++k) step(tail, 0, P, k & 1, b, k + 1, kFirst, k == 0 ? L : kFirst, s + NB - 1);
+            step(tail, 0, kHalf, (KK - 1) & 1, b, -1, 0, 0, 0);
+            landed_but<(NB - 2) * L>();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            step(tail, kHalf, P, (KK - 1) & 1, b1, 0, 0, kFirst, s + NB);  // behind the last stage the reads are of what the buffer holds, not used
+            b = b1;
+        };
+        int s = 0;
+        for (; s < stages - NB - 1; ++s) stage(no, s);
+        for (; s < stages; ++s) stage(yes, s);
+    }
     landed_but<0>();  // LDS is no longer written when the workgroup gives it back
 
     // lane: token m, channels n .. n + 3 of each i / 4
@@ -224,11 +282,11 @@ __global__ __launch_bounds__(64 * WM * WN) void w8a8_tile_kernel(const int8_t* _
     }
 }
 
-template <int BM, int BN, int WM, int WN, int NB>
+template <int BM, int BN, int WM, int WN, int NB, bool AHEAD = false>
 hipError_t run_tile(const int8_t* A, const float* sa, const int8_t* W, const float* sw, int M, int N, int K, uint16_t* Y, hipStream_t st) {
     static std::atomic<uint64_t> done{0};
     constexpr int bytes = NB * (BM + BN) * kStage;
-    const auto k = w8a8_tile_kernel<BM, BN, WM, WN, NB>;
+    const auto k = w8a8_tile_kernel<BM, BN, WM, WN, NB, AHEAD>;
     const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(k), bytes, done);
     if (e != hipSuccess) return e;
     const int64_t tiles = static_cast<int64_t>((M + BM - 1) / BM) * ((N + BN - 1) / BN);
@@ -271,12 +329,12 @@ double cost_of(const Form& f, int64_t M, int64_t N, int64_t K, int cus) {
 
 // Up to 64 rows the weights' bytes bound the call: tiles of few rows, and as narrow as
 // still gives no compute unit more than one (8192 channels, 32 and 64 rows: 64 x 32 tiles
-// 17.7 and 19.2 us, 32 x 64 19.5 and 64 x 64 23.7; 57344 channels: 126 and 129, 89 and 99).
+// 16.5 and 18.9 us, 32 x 64 19.5 and 64 x 64 23.7; 57344 channels: 126 and 129, 89 and 99).
 hipError_t launch_w8a8_tiles(const int8_t* A, const float* sa, const int8_t* W, const float* sw, int M, int N, int K, uint16_t* Y,
                              hipStream_t st) {
     const int cus = device_cu_count();
     if (M <= 64) {
-        if ((N + 31) / 32 <= cus) return run_tile<64, 32, 2, 1, 6>(A, sa, W, sw, M, N, K, Y, st);
+        if ((N + 31) / 32 <= cus) return run_tile<64, 32, 2, 1, 6, true>(A, sa, W, sw, M, N, K, Y, st);
         if (M <= 32) return run_tile<32, 64, 1, 2, 6>(A, sa, W, sw, M, N, K, Y, st);
         return run_tile<64, 64, 2, 2, 5>(A, sa, W, sw, M, N, K, Y, st);
     }

@@ -110,6 +110,15 @@ def test_product(pk, M, N, K):
     assert same(pk.apex4_w8a8_gemm(dev(A), dev(sa), dev(W), dev(sw)), product(A, sa, W, sw))
 
 
+@pytest.mark.parametrize("K", [32, 128, 160, 256, 640, 736, 768, 800, 896, 928, 1024, 1056, 1152, 1280, 2080, 4128])
+def test_stages_of_narrow_tiles(pk, K):
+    """Fewer stages than buffers, as many, some more; even and odd counts, the last one whole or not."""
+    g = np.random.default_rng(K)
+    for M, N in ((33, 100), (64, 65), (9, 4130), (32, 4129)):
+        A, W, sa, sw = codes(g, M, K), codes(g, N, K), scales(g, M), scales(g, N)
+        assert same(pk.apex4_w8a8_gemm(dev(A), dev(sa), dev(W), dev(sw)), product(A, sa, W, sw))
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 64, 32), (1, 333, 8192), (1, 40, 28672), (1, 33, 32768), (1, 20, 32800), (2, 100, 1056), (20, 520, 544), (100, 333, 224)])
 def test_linear_is_the_two_calls(pk, M, N, K):
     g = np.random.default_rng(M + N + K)
