@@ -174,13 +174,14 @@ hipError_t run(const int8_t* A, const float* sa, const uint16_t* x, const int8_t
 
 }  // namespace
 
-// Up to 8 rows, and up to 32 where the tiles of 64 channels would leave three quarters of the compute
-// units idle (1024 channels, K 8192, 16 and 32 rows: 9.7 and 13.0 us, tiles 16.8 and 16.9).
+// Up to 8 rows, and up to 24 where no compute unit gets more than one workgroup (1024 channels,
+// K 8192, 16, 24 and 32 rows: 9.8, 12.7 and 14.6 us, tiles 14.6; 4096 of K 28672, 16, 24 and 32
+// rows: 29.4, 42.9 and 49.2, tiles 42.6 to 43.3).
 // One group of 16 channels a workgroup: two fill the chip with half as many waves (8 rows of
 // 8192 and 57344 channels: 15.9 and 87.8 us, two groups 19.8 and 102).
 bool w8a8_rows_fits(int64_t M, int64_t N) {
     if (N > 1 << 26) return false;  // a grid holds less than 2^32 threads
-    return M <= 8 || (M <= 32 && N <= 16 * static_cast<int64_t>(device_cu_count()));
+    return M <= 8 || (M <= 24 && N <= 16 * static_cast<int64_t>(device_cu_count()));
 }
 bool w8a8_fused_fits(int64_t M, int64_t N, int64_t K) { return M == 1 && N <= 1 << 26 && K <= kMostFused; }
 

@@ -354,3 +354,26 @@ def test_captured_and_on_another_stream(pk):
                 assert out[0].equal(eager[0])
             u.copy_(torch.rand(6, device="cuda"))
             p.mul_(0.9)
+
+
+@pytest.mark.parametrize("dtype,V", [(np.float16, 1000), (np.float16, 70001), (np.float32, 131072)])
+def test_two_streams_at_once(pk, dtype, V):
+    """Calls under way together have a workspace each."""
+    import torch
+    g = np.random.default_rng(V)
+    x = [dev(logits(g, 5, V, dtype)) for _ in range(2)]
+    u = [dev(g.random((20, 5)).astype(F32)) for _ in range(2)]
+    kw = ({"top_p": 0.9}, {"top_k": 40, "top_p": 0.8, "min_p": 0.01})
+    want = [[pk.apex4_sample(x[i], u[i][n], **kw[i]) for n in range(20)] for i in range(2)]
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    for s in sides:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for n in range(20):
+        for i in range(2):
+            got[i].append(pk.apex4_sample(x[i], u[i][n], stream=sides[i], **kw[i]))
+    for s in sides:
+        torch.cuda.current_stream().wait_stream(s)
+    for i in range(2):
+        for (a, b), (c, d) in zip(got[i], want[i]):
+            assert a.equal(c) and b.equal(d)

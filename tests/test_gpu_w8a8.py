@@ -111,10 +111,11 @@ def test_product(pk, M, N, K):
 
 
 @pytest.mark.parametrize("K", [32, 128, 160, 256, 640, 736, 768, 800, 896, 928, 1024, 1056, 1152, 1280, 2080, 4128])
-def test_stages_of_narrow_tiles(pk, K):
-    """Fewer stages than buffers, as many, some more; even and odd counts, the last one whole or not."""
+def test_stages_of_few_rows(pk, K):
+    """Fewer stages than buffers, as many, some more; even and odd counts, the last one whole or
+    not: of narrow tiles, and of weights streamed once."""
     g = np.random.default_rng(K)
-    for M, N in ((33, 100), (64, 65), (9, 4130), (32, 4129)):
+    for M, N in ((33, 100), (64, 65), (25, 70), (9, 4130), (32, 4129), (24, 333), (17, 4096), (8, 40)):
         A, W, sa, sw = codes(g, M, K), codes(g, N, K), scales(g, M), scales(g, N)
         assert same(pk.apex4_w8a8_gemm(dev(A), dev(sa), dev(W), dev(sw)), product(A, sa, W, sw))
 
