@@ -96,7 +96,9 @@ __global__ __launch_bounds__(kThreads) void w8a8_rows_kernel(const int8_t* __res
         const Scale sc = scale_of(am);
         s_token = sc.s;
         auto put = [&](int i, u32x4 t) {  // whole pieces: zeros behind K
-            if (i < pieces * (kPiece / 8)) *reinterpret_cast<u32x2*>(smem + 8 * i) = codes8(t, sc);
+            // (RARE's branch takes 12 registers and with them one workgroup of four: 32000 channels
+            // of K 4096 25.7 and 26.0 us)
+            if (i < pieces * (kPiece / 8)) *reinterpret_cast<u32x2*>(smem + 8 * i) = codes8<(SLOTS > 2)>(t, sc);
         };
         if constexpr (SLOTS <= 2) {
 #pragma unroll

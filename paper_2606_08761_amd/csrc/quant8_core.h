@@ -37,20 +37,35 @@ __device__ __forceinline__ int code_of(float x, const Scale& c) {
     return static_cast<int>(__builtin_amdgcn_fmed3f(q, -127.f, 127.f));
 }
 
+// Nearly always no quotient of the wave's is next to a border, and rint(x inv) is the code:
+// RARE looks once for all eight (4096 rows of 8192: 21.9 -> 18.4 us).
+template <bool RARE>
 __device__ __forceinline__ u32x2 codes8(u32x4 v, const Scale& c) {
     u32x2 out = {0u, 0u};
     if (c.inv == 0.f) return out;
+    auto all = [&](auto code) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        uint32_t b[4];
+        for (int i = 0; i < 2; ++i) {
+            uint32_t b[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t w = v[2 * i + (j >> 1)];
-            b[j] = static_cast<uint32_t>(code_of(h2f(j & 1 ? w >> 16 : w & 0xFFFFu), c));
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w = v[2 * i + (j >> 1)];
+                b[j] = static_cast<uint32_t>(code(h2f(j & 1 ? w >> 16 : w & 0xFFFFu)));
+            }
+            out[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u),
+                                           0x05040100u);
         }
-        out[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u),
-                                       0x05040100u);
+    };
+    if constexpr (RARE) {
+        float most = 0.f;
+        all([&](float x) {
+            const float q = rintf(x * c.inv);  // +-127 at most
+            most = fmaxf(most, fabsf(fmaf(-q, c.s, x)));
+            return static_cast<int>(q);
+        });
+        if (!__any(most >= 0.5f * c.s)) return out;
     }
+    all([&](float x) { return code_of(x, c); });
     return out;
 }
 

@@ -14,7 +14,8 @@
 // A row of zeros (or whose S is zero) gets zero codes; a row that holds an infinity or a
 // NaN gets a scale that is one and zero codes, so that its products are NaN.
 //
-// 4096 rows of 8192: 21 us (101 MB, 4.7 TB/s); 300 rows 6 us, 27 rows 5, a launch mostly.
+// 4096 rows of 8192: 18.4 us (101 MB, 5.5 TB/s); 300 rows 4.3 us, 16 rows 3.5, a launch mostly;
+// 16 rows of 28672 5.3.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -57,7 +58,7 @@ __global__ __launch_bounds__(T) void quant8_kernel(const uint16_t* __restrict__ 
 #pragma unroll
     for (int j = 0; j < U; ++j) {
         const int i = static_cast<int>(threadIdx.x) + j * T;
-        if (i < slots) qr[i] = codes8(v[j], sc);
+        if (i < slots) qr[i] = codes8<true>(v[j], sc);
     }
 }
 
@@ -73,7 +74,7 @@ hipError_t run(const uint16_t* x, int64_t M, int slots, int8_t* q, float* s, hip
 
 // K < 2^17: at most 16384 slots a row.  Two slots a thread keep more rows on a compute
 // unit than four do, one leaves its threads too little to load (4096 rows of 8192: 512
-// threads with two 21.4 us, 4.7 TB/s; 256 with four 24.2, 1024 with one 24.9; few rows: all alike).
+// threads with two 18.4 us, 5.5 TB/s; 256 with four 20.6, 1024 with one 21.2; 300 rows 4.3, 5.3 and 4.2).
 hipError_t launch_quantize8(const uint16_t* x, int64_t M, int64_t K, int8_t* q, float* s, hipStream_t st) {
     const int n = static_cast<int>(K / 8);
     if (n <= 64) return run<64, 1>(x, M, n, q, s, st);
