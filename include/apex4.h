@@ -472,9 +472,10 @@ int apex4_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
  * The values from rot on are copied.
  *   freq [rot / 2] binary64 (device, 8-byte aligned): how contexts are stretched is in
  *   these numbers (apex4_rope_freq of the Python binding makes them);
- *   mag: positive and finite.
+ *   mag: positive, 3.4e38 at most.
  *   positions [T] int32 (device), any values: a negative one turns back.
- * Angles are binary64, turned values binary32, rounded once to binary16.
+ * Angles, sines and their products with mag are binary64, rounded to binary32; both products
+ * and their sum are binary32, each rounded (no fma); the sum is rounded to binary16.
  *
  * apex4_rope: T rows of heads * head_dim binary16, x_stride and out_stride elements
  *   apart (multiples of 8; the heads of a fused projection's queries and keys are one
@@ -486,7 +487,7 @@ int apex4_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
 #define APEX4_ROPE_HALF 0
 #define APEX4_ROPE_INTERLEAVED 1
 int apex4_rope(const void* x, int64_t x_stride, const int32_t* positions, int64_t T, int64_t heads, int64_t head_dim,
-               const double* freq, int64_t rot, int layout, float mag, void* out, int64_t out_stride, void* stream);
+               const double* freq, int64_t rot, int layout, double mag, void* out, int64_t out_stride, void* stream);
 
 /*
  * apex4_kv_append with rotary positions on the way, in one launch: the keys are
@@ -499,7 +500,7 @@ int apex4_rope(const void* x, int64_t x_stride, const int32_t* positions, int64_
  */
 int apex4_kv_append_rope(const void* q, int64_t q_stride, int64_t heads, void* q_out, const void* k, int64_t k_stride,
                          const void* v, int64_t v_stride, const int32_t* q_start, int64_t T, const int32_t* positions,
-                         const double* freq, int64_t rot, int layout, float mag, void* k_pages, void* v_pages,
+                         const double* freq, int64_t rot, int layout, double mag, void* k_pages, void* v_pages,
                          int64_t n_pages, const int32_t* table, int64_t width, const int32_t* kv_len, int64_t B,
                          int64_t kv_heads, int64_t head_dim, int64_t page, int cache, void* stream);
 

@@ -89,7 +89,7 @@ def lib() -> ctypes.CDLL:
     L.apex4_w4a4_gemm_ws.argtypes = [P, P, P, P, I, I, I, I, P, P, I, P]
     L.apex4_w4a4_gemm_noalloc.argtypes = [P, P, P, P, I, I, I, I, P, P]
     L.apex4_w4a4_gemm_fp6.argtypes = [P, P, P, P, I, I, I, I, P, P]
-    C, F = ctypes.c_int, ctypes.c_float
+    C, F, D = ctypes.c_int, ctypes.c_float, ctypes.c_double
     L.apex4_kv_page_bytes.argtypes = [C, I, I, I, P]
     L.apex4_kv_append.argtypes = [P, I, P, I, P, I, P, P, I, P, I, P, I, I, I, I, C, P]
     L.apex4_kv_gather.argtypes = [P, P, I, P, I, P, I, I, I, I, C, P, I, P, P, P]
@@ -103,8 +103,8 @@ def lib() -> ctypes.CDLL:
     L.apex4_pages_free.argtypes = [P, I, I, P, P, I, P, I, P]
     L.apex4_pages_compact.argtypes = [P, I, I, P, I, I, P, I, P, P, I, P]
     L.apex4_pages_copy.argtypes = [P, I, I, I, P, P, I, P]
-    L.apex4_rope.argtypes = [P, I, P, I, I, I, P, I, C, F, P, I, P]
-    L.apex4_kv_append_rope.argtypes = [P, I, I, P, P, I, P, I, P, I, P, P, I, C, F, P, P, I, P, I, P, I, I, I, I, C, P]
+    L.apex4_rope.argtypes = [P, I, P, I, I, I, P, I, C, D, P, I, P]
+    L.apex4_kv_append_rope.argtypes = [P, I, I, P, P, I, P, I, P, I, P, P, I, C, D, P, P, I, P, I, P, I, I, I, I, C, P]
     L.apex4_quantize_act8.argtypes = [P, I, I, P, P, P]
     L.apex4_w8a8_gemm.argtypes = [P, P, P, P, I, I, I, P, P]
     L.apex4_w8a8_linear.argtypes = [P, P, P, I, I, I, P, P, P, P]

@@ -81,10 +81,10 @@ bool overlap(const void* x, int64_t x_stride, int64_t n, const void* out, int64_
     return d < n || d + out_n > x_stride;
 }
 
-int make_rotary(Rotary& r, const double* freq, int64_t D, int64_t rot, int layout, float mag) {
+int make_rotary(Rotary& r, const double* freq, int64_t D, int64_t rot, int layout, double mag) {
     if (rot < 2 || rot > D || rot % 2 != 0) return APEX4_ERR_SHAPE;
     if (layout != APEX4_ROPE_HALF && layout != APEX4_ROPE_INTERLEAVED) return APEX4_ERR_SHAPE;
-    if (!(mag > 0.f) || mag > 3.4e38f) return APEX4_ERR_SHAPE;
+    if (!(mag > 0.0) || mag > 3.4e38) return APEX4_ERR_SHAPE;
     r.freq = freq;
     r.mag = mag;
     r.rot = static_cast<int>(rot);
@@ -180,7 +180,7 @@ int apex4_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
 }
 
 int apex4_rope(const void* x, int64_t x_stride, const int32_t* positions, int64_t T, int64_t heads, int64_t head_dim,
-               const double* freq, int64_t rot, int layout, float mag, void* out, int64_t out_stride, void* stream) {
+               const double* freq, int64_t rot, int layout, double mag, void* out, int64_t out_stride, void* stream) {
     if (!present(x, T) || !present(positions, T) || !freq || !present(out, T)) return APEX4_ERR_NULL;
     Rotary r;
     if (heads < 1 || heads > 65536 || head_dim < 8 || head_dim > 512 || head_dim % 8 != 0) return APEX4_ERR_SHAPE;
@@ -199,7 +199,7 @@ int apex4_rope(const void* x, int64_t x_stride, const int32_t* positions, int64_
 
 int apex4_kv_append_rope(const void* q, int64_t q_stride, int64_t heads, void* q_out, const void* k, int64_t k_stride,
                          const void* v, int64_t v_stride, const int32_t* q_start, int64_t T, const int32_t* positions,
-                         const double* freq, int64_t rot, int layout, float mag, void* k_pages, void* v_pages,
+                         const double* freq, int64_t rot, int layout, double mag, void* k_pages, void* v_pages,
                          int64_t n_pages, const int32_t* table, int64_t width, const int32_t* kv_len, int64_t B,
                          int64_t kv_heads, int64_t head_dim, int64_t page, int cache, void* stream) {
     const int64_t queries = heads == 0 ? 0 : T;

@@ -7,9 +7,8 @@
 // are shared by all heads of a token.  A lane holds both values of each of its
 // pairs before it writes either, which is what lets a row be turned in place.
 // Bound by memory (4 bytes a value moved, 3 operations): 8192 tokens of 72 heads of 128 take 63
-// us (302 MB, 4.8 TB/s), 4001 of 40 heads of 64, interleaved, 9.9 (41 MB, 4.2 TB/s), 16
-// tokens of 72 heads 3.8, the launch and one chain of loads.  Binary64 for sines and
-// products costs none of it (62.8 us with binary32).
+// us (302 MB, 4.8 TB/s), 4001 of 40 heads of 64, interleaved, 9.3 (41 MB, 4.4 TB/s), 16
+// tokens of 72 heads 3.8, the launch and one chain of loads.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 

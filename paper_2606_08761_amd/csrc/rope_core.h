@@ -5,11 +5,14 @@
 // the pair is (j, j + rot / 2) in the half layout and (2 j, 2 j + 1) in the
 // interleaved one, and the values from rot on stay.  A position of any sign and size
 // has its angle: the turns are a binary64 product, and only what is left past whole
-// turns (exact) goes into the sine.  Sine, cosine and the turned values are binary64
-// (which the kernels, bound by memory, have the time for), rounded to binary32 and then
-// to binary16: a quarter as many results next to a border fall to its other side as with
-// binary32 sines and products, and a 4-bit code on the way into a cache is decided by
-// such results.  In binary32 the angle of position 10^6 would be off by 2^-5 of a radian.
+// turns (exact) goes into the sine.  (In binary32 the angle of position 10^6 would be off
+// by 2^-5 of a radian.)
+//
+// Roundings: cos and sin times mag (binary64) to binary32; each product and their sum to
+// binary32, which is what elementary operations in that type give, bit for bit; then to
+// binary16.  No fma, which drops one of the products' roundings: a value in ten thousand
+// would be another, and a 4-bit code on the way into a cache is decided by such values.  The
+// result is 2^-11 of itself and 2^-22 of |a| + |b| off at most.
 #pragma once
 
 #include <hip/hip_fp16.h>
@@ -40,28 +43,22 @@ __host__ __device__ inline int form_of(const Rotary& r, int D) {
 }
 
 // (cos, sin) of pair j at position p, times mag.
-typedef double Turn __attribute__((ext_vector_type(2)));
+typedef float Turn __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ Turn turn_of(const Rotary& r, int p, int j) {
     const double t = static_cast<double>(p) * r.freq[j];
     double s, c;
     sincospi(2.0 * (t - rint(t)), &s, &c);
-    return Turn{c * r.mag, s * r.mag};
+    return Turn{static_cast<float>(c * r.mag), static_cast<float>(s * r.mag)};
 }
 
-// One order of operations for every kernel, so that their results are the same bits.
-// The compiler may join the two roundings into one, here and not there; the empty
-// statement keeps them apart.
-__device__ __forceinline__ float apart(double x) {
-    float y = static_cast<float>(x);
-    asm("" : "+v"(y));
-    return y;
+// The compiler may join a product and the sum, or the sum and its rounding to binary16,
+// into one instruction that rounds once; the empty statement keeps them apart.
+__device__ __forceinline__ float apart(float x) {
+    asm("" : "+v"(x));
+    return x;
 }
-__device__ __forceinline__ float first_of(float a, float b, Turn t) {
-    return apart(fma(static_cast<double>(a), t.x, -(static_cast<double>(b) * t.y)));
-}
-__device__ __forceinline__ float second_of(float a, float b, Turn t) {
-    return apart(fma(static_cast<double>(b), t.x, static_cast<double>(a) * t.y));
-}
+__device__ __forceinline__ float first_of(float a, float b, Turn t) { return apart(apart(a * t.x) - apart(b * t.y)); }
+__device__ __forceinline__ float second_of(float a, float b, Turn t) { return apart(apart(b * t.x) + apart(a * t.y)); }
 
 // The pieces (of 8 values) of lane l of a head.
 template <int FORM>
