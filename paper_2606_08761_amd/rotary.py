@@ -14,7 +14,7 @@ from .cache import _empty, _freq, _layout, _one_device, _output, _ptr, _rows
 
 
 def apex4_rope_freq(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: int = 8192,
-                    low: float = 1.0, high: float | None = None, device="cuda"):
+                    low: float = 1.0, high: float | None = None, device="cuda", whole_pairs: bool = True):
     """(freq, mag): whole turns a position of each of the rot / 2 pairs, float64 [rot / 2],
     and the factor of the turned values.  Unscaled, pair j turns base^(-2 j / rot) radians.
 
@@ -23,7 +23,10 @@ def apex4_rope_freq(rot: int, base: float = 10000.0, scaling: str = "none", fact
       "ntk"     the base grows so that the slowest pair turns factor times slower;
       "yarn"    pairs that turn more than ``high`` (32) times in ``trained`` positions stay,
                 those below ``low`` times are slowed, a ramp over the pairs' numbers
-                between; mag = 0.1 ln(factor) + 1;
+                between; mag = 0.1 ln(factor) + 1.  The ramp goes from a whole pair to a
+                whole pair, the first number rounded down (0 at least) and the last one up
+                (rot - 1 at most), as checkpoints that were trained so expect;
+                whole_pairs=False: from and to the very numbers;
       "bands"   the same by the number of turns, from ``high`` (4) down to ``low``."""
     torch = _torch()
     if rot < 2 or rot % 2:
@@ -42,6 +45,10 @@ def apex4_rope_freq(rot: int, base: float = 10000.0, scaling: str = "none", fact
             raise ValueError("high must be above low, and low above 0")
         if scaling == "yarn":
             first, last = (n * math.log(trained / (turns * 2 * math.pi)) / math.log(base) for turns in (high, low))
+            if whole_pairs:
+                first, last = math.floor(first), math.ceil(last)
+                if max(first, 0) < min(last, rot - 1):  # else every pair is on one side
+                    first, last = max(first, 0), min(last, rot - 1)
             keep = 1.0 - ((j - first) / (last - first)).clamp(0.0, 1.0)
             mag = 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
         else:

@@ -93,3 +93,32 @@ def test_frequencies(rot, base):
     if rot > 2:  # the slowest pair turns factor times slower, the fastest as before
         n = pk.apex4_rope_freq(rot, base, "ntk", 8.0, device="cpu")[0]
         assert n[0] == plain[0] and float(n[-1]) == pytest.approx(plain[-1] / 8, rel=1e-12)
+
+
+@pytest.mark.parametrize("rot,base,trained,kw,kept", [
+    # the ramp's ends: 20.94 and 45.03, so 20 and 46
+    (128, 10000.0, 4096, {}, {20: 1, 21: 25 / 26, 30: 16 / 26, 33: 0.5, 45: 1 / 26, 46: 0}),
+    (128, 10000.0, 8192, {}, {25: 1, 30: 0.8, 49: 0.04, 50: 0}),                          # 25.76 and 49.84
+    (64, 500000.0, 4096, {}, {7: 1, 10: 2 / 3, 15: 1 / 9, 16: 0}),                        # 7.35 and 15.80
+    (64, 10000.0, 100, {}, {0: 1, 1: 0.9, 5: 0.5, 10: 0}),                                # -2.43 and 9.61
+    (8, 100.0, 16384, dict(high=1000.0, low=0.5), {0: 1, 1: 6 / 7, 3: 4 / 7}),            # 0.83 and 7.43: 7 at most
+    (64, 10000.0, 4, {}, {0: 0, 1: 0, 31: 0}),                                            # all turn less than once
+    (8, 10000.0, 1 << 40, {}, {0: 1, 1: 1, 3: 1}),                                        # all turn more than 32 times
+    (128, 10000.0, 4096, dict(whole_pairs=False),  # from 20.944482 to 45.026881
+     {20: 1, 21: 1 - 0.055518 / 24.0824, 33: 1 - 12.055518 / 24.0824, 45: 0.026881 / 24.0824, 46: 0})])
+def test_yarn_ramp(rot, base, trained, kw, kept):
+    """Pairs between the ramp's ends, worked out by hand: kept shares, the rest 8 times slower."""
+    import paper_2606_08761_amd as pk
+    f = pk.apex4_rope_freq(rot, base, "yarn", 8.0, trained, device="cpu", **kw)[0]
+    for j, keep in kept.items():
+        plain = base ** (-2 * j / rot) / (2 * math.pi)
+        assert float(f[j]) == pytest.approx(plain * (keep + (1 - keep) / 8), rel=1e-6 if "whole_pairs" in kw else 1e-12), j
+
+
+def test_bands_ramp():
+    """Pairs that turn 2.5 and 1.25 times: (2.5 - 1) / 3 and 0.25 / 3 kept."""
+    import paper_2606_08761_amd as pk
+    f, mag = pk.apex4_rope_freq(4, 4.0, "bands", 8.0, 2.5 * 2 * math.pi, device="cpu")
+    assert mag == 1.0
+    for j, keep in ((0, 0.5), (1, 1 / 12)):
+        assert float(f[j]) == pytest.approx(0.5 ** j / (2 * math.pi) * (keep + (1 - keep) / 8), rel=1e-12)
