@@ -144,7 +144,7 @@ struct Row {
     int skip, V, pieces;   // logits between base and the first; pieces that hold the row
     int from, to;          // the pieces that the passes go over
     bool infinite;         // the largest logit is infinite: its like count as 0, the others as nothing
-    float half, c32;
+    float scale, scaled, c32;  // below() is the scaled difference times c32
     double max, c64;       // 512 c
 
     static constexpr uint32_t kNone = F16 ? 0xFC00FC00u : 0xFF800000u;  // -infinity
@@ -219,9 +219,9 @@ struct Row {
     }
     __device__ __forceinline__ int part() const { return (pieces + kWaves - 1) / kWaves; }  // pieces of a part of the row
 
-    // 1/16 octaves below the largest: rises as x falls (halves, whose difference cannot
-    // overflow).  NaN and -infinity are not below kBuckets: they are not live.
-    __device__ __forceinline__ float below(float x) const { return fmaf(-0.5f, x, half) * c32; }
+    // 1/16 octaves below the largest: rises as x falls.  NaN and -infinity are not below
+    // kBuckets: they are not live.
+    __device__ __forceinline__ float below(float x) const { return fmaf(-scale, x, scaled) * c32; }
     __device__ __forceinline__ static bool live(float y) { return y < static_cast<float>(kBuckets); }
     // 2^45 2^((x - max) c), the power not below -60, in binary64: 512 (x - max) c = k + f, |f| <=
     // 1/2, the table's 2^(k % 512 / 512), a power of two (which only adds to its exponent), and
@@ -752,9 +752,13 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
     }
     const double c = 1.4426950408889634074 / static_cast<double>(t);
     row.max = m;
-    row.half = 0.5f * m;
     row.c64 = kSteps * c;
-    row.c32 = fminf(static_cast<float>(32.0 * c), 3.4e38f);  // 0 times it is 0
+    // Halves, whose difference cannot overflow.  A temperature below some 2^-120 would take their
+    // factor past binary32 and logits thousands of octaves down for live ones; there the differences
+    // that count are small numbers and are made larger, unless the largest logit's next is far below it anyhow.
+    row.scale = c >= 0x1p120 && fabsf(m) < 0x1p60f ? 0x1p60f : 0.5f;
+    row.scaled = row.scale * m;
+    row.c32 = fminf(static_cast<float>(16.0 * c / row.scale), 3.4e38f);  // 0 times it is 0
 
     // 2, 3: the border
     const bool by_k = k > 1 && k < a.V, by_p = p < 1.f;

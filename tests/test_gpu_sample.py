@@ -377,3 +377,24 @@ def test_two_streams_at_once(pk, dtype, V):
     for i in range(2):
         for (a, b), (c, d) in zip(got[i], want[i]):
             assert a.equal(c) and b.equal(d)
+
+
+@pytest.mark.parametrize("V", [600, 50001, 131072])
+@pytest.mark.parametrize("t", [1e-45, 3e-43, 1e-40, 5e-38, 1e-36, 2e-36])
+def test_borders_at_the_smallest_temperatures(pk, V, t):
+    """Logits some octaves of the weight apart, and hundreds to millions of octaves down, whose
+    weight is nothing, all as small as such a temperature makes them; then with a largest logit that
+    has no neighbour so near."""
+    g = np.random.default_rng(V)
+    B = 6
+    u = ((np.arange(B) + g.random(B)) / B).astype(F32)
+    near, far = g.random((B, V)) * 45 * t, 10.0 ** (g.random((B, V)) * 7 + 2) * t
+    x = -np.where(g.random((B, V)) < 0.3, near, far).astype(F32)
+    x[:, V // 2] = x[:, V // 3] = 0.0
+    x[1] += F32(30 * t)    # the largest above and below 0
+    x[2] -= F32(200 * t)
+    x[3, V // 5:] = -np.inf
+    x[4, V // 7] = 5.0     # nothing else counts
+    x[5, ::2] = -3e38
+    for kw in (dict(), dict(p=0.3), dict(p=0.9), dict(k=30), dict(k=V // 4), dict(k=V // 2, p=0.95), dict(least=1e-3), dict(p=0.99, least=0.05), dict(k=20, p=0.8)):
+        check(pk, x, u, t=float(F32(t)), **kw)
