@@ -842,9 +842,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, uint32_t
 
     // 4: the token.  The weight of a logit if it is kept, or 0: above `low`, and not one of
     // those equal to the border's that come after its last.
-    // Where no border is, what is 50 octaves below the largest (rounded anyhow: 46 to 60
-    // would do) stays out, and what is no number.
-    const float dead = fminf(m - static_cast<float>(50.0 / c), under(ordered(m)));
+    // Where no border is, what is 100 octaves below the largest stays out (46 to 1000 would do:
+    // a difference of few steps of binary32 is rounded by half a step), and what is no number.
+    const float dead = fminf(m - static_cast<float>(100.0 / c), under(ordered(m)));
     const float low = border.key ? under(border.key) : dead;
     const float tied = border.last < a.V ? unordered(border.key) : __builtin_nanf("");
     auto kept = [&](float x, int i) -> u64 {

@@ -398,3 +398,17 @@ def test_borders_at_the_smallest_temperatures(pk, V, t):
     x[5, ::2] = -3e38
     for kw in (dict(), dict(p=0.3), dict(p=0.9), dict(k=30), dict(k=V // 4), dict(k=V // 2, p=0.95), dict(least=1e-3), dict(p=0.99, least=0.05), dict(k=20, p=0.8)):
         check(pk, x, u, t=float(F32(t)), **kw)
+
+
+@pytest.mark.parametrize("V", [2, 5000, 70000])
+def test_the_last_octaves_that_count(pk, V):
+    """Neighbours of the largest logit whose weight is 2^-30 to 2^-45 of its own are kept, however few
+    steps of binary32 that is: u from 1 on takes the last kept one."""
+    for m, step in ((1e8, 8.0), (1.0, 2.0 ** -24), (-(2.0 ** 20), 2.0 ** -3)):
+        for steps in (1, 2, 3, 7):
+            for octaves in (30.0, 34.0, 41.7, 44.5):
+                x = np.full((1, V), m - 1e6 * step, F32)
+                x[0, 0], x[0, -1] = m, m - steps * step
+                t = steps * step * np.log2(np.e) / octaves
+                for kw in (dict(), dict(least=2e-14)):
+                    check(pk, x, [1.0], t=float(F32(t)), **kw)
