@@ -200,7 +200,7 @@ struct SampleArgs {
     float temperature_all = 1.f, top_p_all = 1.f, min_p_all = 0.f;
 };
 // Bytes for workgroups that share long rows, where the rows are few (0: none do).
-int64_t sample_workspace(int64_t B, int64_t V, bool f16);
+int64_t sample_workspace(int64_t B, int64_t V);
 hipError_t launch_sample(const SampleArgs& a, int64_t B, bool f16, hipStream_t stream);
 
 // A paged key-value cache as the kernels see it (layout: kv_cache.h).

@@ -22,7 +22,7 @@ extern "C" int apex4_sample_workspace_size(int type, int64_t B, int64_t V, int64
     if (!bytes) return APEX4_ERR_NULL;
     int rc = check_shape(type, B, V);
     if (rc || (rc = apex4::check_device())) return rc;
-    *bytes = apex4::sample_workspace(B, V, type == APEX4_LOGITS_FP16);
+    *bytes = apex4::sample_workspace(B, V);
     return APEX4_OK;
 }
 
@@ -39,7 +39,7 @@ extern "C" int apex4_sample(const void* logits, int type, int64_t stride, int64_
         return APEX4_ERR_ALIGN;
     if ((rc = apex4::check_device())) return rc;
     if (B == 0) return APEX4_OK;
-    const int64_t need = apex4::sample_workspace(B, V, type == APEX4_LOGITS_FP16);
+    const int64_t need = apex4::sample_workspace(B, V);
     if (need > 0 && (!workspace || workspace_bytes < need)) return APEX4_ERR_WORKSPACE;
     apex4::SampleArgs a;
     a.logits = logits;

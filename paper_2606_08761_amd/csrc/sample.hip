@@ -1005,13 +1005,13 @@ hipError_t run_shared(const SampleArgs& a, int64_t B, hipStream_t st) {
 // shared: 131072 binary32 logits 1 row 86 and 43, 32 rows 89 and 64, 64 rows 88 and 96;
 // 65000 of binary16 1 row 48 and 37, 16 rows 54 and 46, 32 rows 52 and 57; 32000 1 row 23 and
 // 26, 32 rows 34 and 54.
-int64_t sample_workspace(int64_t B, int64_t V, bool) {
+int64_t sample_workspace(int64_t B, int64_t V) {
     const bool shared = B > 0 && V >= kSharedLogits && B * kWaves * kSharedLogits <= device_cu_count() * V;
     return shared ? B * static_cast<int64_t>(sizeof(Work)) : 0;
 }
 
 hipError_t launch_sample(const SampleArgs& a, int64_t B, bool f16, hipStream_t stream) {
-    if (sample_workspace(B, a.V, f16)) return f16 ? run_shared<true>(a, B, stream) : run_shared<false>(a, B, stream);
+    if (sample_workspace(B, a.V)) return f16 ? run_shared<true>(a, B, stream) : run_shared<false>(a, B, stream);
     const int bytes = (a.V * (f16 ? 2 : 4) + 15) / 16 * 16 + 16;  // a row that begins inside a piece has one more
     if (bytes <= kStageBytes) return f16 ? run<true, true, kWhole>(a, B, bytes, stream) : run<false, true, kWhole>(a, B, bytes, stream);
     return f16 ? run<true, false, kWhole>(a, B, bytes, stream) : run<false, false, kWhole>(a, B, bytes, stream);
