@@ -408,9 +408,9 @@ int apex4_w4a4_gemm_mx_ws(const uint8_t* A_6, const uint8_t* e_a,
  *   127), taken on the exact quotient; a row whose s is zero gets zero codes, and one that
  *   holds an infinity or a NaN gets a scale that is one and zero codes.  Deterministic.
  *   The same call quantizes weights ([N, K] -> W_8, s_w).
- * apex4_w8a8_gemm: Y[m,n] = binary16(s_a[m] s_w[n] sum_k A_8[m,k] W_8[n,k]), the sum
- *   exact (int32), the products binary32, rounded once more to binary16.  A row's bits do
- *   not depend on the other rows.
+ * apex4_w8a8_gemm: Y[m,n] = binary16(s_a[m] s_w[n] sum_k A_8[m,k] W_8[n,k]): the sum is
+ *   exact (int32), rounded to binary32, times s_a[m] and then times s_w[n], each rounded to
+ *   binary32, and rounded to binary16.  A row's bits do not depend on the other rows.
  * apex4_w8a8_linear: both, Y bit for bit as after the two calls.  A_8_work [M, K] and
  *   s_a_work [M] are scratch (a single token is quantized on the way and leaves them alone).
  *
@@ -479,7 +479,8 @@ int apex4_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
  *
  * apex4_rope: T rows of heads * head_dim binary16, x_stride and out_stride elements
  *   apart (multiples of 8; the heads of a fused projection's queries and keys are one
- *   call).  out is x itself with the same stride, or overlaps it nowhere.
+ *   call).  out is x itself with the same stride, or overlaps it nowhere (of unequal strides
+ *   the whole ranges count, from the first row's first value to the last row's last one).
  *   head_dim: a multiple of 8, 8 to 512; rot even, 2 to head_dim; heads up to 65536, T
  *   up to 2^24, T heads up to 2^27.  Fastest where head_dim is a multiple of 16 and rot
  *   one of 16 (half) or 8 (interleaved).
@@ -495,7 +496,8 @@ int apex4_rope(const void* x, int64_t x_stride, const int32_t* positions, int64_
  * they are, and the queries are turned into q_out [T, heads, head_dim].  Cache and
  * q_out end up as after apex4_rope of queries and keys and apex4_kv_append, bit for bit.
  *   positions [T] int32, or NULL: each new token's own position in its sequence.
- *   heads == 0: no queries (q and q_out may be NULL).  q_out overlaps no input.
+ *   heads == 0: no queries (q and q_out may be NULL).  q_out overlaps none of q, k and v
+ *   (as above: where their strides are not heads * head_dim, the whole ranges count).
  * Rows of q_out behind the last sequence's are left as they were.
  */
 int apex4_kv_append_rope(const void* q, int64_t q_stride, int64_t heads, void* q_out, const void* k, int64_t k_stride,
@@ -628,9 +630,9 @@ int apex4_pages_copy(void* pool, int64_t planes, int64_t page_bytes, int64_t n_p
  *   temperature, top_k, top_p, min_p: [B] on the device, or NULL: the value beside it
  *   for every row.  u [B] binary32.
  *   tokens [B] int32, probs [B] binary32 or NULL (outputs).
- * Weights are binary64 and summed exactly, in units of 2^-45 of the largest: the outcome
- * is a function of the row and its settings alone.  Logits below 2^-46 of the largest
- * weight count as never chosen.
+ * Weights are binary64, rounded to whole units of 2^-45 of the largest and summed exactly: the
+ * outcome is a function of the row and its settings alone.  Logits below 2^-46 of the
+ * largest weight count as never chosen.
  *   workspace: apex4_sample_workspace_size bytes, 16-byte aligned (NULL where that is 0); calls
  *   that share one must be ordered on one stream.  Where rows are few and long,
  *   several workgroups share each.

@@ -5,10 +5,10 @@
 // A wave owns TM x TN outputs as 32 x 32 blocks of v_mfma_i32_32x32x32_i8 (weights the
 // rows, tokens the columns, so that a lane holds neighbouring channels of one token).  The
 // sums are whole numbers below 2^31 in any order (K is bounded), so outputs do not depend on
-// the tile: they are rounded twice, s_a s_w and the product, and then to binary16.
+// the tile: the sum to binary32, times s_a, times s_w, each rounded, and then to binary16.
 //
 // Many rows are bound by the matrix cores and the power that they draw: 4096 x 10240 of
-// K 8192 298 us, 2.3e15 operations a second at about 1.5 GHz; 8192^3 485 us with the matrix
+// K 8192 292 to 303 us, by card, 2.3e15 operations a second at about 1.5 GHz; 8192^3 485 us with the matrix
 // cores 0.70 busy.  Steps there: all loads in a burst behind the barrier 507 us (0.59 busy),
 // spread among the products 502 (0.64), no branches in the loop and the barrier in the
 // midst of the last step's products 485; stages of 64 bytes in four buffers 513, four waves
@@ -18,6 +18,7 @@
 // 40 (55 KB a us; 100 from a warm L2), its products and LDS reads alone 27 to 33.  No gain
 // from: four waves or eight, three to five buffers, fragments read a whole stage ahead, K
 // begun elsewhere by every tile; a wave that reads W ahead for the tiles that share it: 44 to 48.
+// Not tried: larger tiles that each take a part of K, with partial sums to be added.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -302,7 +303,7 @@ namespace {
 // The forms: us for K = 8192 of a tile alone on its compute unit with nearly all others idle,
 // and with all of them busy.  Tiles of 256 x 256 read the fewest bytes for their products, the
 // others are for counts of tiles that leave units idle (4096 x 10240: 2.5 rounds of 256 x 256
-// 357 us, 2 of 256 x 320 302; 300 x 57344: 128 x 256 200, 320 x 256 168; 1024 x 10240:
+// 333 to 357 us, 2 of 256 x 320 292 to 303; 300 x 57344: 128 x 256 200, 320 x 256 168; 1024 x 10240:
 // 256 x 256 109, 256 x 192 100; 3000 x 8192: 128 x 256 222, 192 x 256 210; 768 x 8192 of K
 // 28672: 128 x 256 200, 192 x 128 183; 200 x 8192: 128 x 128 39, 128 x 64 29).
 struct Form {
@@ -316,8 +317,9 @@ constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
 // Time of a form: whole rounds of a tile a unit, and a last one that takes the longer the more
 // units it keeps busy (clock and memory are shared); a tile starts in 5 us and goes over K
 // evenly.  For 70 to 4096 rows of 2048 to 57344 channels, K 4096 to 28672 (133 calls, each
-// form timed on each, weights from memory), what it picks takes 0.06 % longer than the
-// fastest form on average and 3 % at most, and 0.87 of the library's int8 product without scales.
+// form timed on each, weights from memory), what it picks takes 0.2 % longer than the
+// fastest form on average and 6 % at most (on the card that the forms' times are of 0.06 and 3
+// %), and 0.88 of the library's int8 product without scales.
 double cost_of(const Form& f, int64_t M, int64_t N, int64_t K, int cus) {
     const double tiles = static_cast<double>((M + f.bm - 1) / f.bm) * static_cast<double>((N + f.bn - 1) / f.bn);
     const double whole = static_cast<double>(static_cast<int64_t>(tiles / cus)), left = tiles / cus - whole, deep = static_cast<double>(K) / 8192.0;

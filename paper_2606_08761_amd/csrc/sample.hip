@@ -9,7 +9,8 @@
 //
 // Weights are computed in binary64 and held as whole numbers of 2^-45 of the largest
 // one: their sums are exact in any order, so that no result depends on which thread was
-// first, and a border moves by 2^-45 of a weight at most.  (In binary32 one row in some
+// first.  A weight is rounded by half such a unit, so running sums, and with them a border and the
+// token's share, are off by n 2^-46 of the largest weight at most for n logits.  (In binary32 one row in some
 // hundred of a flat distribution over 10^5 tokens would get another token.)  A logit 46
 // octaves below the largest weighs nothing.
 //
